@@ -376,6 +376,157 @@ stream_status stream_run_host_var(const stream_problem *p, const void *q_host, c
                                   const int32_t *k_row_host, int32_t *mask_host, void *out_host, float scale, void *staging,
                                   size_t staging_bytes, void *cuda_stream);
 
+/*
+ * ------------------------------------------------------------------------------------------------
+ * Dense attention, and the key-value cache of chains that are being generated: what the masks and the
+ * sparse pass above are set against, the layers that stay dense, and how the chains that are traced
+ * come about (one prompt, several chains forked from it, one token after the other).
+ * ------------------------------------------------------------------------------------------------
+ */
+
+/* Prompts packed one behind the other. Q is [total_q, n_q_heads, d], K and V are [total_k, n_kv_heads, d]
+ * (innermost stride 1, K and V share their strides). */
+typedef struct {
+    int32_t n_seqs;         /* >= 1 */
+    int32_t n_q_heads;      /* >= 1 */
+    int32_t n_kv_heads;     /* >= 1 and divides n_q_heads */
+    int32_t d;              /* 16, 32, 64, 128 or 256 */
+    int64_t total_q;        /* rows of Q and of the output, 0 .. 2^31 - 1 */
+    int64_t total_k;        /* rows of K and V, 0 .. 2^31 - 1 */
+    int32_t causal;         /* 1: a sequence's last query sees all its keys, the one before it all but the last, ...; 0: all see all */
+    int32_t dtype;          /* stream_dtype */
+    int64_t q_stride_t, q_stride_h, kv_stride_t, kv_stride_h; /* elements; a stride whose extent is 1 does not matter */
+} stream_prompt;
+
+/*
+ * Attention of whole prompts. Sequence s has the queries cu_q[s] .. cu_q[s+1] - 1 and the keys
+ * cu_k[s] .. cu_k[s+1] - 1; with n queries and m keys, query i sees the keys j <= i + m - n if causal
+ * (m > n: a prompt whose first part was computed before; m < n: the first n - m queries see nothing).
+ *     out[i, h] = sum_j softmax_j(scale q_i.k_j) v_j,     lse[h, i] = log sum_j exp(scale q_i.k_j)
+ * A query that sees nothing gets zeros and -inf. What K and V hold outside a query's own sequence, or beyond
+ * the last one, does not matter, whatever it is (NaN included); Q, K and V of the sequences must be finite.
+ *
+ *   q, k, v     device, read only
+ *   cu_q, cu_k  device int32 [n_seqs + 1], ascending; an entry outside 0 .. total_q (total_k), or below the one
+ *               before it, is taken as the nearest that is not
+ *   scale       logit scale; <= 0 selects 1/sqrt(d)
+ *   out         device, dtype of the problem, contiguous [total_q, n_q_heads, d]; rows of no sequence stay as they are
+ *   lse_out     device float32 [n_q_heads, total_q] or NULL; likewise
+ * Softmax statistics and the output accumulate in fp32.
+ */
+stream_status stream_prompt_attention(const stream_prompt *p, const void *q, const void *k, const void *v, const int32_t *cu_q,
+                                      const int32_t *cu_k, float scale, void *out, float *lse_out, void *cuda_stream);
+
+/* A paged key-value cache. Token t of the sequence in slot s lies in row t % page_size of page
+ * page_table[s][t / page_size]; K and V are each [n_layers, n_pages, page_size, n_kv_heads, d] with the
+ * strides below (in elements; innermost 1; K and V share them; any order of the dimensions).
+ *
+ * The ledger, three device arrays that all layers share and only the calls below change:
+ *   page_table  int32 [n_slots, max_pages]: a slot's first ceil(seq_len / page_size) entries are pages, the rest -1
+ *   seq_len     int32 [n_slots]: tokens, 0 = the slot is empty
+ *   ref_count   int32 [n_pages]: how many entries of the table name the page, 0 = it is free
+ * A new cache has -1, 0 and 0 everywhere. A page that is not full belongs to one slot alone (a fork copies it);
+ * full pages may be shared, and are not written again. The lowest-numbered free pages are taken first. */
+typedef struct {
+    int32_t n_slots;        /* >= 1; n_slots * max_pages < 2^31 */
+    int32_t n_pages;        /* 1 .. 2^30 */
+    int32_t page_size;      /* tokens; >= 1; max_pages * page_size < 2^31 */
+    int32_t max_pages;      /* >= 1 */
+    int32_t n_kv_heads;     /* >= 1 */
+    int32_t d;              /* 16, 32, 64, 128 or 256 */
+    int32_t n_layers;       /* >= 1 */
+    int32_t dtype;          /* stream_dtype */
+    int64_t stride_l, stride_p, stride_t, stride_h; /* layer, page, token, head; one whose extent is 1 does not matter */
+} stream_cache;
+
+/* Bytes of device workspace that the ledger calls (reserve, fork, free, compact) need; 0 = invalid cache. */
+size_t stream_cache_workspace_bytes(const stream_cache *c);
+
+/*
+ * The ledger calls. Each is done as a whole or not at all, and writes info_out, device int32 [4], 16-byte aligned:
+ *   [0] 1 = done, 0 = refused: nothing was changed
+ *   [1] pages taken (reserve, fork: and copies due), given back (free) or to be moved (compact); what it would
+ *       have taken where it was refused
+ *   [2] free pages after the call
+ *   [3] slots that the call has to refuse for (an index or a length out of range; see each call); free: entries of the
+ *       table or counts that cannot be, passed over
+ * workspace: device, 256-byte aligned, >= stream_cache_workspace_bytes(c); overwritten, nothing is kept in it. Calls on
+ * one cache, or with one workspace, must not overlap on the GPU.
+ *
+ * reserve: room for n_new[s] >= 0 more tokens in every slot s, and seq_len[s] grows by as many (their keys and
+ * values are then written with stream_cache_write, layer by layer). Refused if pages are missing, if an n_new is negative
+ * or if a row of the table would have to be longer than max_pages.
+ */
+stream_status stream_cache_reserve(const stream_cache *c, const int32_t *n_new, int32_t *page_table, int32_t *seq_len,
+                                   int32_t *ref_count, int32_t *info_out, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * fork: every slot s with parent[s] >= 0 becomes another chain with the tokens that slot parent[s] has: it shares
+ * the full pages, and a last page that is not full gets a copy of its own. The copies are due before
+ * anything is written: pairs_out, device int32 [n_slots, 2], 8-byte aligned, gets their {from, to}, by ascending s, then -1;
+ * hand it with info_out + 1 to stream_cache_copy_pages. (Where the call was refused all of it is -1.) Refused if pages are
+ * missing, if such a slot is not empty, if its parent is no slot, is itself to become a copy in this call, or has an
+ * impossible length.
+ */
+stream_status stream_cache_fork(const stream_cache *c, const int32_t *parent, int32_t *page_table, int32_t *seq_len,
+                                int32_t *ref_count, int32_t *pairs_out, int32_t *info_out, void *workspace, size_t workspace_bytes,
+                                void *cuda_stream);
+
+/* free: every slot s with done[s] != 0 is empty afterwards; pages that nobody names any more are free. Never refused. */
+stream_status stream_cache_free(const stream_cache *c, const int32_t *done, int32_t *page_table, int32_t *seq_len,
+                                int32_t *ref_count, int32_t *info_out, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * compact: with n pages in use, those of them with a number of n or more move to the free ones below n, the lowest to
+ * the lowest, so that 0 .. n - 1 are in use. pairs_out, device int32 [n_pages / 2, 2], 8-byte aligned: {from, to} by ascending
+ * number, then -1, for stream_cache_copy_pages (before anything is written or read).
+ */
+stream_status stream_cache_compact(const stream_cache *c, int32_t *page_table, int32_t *seq_len, int32_t *ref_count,
+                                   int32_t *pairs_out, int32_t *info_out, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * Copies whole pages, in all layers, of K and V: for i < *count (device; at most n_pairs) page pairs[i][0] to page
+ * pairs[i][1]. Pairs with a number outside the cache are passed over. No page may be written that another pair reads or
+ * writes. k_pages and v_pages are the caches' first elements.
+ */
+stream_status stream_cache_copy_pages(const stream_cache *c, void *k_pages, void *v_pages, const int32_t *pairs,
+                                      const int32_t *count, int32_t n_pairs, void *cuda_stream);
+
+/*
+ * Keys and values of new tokens into the pages of one layer, after stream_cache_reserve. The rows cu_new[s] ..
+ * cu_new[s+1] - 1 of k and v are the last tokens of slot s, up to seq_len[s] - 1. Rows of no slot, and tokens whose
+ * position or page cannot be, are passed over.
+ *   k, v     device, [total, n_kv_heads, d] with the strides given (elements, innermost 1); read only
+ *   cu_new   device int32 [n_slots + 1], ascending, clamped like cu_q
+ *   k_pages, v_pages  the caches' first elements (layer 0); written: layer `layer`
+ */
+stream_status stream_cache_write(const stream_cache *c, int32_t layer, const void *k, const void *v, int64_t total,
+                                 int64_t stride_t, int64_t stride_h, const int32_t *cu_new, const int32_t *page_table,
+                                 const int32_t *seq_len, void *k_pages, void *v_pages, void *cuda_stream);
+
+/*
+ * Attention of one new token of every slot over its cached tokens (its own among them, if it has been written):
+ *     out[s, h] = sum_{t < seq_len[s]} softmax_t(scale q_s.k_t) v_t,     lse[s, h] = log sum_t exp(scale q_s.k_t)
+ * An empty slot gets zeros and -inf. The tokens of all slots and heads are dealt evenly to the SMs, and pieces of a
+ * long slot are joined in a fixed order: the same call gives the same bits. What the pages hold beyond a slot's tokens
+ * does not matter (NaN included). Tokens whose page number is outside the cache are left out, and recorded:
+ * stream_read_stats(workspace, ...) then returns STREAM_ERR_DEVICE_CHECK with error = 701 and error_info = such a slot. A seq_len below 0
+ * counts as 0, one above max_pages * page_size as that.
+ *
+ *   n_q_heads   a multiple of n_kv_heads
+ *   q           device [n_slots, n_q_heads, d] with the strides given (elements, innermost 1); read only
+ *   scale       logit scale; <= 0 selects 1/sqrt(d)
+ *   out         device, dtype of the cache, contiguous [n_slots, n_q_heads, d]; overwritten
+ *   lse_out     device float32 [n_slots, n_q_heads] or NULL
+ *   workspace   device, 256-byte aligned, >= stream_decode_workspace_bytes(c, n_q_heads); overwritten, nothing is kept
+ *               in it but the record. Calls that can overlap on the GPU need one each.
+ */
+size_t stream_decode_workspace_bytes(const stream_cache *c, int32_t n_q_heads);  /* 0 = invalid */
+stream_status stream_decode_attention(const stream_cache *c, int32_t layer, int32_t n_q_heads, const void *q, int64_t q_stride_s,
+                                      int64_t q_stride_h, const void *k_pages, const void *v_pages, const int32_t *page_table,
+                                      const int32_t *seq_len, float scale, void *out, float *lse_out, void *workspace,
+                                      size_t workspace_bytes, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

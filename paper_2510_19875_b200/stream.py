@@ -5,6 +5,10 @@ CUDA tensors (or raw integer addresses) where the C side takes device pointers. 
 ``sparse_attention`` and ``run_host`` are conveniences that allocate outputs with torch and fill
 in the problem struct from tensor shapes and strides. PyTorch is used for device memory and
 streams only.
+
+Masks and the sparse attention on them: ``build_mask`` ... ``mask_difference``. Dense attention and the
+key-value cache of chains that are being generated: ``prompt_attention``, ``decode_attention``,
+``PagedCache`` and the ``cache_*`` functions.
 """
 from __future__ import annotations
 
@@ -40,6 +44,23 @@ class StreamProblem(ctypes.Structure):
 
 _PROBLEM = struct.Struct("@iiiqiiiiiiiqqqqqq")  # StreamProblem's fields with the C compiler's padding
 assert _PROBLEM.size == ctypes.sizeof(StreamProblem)
+
+
+class StreamPrompt(ctypes.Structure):
+    """``stream_prompt`` of stream.h."""
+
+    _fields_ = [("n_seqs", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("d", ctypes.c_int32),
+                ("total_q", ctypes.c_int64), ("total_k", ctypes.c_int64), ("causal", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("q_stride_t", ctypes.c_int64), ("q_stride_h", ctypes.c_int64), ("kv_stride_t", ctypes.c_int64),
+                ("kv_stride_h", ctypes.c_int64)]
+
+
+class StreamCache(ctypes.Structure):
+    """``stream_cache`` of stream.h."""
+
+    _fields_ = [("n_slots", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("d", ctypes.c_int32), ("n_layers", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("stride_l", ctypes.c_int64), ("stride_p", ctypes.c_int64), ("stride_t", ctypes.c_int64), ("stride_h", ctypes.c_int64)]
 
 
 class StreamStats(ctypes.Structure):
@@ -122,6 +143,27 @@ def _load():
     lib.stream_run_host.argtypes = [P, vp, vp, vp, vp, vp, ctypes.c_float, vp, sz, vp]
     lib.stream_run_host_var.restype = ctypes.c_int
     lib.stream_run_host_var.argtypes = [P, vp, vp, vp, vp, vp, vp, ctypes.c_float, vp, sz, vp]
+    PP, PC, i32, i64 = ctypes.POINTER(StreamPrompt), ctypes.POINTER(StreamCache), ctypes.c_int32, ctypes.c_int64
+    lib.stream_prompt_attention.restype = ctypes.c_int
+    lib.stream_prompt_attention.argtypes = [PP, vp, vp, vp, vp, vp, ctypes.c_float, vp, vp, vp]
+    lib.stream_cache_workspace_bytes.restype = sz
+    lib.stream_cache_workspace_bytes.argtypes = [PC]
+    lib.stream_cache_reserve.restype = ctypes.c_int
+    lib.stream_cache_reserve.argtypes = [PC, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.stream_cache_fork.restype = ctypes.c_int
+    lib.stream_cache_fork.argtypes = [PC, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.stream_cache_free.restype = ctypes.c_int
+    lib.stream_cache_free.argtypes = [PC, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.stream_cache_compact.restype = ctypes.c_int
+    lib.stream_cache_compact.argtypes = [PC, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.stream_cache_copy_pages.restype = ctypes.c_int
+    lib.stream_cache_copy_pages.argtypes = [PC, vp, vp, vp, vp, i32, vp]
+    lib.stream_cache_write.restype = ctypes.c_int
+    lib.stream_cache_write.argtypes = [PC, i32, vp, vp, i64, i64, i64, vp, vp, vp, vp, vp, vp]
+    lib.stream_decode_workspace_bytes.restype = sz
+    lib.stream_decode_workspace_bytes.argtypes = [PC, i32]
+    lib.stream_decode_attention.restype = ctypes.c_int
+    lib.stream_decode_attention.argtypes = [PC, i32, i32, vp, i64, i64, vp, vp, vp, vp, ctypes.c_float, vp, vp, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -269,6 +311,62 @@ def stream_run_host_var(p: StreamProblem, q_host, k_host, v_host, k_row_host, ma
     _raise(_load().stream_run_host_var(ctypes.byref(p), _addr(q_host), _addr(k_host), _addr(v_host), _addr(k_row_host),
                                        _addr(mask_host), _addr(out_host), float(scale), _addr(staging), staging_bytes,
                                        _stream_handle(stream)))
+
+
+def stream_prompt_attention(p: StreamPrompt, q, k, v, cu_q, cu_k, scale: float, out, lse_out, stream=None) -> None:
+    """Dense attention of packed prompts."""
+    _raise(_load().stream_prompt_attention(ctypes.byref(p), _addr(q), _addr(k), _addr(v), _addr(cu_q), _addr(cu_k), float(scale),
+                                           _addr(out), _addr(lse_out), _stream_handle(stream)))
+
+
+def stream_cache_workspace_bytes(c: StreamCache) -> int:
+    return int(_load().stream_cache_workspace_bytes(ctypes.byref(c)))
+
+
+def stream_cache_reserve(c: StreamCache, n_new, page_table, seq_len, ref_count, info_out, workspace, workspace_bytes: int, stream=None) -> None:
+    _raise(_load().stream_cache_reserve(ctypes.byref(c), _addr(n_new), _addr(page_table), _addr(seq_len), _addr(ref_count),
+                                        _addr(info_out), _addr(workspace), workspace_bytes, _stream_handle(stream)))
+
+
+def stream_cache_fork(c: StreamCache, parent, page_table, seq_len, ref_count, pairs_out, info_out, workspace, workspace_bytes: int,
+                      stream=None) -> None:
+    _raise(_load().stream_cache_fork(ctypes.byref(c), _addr(parent), _addr(page_table), _addr(seq_len), _addr(ref_count),
+                                     _addr(pairs_out), _addr(info_out), _addr(workspace), workspace_bytes, _stream_handle(stream)))
+
+
+def stream_cache_free(c: StreamCache, done, page_table, seq_len, ref_count, info_out, workspace, workspace_bytes: int, stream=None) -> None:
+    _raise(_load().stream_cache_free(ctypes.byref(c), _addr(done), _addr(page_table), _addr(seq_len), _addr(ref_count),
+                                     _addr(info_out), _addr(workspace), workspace_bytes, _stream_handle(stream)))
+
+
+def stream_cache_compact(c: StreamCache, page_table, seq_len, ref_count, pairs_out, info_out, workspace, workspace_bytes: int,
+                         stream=None) -> None:
+    _raise(_load().stream_cache_compact(ctypes.byref(c), _addr(page_table), _addr(seq_len), _addr(ref_count), _addr(pairs_out),
+                                        _addr(info_out), _addr(workspace), workspace_bytes, _stream_handle(stream)))
+
+
+def stream_cache_copy_pages(c: StreamCache, k_pages, v_pages, pairs, count, n_pairs: int, stream=None) -> None:
+    _raise(_load().stream_cache_copy_pages(ctypes.byref(c), _addr(k_pages), _addr(v_pages), _addr(pairs), _addr(count), int(n_pairs),
+                                           _stream_handle(stream)))
+
+
+def stream_cache_write(c: StreamCache, layer: int, k, v, total: int, stride_t: int, stride_h: int, cu_new, page_table, seq_len,
+                       k_pages, v_pages, stream=None) -> None:
+    _raise(_load().stream_cache_write(ctypes.byref(c), int(layer), _addr(k), _addr(v), int(total), int(stride_t), int(stride_h),
+                                      _addr(cu_new), _addr(page_table), _addr(seq_len), _addr(k_pages), _addr(v_pages),
+                                      _stream_handle(stream)))
+
+
+def stream_decode_workspace_bytes(c: StreamCache, n_q_heads: int) -> int:
+    return int(_load().stream_decode_workspace_bytes(ctypes.byref(c), int(n_q_heads)))
+
+
+def stream_decode_attention(c: StreamCache, layer: int, n_q_heads: int, q, q_stride_s: int, q_stride_h: int, k_pages, v_pages,
+                            page_table, seq_len, scale: float, out, lse_out, workspace, workspace_bytes: int, stream=None) -> None:
+    """Attention of one new token of every slot over a paged cache."""
+    _raise(_load().stream_decode_attention(ctypes.byref(c), int(layer), int(n_q_heads), _addr(q), int(q_stride_s), int(q_stride_h),
+                                           _addr(k_pages), _addr(v_pages), _addr(page_table), _addr(seq_len), float(scale),
+                                           _addr(out), _addr(lse_out), _addr(workspace), workspace_bytes, _stream_handle(stream)))
 
 
 # ----------------------------------------------------------------------------------------------
@@ -472,3 +570,218 @@ def probe_unit_rates(device="cuda", stream=None) -> StreamUnitRates:
         raise RuntimeError("no CUDA device to probe")
     scratch = torch.empty(n, dtype=torch.uint8, device=device)
     return stream_probe_unit_rates(scratch, n, stream)
+
+
+# ----------------------------------------------------------------------------------------------
+# Dense attention and the paged cache
+# ----------------------------------------------------------------------------------------------
+_DTYPES = {torch.float32: STREAM_F32, torch.bfloat16: STREAM_BF16}
+
+
+def _checked(x: torch.Tensor, dtype, shape, what: str, device) -> torch.Tensor:
+    if x.dtype is not dtype or not x.is_contiguous() or tuple(x.shape) != tuple(shape) or x.device != device:
+        raise ValueError(f"{what} must be a contiguous {str(dtype)[6:]} tensor of shape {tuple(shape)} on {device}")
+    return x
+
+
+class _Here:
+    def __enter__(self):
+        return None
+
+    def __exit__(self, *exc):
+        return False
+
+
+_HERE_ALREADY = _Here()
+
+
+def _on(device: torch.device):
+    """The tensors' device as the current one, for a launch."""
+    if device.index is None or device.index == torch.cuda.current_device():
+        return _HERE_ALREADY
+    return torch.cuda.device(device)
+
+
+def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor, cu_k: torch.Tensor | None = None, *,
+                     causal: bool = True, scale: float = 0.0, want_lse: bool = False, out: torch.Tensor | None = None,
+                     lse_out: torch.Tensor | None = None, stream=None):
+    """Dense attention of packed prompts: q ``[total_q, H, d]``, k and v ``[total_k, G, d]``, ``cu_q`` and ``cu_k``
+    int32 CUDA tensors ``[n_seqs + 1]`` with the sequences' first rows (``cu_k``: default ``cu_q``). Under a causal
+    mask a sequence's last query sees all its keys. Returns the output ``[total_q, H, d]``, with ``want_lse`` (or
+    ``lse_out``) also the logarithms of the softmax sums, float32 ``[H, total_q]``. Rows of no sequence are left as they are."""
+    if not (q.is_cuda and k.is_cuda and v.is_cuda and cu_q.is_cuda):
+        raise ValueError("q, k, v and cu_q must be CUDA tensors (there is no CPU path)")
+    if q.dim() != 3 or k.dim() != 3 or q.shape[2] != k.shape[2]:
+        raise ValueError("q must be [total_q, H, d] and k [total_k, G, d]")
+    if v.shape != k.shape or v.stride() != k.stride():
+        raise ValueError("v must have k's shape and strides")
+    if q.dtype not in _DTYPES or k.dtype is not q.dtype or v.dtype is not q.dtype:
+        raise ValueError("q, k and v must all be float32 or all bfloat16")
+    if q.stride(2) != 1 or k.stride(2) != 1:
+        raise ValueError("innermost stride must be 1")
+    device = q.device
+    if k.device != device or v.device != device:
+        raise ValueError("q, k and v must be on one device")
+    if cu_q.dim() != 1 or cu_q.shape[0] < 2:
+        raise ValueError("cu_q must be [n_seqs + 1]")
+    _checked(cu_q, torch.int32, cu_q.shape, "cu_q", device)
+    cu_k = cu_q if cu_k is None else _checked(cu_k, torch.int32, cu_q.shape, "cu_k", device)
+    total, H, d = q.shape
+    p = StreamPrompt(cu_q.shape[0] - 1, H, k.shape[1], d, total, k.shape[0], int(causal), _DTYPES[q.dtype], q.stride(0), q.stride(1),
+                     k.stride(0), k.stride(1))
+    out = _empty((total, H, d), q.dtype, device) if out is None else _checked(out, q.dtype, (total, H, d), "out", device)
+    if lse_out is not None:
+        _checked(lse_out, torch.float32, (H, total), "lse_out", device)
+    elif want_lse:
+        lse_out = _empty((H, total), torch.float32, device)
+    with _on(device):
+        stream_prompt_attention(p, q, k, v, cu_q, cu_k, scale, out, lse_out, stream)
+    return out if lse_out is None else (out, lse_out)
+
+
+@dataclass
+class CacheMoves:
+    """Page copies that are due (:func:`cache_copy_pages`) and what the call that asks for them says of itself."""
+
+    pairs: torch.Tensor  # int32 [n, 2]: {from, to}, then -1
+    info: torch.Tensor   # int32 [4]: done, pages to copy, free pages, refusals
+
+
+class PagedCache:
+    """A paged key-value cache of one or several layers and its ledger; see ``stream_cache`` in stream.h.
+
+    ``k`` and ``v`` are ``[n_layers, n_pages, page_size, n_kv_heads, d]`` (views of any stride order, innermost
+    stride 1, both alike), ``page_table`` int32 ``[n_slots, max_pages]``, ``seq_len`` int32 ``[n_slots]`` and
+    ``ref_count`` int32 ``[n_pages]``, all on one device. The object keeps them and a workspace for the ledger
+    calls; :func:`new_cache` makes an empty one."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, seq_len: torch.Tensor, ref_count: torch.Tensor):
+        if not k.is_cuda or not v.is_cuda:
+            raise ValueError("k and v must be CUDA tensors (there is no CPU path)")
+        if k.dim() != 5 or v.shape != k.shape or v.stride() != k.stride() or v.dtype is not k.dtype or v.device != k.device:
+            raise ValueError("k and v must be [n_layers, n_pages, page_size, n_kv_heads, d], alike in strides, dtype and device")
+        if k.dtype not in _DTYPES:
+            raise ValueError("k and v must be float32 or bfloat16")
+        if k.stride(4) != 1:
+            raise ValueError("innermost stride must be 1")
+        if page_table.dim() != 2:
+            raise ValueError("page_table must be [n_slots, max_pages]")
+        self.device = k.device
+        self.n_layers, self.n_pages, self.page_size, self.n_kv_heads, self.d = k.shape
+        self.n_slots, self.max_pages = page_table.shape
+        self.k, self.v = k, v
+        self.page_table = _checked(page_table, torch.int32, page_table.shape, "page_table", self.device)
+        self.seq_len = _checked(seq_len, torch.int32, (self.n_slots,), "seq_len", self.device)
+        self.ref_count = _checked(ref_count, torch.int32, (self.n_pages,), "ref_count", self.device)
+        self.struct = StreamCache(self.n_slots, self.n_pages, self.page_size, self.max_pages, self.n_kv_heads, self.d, self.n_layers,
+                                  _DTYPES[k.dtype], *k.stride()[:4])
+        n = stream_cache_workspace_bytes(self.struct)
+        if n == 0:
+            raise StreamError(STREAM_ERR_INVALID_ARG, stream_last_error())
+        self.workspace = _empty((n,), torch.uint8, self.device)
+
+    def _ledger(self):
+        return self.page_table.data_ptr(), self.seq_len.data_ptr(), self.ref_count.data_ptr()
+
+
+def new_cache(n_slots: int, n_pages: int, page_size: int, max_pages: int, n_kv_heads: int, d: int, *, n_layers: int = 1,
+              dtype: torch.dtype = torch.bfloat16, device="cuda") -> PagedCache:
+    """An empty cache: all slots empty, all pages free (what the pages hold is not set)."""
+    k, v = (torch.empty(n_layers, n_pages, page_size, n_kv_heads, d, dtype=dtype, device=device) for _ in range(2))
+    return PagedCache(k, v, torch.full((n_slots, max_pages), -1, dtype=torch.int32, device=k.device),
+                      torch.zeros(n_slots, dtype=torch.int32, device=k.device), torch.zeros(n_pages, dtype=torch.int32, device=k.device))
+
+
+def cache_reserve(cache: PagedCache, n_new: torch.Tensor, stream=None) -> torch.Tensor:
+    """Room for ``n_new`` (int32 ``[n_slots]``) more tokens in every slot, all of it or none; ``seq_len`` grows. Returns
+    the info ``[done, pages taken, free pages, refusals]`` (int32, on the device)."""
+    c = cache
+    _checked(n_new, torch.int32, (c.n_slots,), "n_new", c.device)
+    info = _empty((4,), torch.int32, c.device)
+    with _on(c.device):
+        stream_cache_reserve(c.struct, n_new, *c._ledger(), info, c.workspace, c.workspace.numel(), stream)
+    return info
+
+
+def cache_fork(cache: PagedCache, parent: torch.Tensor, stream=None) -> CacheMoves:
+    """Every slot s with ``parent[s] >= 0`` (int32 ``[n_slots]``) becomes a chain of its own with the tokens of slot
+    ``parent[s]``. Full pages are shared; the copies of the others are due: hand the result to :func:`cache_copy_pages`."""
+    c = cache
+    _checked(parent, torch.int32, (c.n_slots,), "parent", c.device)
+    info, pairs = _empty((4,), torch.int32, c.device), _empty((c.n_slots, 2), torch.int32, c.device)
+    with _on(c.device):
+        stream_cache_fork(c.struct, parent, *c._ledger(), pairs, info, c.workspace, c.workspace.numel(), stream)
+    return CacheMoves(pairs, info)
+
+
+def cache_free(cache: PagedCache, done: torch.Tensor, stream=None) -> torch.Tensor:
+    """Empties every slot with ``done[s] != 0`` (int32 ``[n_slots]``). Returns ``[1, pages freed, free pages, impossible entries]``."""
+    c = cache
+    _checked(done, torch.int32, (c.n_slots,), "done", c.device)
+    info = _empty((4,), torch.int32, c.device)
+    with _on(c.device):
+        stream_cache_free(c.struct, done, *c._ledger(), info, c.workspace, c.workspace.numel(), stream)
+    return info
+
+
+def cache_compact(cache: PagedCache, stream=None) -> CacheMoves:
+    """Moves the pages in use to the lowest numbers; the copies are due (:func:`cache_copy_pages`)."""
+    c = cache
+    info, pairs = _empty((4,), torch.int32, c.device), _empty((c.n_pages // 2, 2), torch.int32, c.device)
+    with _on(c.device):
+        stream_cache_compact(c.struct, *c._ledger(), pairs, info, c.workspace, c.workspace.numel(), stream)
+    return CacheMoves(pairs, info)
+
+
+def cache_copy_pages(cache: PagedCache, moves: CacheMoves, stream=None) -> None:
+    """Makes the copies that :func:`cache_fork` or :func:`cache_compact` asks for, in all layers."""
+    c = cache
+    _checked(moves.pairs, torch.int32, (moves.pairs.shape[0], 2), "pairs", c.device)
+    _checked(moves.info, torch.int32, (4,), "info", c.device)
+    with _on(c.device):
+        stream_cache_copy_pages(c.struct, c.k, c.v, moves.pairs, moves.info.data_ptr() + 4, moves.pairs.shape[0], stream)
+
+
+def cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, cu_new: torch.Tensor, *, layer: int = 0, stream=None) -> None:
+    """Writes new tokens' keys and values (``[total, n_kv_heads, d]``, rows ``cu_new[s] .. cu_new[s + 1]`` being slot s's
+    last tokens) to the pages of one layer, after :func:`cache_reserve`."""
+    c = cache
+    if k.dim() != 3 or tuple(k.shape[1:]) != (c.n_kv_heads, c.d) or v.shape != k.shape or v.stride() != k.stride():
+        raise ValueError("k and v must be [total, n_kv_heads, d], alike in strides")
+    if k.dtype is not c.k.dtype or v.dtype is not c.k.dtype or k.device != c.device or v.device != c.device:
+        raise ValueError("k and v must have the cache's dtype and device")
+    if k.stride(2) != 1:
+        raise ValueError("innermost stride must be 1")
+    _checked(cu_new, torch.int32, (c.n_slots + 1,), "cu_new", c.device)
+    with _on(c.device):
+        stream_cache_write(c.struct, layer, k, v, k.shape[0], k.stride(0), k.stride(1), cu_new, c.page_table, c.seq_len, c.k, c.v, stream)
+
+
+def decode_attention(q: torch.Tensor, cache: PagedCache, *, layer: int = 0, scale: float = 0.0, want_lse: bool = False,
+                     out: torch.Tensor | None = None, lse_out: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
+                     stream=None):
+    """Attention of one new token of every slot, q ``[n_slots, H, d]``, over its cached tokens. Returns the output
+    ``[n_slots, H, d]``, with ``want_lse`` (or ``lse_out``) also the logarithms of the softmax sums, float32
+    ``[n_slots, H]``. ``workspace``: uint8, at least :func:`stream_decode_workspace_bytes`, one per call that can overlap."""
+    c = cache
+    if q.dim() != 3 or q.shape[0] != c.n_slots or q.shape[2] != c.d or q.dtype is not c.k.dtype or q.device != c.device:
+        raise ValueError("q must be [n_slots, H, d] with the cache's dtype and device")
+    if q.stride(2) != 1:
+        raise ValueError("innermost stride must be 1")
+    H = q.shape[1]
+    out = _empty(tuple(q.shape), q.dtype, c.device) if out is None else _checked(out, q.dtype, q.shape, "out", c.device)
+    if lse_out is not None:
+        _checked(lse_out, torch.float32, (c.n_slots, H), "lse_out", c.device)
+    elif want_lse:
+        lse_out = _empty((c.n_slots, H), torch.float32, c.device)
+    if workspace is None:
+        n = stream_decode_workspace_bytes(c.struct, H)
+        if n == 0:
+            raise StreamError(STREAM_ERR_INVALID_ARG, stream_last_error())
+        workspace = _empty((n,), torch.uint8, c.device)
+    elif workspace.dtype is not torch.uint8 or not workspace.is_contiguous() or workspace.device != c.device:
+        raise ValueError("workspace must be a contiguous uint8 tensor on the cache's device")
+    with _on(c.device):
+        stream_decode_attention(c.struct, layer, H, q, q.stride(0), q.stride(1), c.k, c.v, c.page_table, c.seq_len, scale, out, lse_out,
+                                workspace, workspace.numel(), stream)
+    return out if lse_out is None else (out, lse_out)
