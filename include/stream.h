@@ -8,7 +8,7 @@
  *     keeps between calls is: the thread-local error text; per device, the two copy streams and
  *     the events of stream_run_host (created at its first call, kept until the process ends);
  *     per device, the built-in scratch array of stream_build_mask_static and its address; and
- *     the status word of the tensor-core attention kernel (stream_check_device_status).
+ *     the status words of the tensor-core attention kernels (stream_check_device_status).
  *   - Work is enqueued on `cuda_stream` (a cudaStream_t passed as void*; NULL = default stream)
  *     and the call returns after enqueue unless stated otherwise.
  *   - Every failure is a returned status; nothing aborts or throws. Arguments are validated on
@@ -407,8 +407,8 @@ typedef struct {
  * the last one, does not matter, whatever it is (NaN included); Q, K and V of the sequences must be finite.
  *
  *   q, k, v     device, read only
- *   cu_q, cu_k  device int32 [n_seqs + 1], ascending; an entry outside 0 .. total_q (total_k), or below the one
- *               before it, is taken as the nearest that is not
+ *   cu_q, cu_k  device int32 [n_seqs + 1], ascending; an entry outside 0 .. total_q (total_k) counts as the nearest
+ *               inside, and a sequence whose end lies before its beginning is empty
  *   scale       logit scale; <= 0 selects 1/sqrt(d)
  *   out         device, dtype of the problem, contiguous [total_q, n_q_heads, d]; rows of no sequence stay as they are
  *   lse_out     device float32 [n_q_heads, total_q] or NULL; likewise

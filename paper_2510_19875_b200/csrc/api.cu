@@ -352,6 +352,8 @@ stream_status stream_check_device_status(void *cuda_stream) {
     if (rc != STREAM_OK) return rc;
     if (words[0] == 0) rc = read_attn_tok_status(words, (cudaStream_t)cuda_stream);
     if (rc != STREAM_OK) return rc;
+    if (words[0] == 0) rc = read_prompt_status(words, (cudaStream_t)cuda_stream);
+    if (rc != STREAM_OK) return rc;
     if (words[0] != 0) {
         set_error("attention kernel gave up on a bounded wait: code %u, block %u", words[0], words[1]);
         return STREAM_ERR_DEVICE_CHECK;

@@ -95,6 +95,7 @@ stream_status launch_attn_tok(const Geom &g, const void *q, const void *k, const
 // Drain `st` and copy a tensor-core attention kernel's status words (code, block) to out.
 stream_status read_attn_status(unsigned int out[2], cudaStream_t st);
 stream_status read_attn_tok_status(unsigned int out[2], cudaStream_t st);
+stream_status read_prompt_status(unsigned int out[2], cudaStream_t st);  // dense attention of prompts
 
 // The kernels of mask builds and attention, but for clusters, are launched as programmatic dependents: a kernel may begin while the one before it on the stream
 // still runs, as far as this point, behind which that one (and with it all before it) is complete and its
