@@ -18,7 +18,12 @@ struct Args {
     float *parts;                // [grid][2][kMaxHeads * (d + 2)]: m, l, O
     unsigned *bad;               // [grid]: slot + 1 with a page outside the cache, or 0
     WorkspaceHeader *header;
+    int q_vec;                   // (mma.sync) q is read in pieces of 16 bytes
 };
+
+// bf16 on mma.sync. May lower A.grid.
+bool mma_supported(const DecodeCall &a, int dtype);
+cudaError_t launch_mma(Args &A, int n_sm, cudaStream_t st);
 
 // Sums over the slots, by whole warps (the same in every lane).
 __device__ __forceinline__ int units_of(const CacheGeom &c, int s) { return s < c.n_slots ? (tokens_of(c, s) + kUnit - 1) / kUnit : 0; }

@@ -1,0 +1,294 @@
+// Decode attention for bf16 on mma.sync: d = 64, 128 or 256, rows of 16-byte pieces.
+//
+// The up to 16 query heads of a segment are the rows of m16n8k16 products, so that a key and its value are read from shared memory
+// once for all of them. (It is the cache that has to be read: 4 d FLOP a head and 4 d bytes a key; tcgen05's tiles of 64 or 128
+// rows would be empty but for these.) The four warps of a CTA take 16 keys each in turn and know nothing of one another until the
+// segment's end: a warp has its own ring of K and V tiles, filled by cp.async, its own softmax reference and sums
+// (ref is moved only when a logit has outgrown it by 2^30: fp32 sums and bf16 weights keep their relative precision), and its own O in
+// registers; at the end the four meet in shared memory. Keys behind the slot's last one, or without a page, are zeros there.
+#include "decode.cuh"
+#include "warp_common.cuh"
+
+namespace stream {
+namespace {
+
+using namespace decode;
+
+constexpr float kOutgrown = 30.f;  // log2
+constexpr int kStep = 16;          // keys of a warp's tile
+
+template <int D>
+struct Form {
+    static constexpr int kRow = D * 2;                         // bytes
+    static constexpr int kTile = kStep * kRow;
+    static constexpr int kStages = D == 64 ? 6 : 3;
+    static constexpr int kWarp = kStages * 2 * kTile;          // bytes of a warp's ring; in the end its O, fp32
+    static constexpr bool kQInRegs = D <= 128;
+    static constexpr int kCtas = D <= 128 ? 2 : 1;             // of an SM
+    static_assert(kMaxHeads * D * 4 <= kWarp, "O over the ring");
+};
+template <int D>
+struct Smem {
+    unsigned char ring[kThreads / 32][Form<D>::kWarp];
+    unsigned char q[kMaxHeads * Form<D>::kRow];
+    float m[kThreads / 32][kMaxHeads], l[kThreads / 32][kMaxHeads];
+};
+
+__device__ __forceinline__ void ldmatrix4(unsigned addr, unsigned &a, unsigned &b, unsigned &c, unsigned &d) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(a), "=r"(b), "=r"(c), "=r"(d) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldmatrix4_t(unsigned addr, unsigned &a, unsigned &b, unsigned &c, unsigned &d) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(a), "=r"(b), "=r"(c), "=r"(d) : "r"(addr) : "memory");
+}
+// Byte of piece x (16 bytes) of row r in a tile: turned within 128 bytes, so that eight rows' same piece touch every bank.
+template <int D>
+__device__ __forceinline__ unsigned piece_at(int r, int x) { return (unsigned)(r * Form<D>::kRow + ((x ^ (r & 7)) << 4)); }
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, Form<D>::kCtas) decode_mma_kernel(const __grid_constant__ Args A) {
+    using F = Form<D>;
+    extern __shared__ __align__(128) unsigned char smem_raw[];
+    Smem<D> &sm = *reinterpret_cast<Smem<D> *>(smem_raw);
+    const CacheGeom &c = A.a.c;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, quad = lane >> 2;
+    after_previous_kernel();
+    __nv_bfloat16 *const out = (__nv_bfloat16 *)A.a.out;
+    write_empty_slots<__nv_bfloat16>(A);
+    const Share mine = share_of(A, all_units(c, lane) * A.per_slot, (int)blockIdx.x);
+    const unsigned ring = wp::smem_addr(sm.ring[warp]), q_smem = wp::smem_addr(sm.q);
+    const bool one_page = c.page % kStep == 0;  // a tile's keys lie side by side
+    constexpr int kPieces = D / 8, kRowsAtOnce = kPieces >= 32 ? 1 : 32 / kPieces;  // of a row; rows that 32 lanes fetch at once
+    constexpr int kPerRow = kPieces > 32 ? kPieces / 32 : 1;
+    static_assert(kPerRow == 1, "a row is at most 512 bytes");
+    const int row_l = lane / kPieces, piece_l = lane % kPieces;
+    // ldmatrix rows of this lane
+    const int k_row = (lane >> 4) * 8 + (lane & 7), k_half = (lane >> 3) & 1, v_row = ((lane >> 3) & 1) * 8 + (lane & 7), v_half = lane >> 4;
+    unsigned bad = 0;
+    Place at = {0, 0, 0};
+    for (long long u = mine.first; u < mine.end;) {
+        at = place_of(c, A.per_slot, u, lane, at);
+        const Segment sg = segment_of(A, at, u, mine.end);
+        const int s = at.slot;
+        const int32_t *const table = c.table + (long long)s * c.max_pages;
+        const __nv_bfloat16 *const ks = (const __nv_bfloat16 *)A.a.k + (long long)sg.kvh * c.s_h, *const vs = (const __nv_bfloat16 *)A.a.v + (long long)sg.kvh * c.s_h;
+        const int n_steps = (sg.key_end - sg.key0 - warp * kStep + 4 * kStep - 1) / (4 * kStep);  // of this warp (0 or fewer: none)
+        // Lane i < 16: the page of key i of the warp's step n, -1: none
+        auto page_of = [&](int n) -> int {
+            const int key = sg.key0 + (4 * n + warp) * kStep + lane;
+            if (n >= n_steps || lane >= kStep || key >= sg.key_end) return -1;
+            const int page = table[key / c.page];
+            if ((unsigned)page < (unsigned)c.n_pages) return page;
+            bad = (unsigned)s + 1u;
+            return -1;
+        };
+        auto fetch = [&](int n, int page) -> unsigned {  // the step's tiles; which of its keys are there
+            const unsigned there = __ballot_sync(0xffffffffu, page >= 0);
+            const int key = sg.key0 + (4 * n + warp) * kStep + lane;
+            const long long own = page >= 0 ? (long long)page * c.s_p + (long long)(key % c.page) * c.s_t : 0;
+            const unsigned dst = ring + (n % F::kStages) * 2 * F::kTile;
+            const long long base = __shfl_sync(0xffffffffu, own, 0);
+#pragma unroll
+            for (int r0 = 0; r0 < kStep; r0 += kRowsAtOnce) {
+                const int r = r0 + row_l;
+                const bool is = (there >> r) & 1u;
+                long long e = one_page ? base + r * c.s_t : 0;
+                if (!one_page) e = __shfl_sync(0xffffffffu, own, r);
+                e = (is ? e : 0) + piece_l * 8;
+                const unsigned to = dst + piece_at<D>(r, piece_l);
+                cp_async16(to, ks + e, is);
+                cp_async16(to + F::kTile, vs + e, is);
+            }
+            return there;
+        };
+        // the first tiles are on their way before anything else
+        unsigned there[F::kStages];  // of the steps in the ring
+        int page = page_of(0);
+#pragma unroll
+        for (int n = 0; n < F::kStages - 1; ++n) {
+            const int next = page_of(n + 1);
+            there[n] = n < n_steps ? fetch(n, page) : 0u;
+            cp_commit();
+            page = next;
+        }
+        for (int i = tid; i < kMaxHeads * kPieces; i += kThreads) {
+            const int h = i / kPieces, x = i % kPieces;
+            const __nv_bfloat16 *const src = (const __nv_bfloat16 *)A.a.q + (long long)s * A.a.qs_s + (long long)(sg.h0 + h) * A.a.qs_h + x * 8;
+            uint4 w = make_uint4(0, 0, 0, 0);
+            if (h < sg.heads) {
+                if (A.q_vec) {
+                    w = *reinterpret_cast<const uint4 *>(src);
+                } else {
+                    __nv_bfloat16 y[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y[e] = src[e];
+                    w = *reinterpret_cast<const uint4 *>(y);
+                }
+            }
+            *reinterpret_cast<uint4 *>(sm.q + piece_at<D>(h, x)) = w;
+        }
+        __syncthreads();
+        const unsigned q_addr = q_smem + (lane & 15) * F::kRow;
+        unsigned qa[F::kQInRegs ? D / 16 : 1][4];
+        if constexpr (F::kQInRegs) {
+#pragma unroll
+            for (int x = 0; x < D / 16; ++x) ldmatrix4(q_addr + (((2 * x + (lane >> 4)) ^ (lane & 7)) << 4), qa[x][0], qa[x][1], qa[x][2], qa[x][3]);
+        }
+        float o[D / 8][4];
+#pragma unroll
+        for (int x = 0; x < D / 8; ++x)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) o[x][y] = 0.f;
+        float ref[2] = {-CUDART_INF_F, -CUDART_INF_F}, l[2] = {0.f, 0.f};  // of rows quad and quad + 8, in units of log2
+        auto step = [&](int n, unsigned keys) {
+            const unsigned kt = ring + (n % F::kStages) * 2 * F::kTile, vt = kt + F::kTile;
+            float sc[2][4];
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int y = 0; y < 4; ++y) sc[x][y] = 0.f;
+#pragma unroll
+            for (int x = 0; x < D / 16; ++x) {
+                unsigned b[4], a[4];
+                ldmatrix4(kt + piece_at<D>(k_row, 2 * x + k_half), b[0], b[1], b[2], b[3]);
+                if constexpr (F::kQInRegs) {
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) a[y] = qa[x][y];
+                } else {
+                    ldmatrix4(q_addr + (((2 * x + (lane >> 4)) ^ (lane & 7)) << 4), a[0], a[1], a[2], a[3]);
+                }
+                wp::mma_bf16(sc[0], a[0], a[1], a[2], a[3], b[0], b[1]);
+                wp::mma_bf16(sc[1], a[0], a[1], a[2], a[3], b[2], b[3]);
+            }
+            bool outgrown = false;
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    const int key = x * 8 + (lane & 3) * 2 + (y & 1);
+                    sc[x][y] = (keys >> key) & 1u ? sc[x][y] * A.a.scale_log2 : -CUDART_INF_F;
+                    outgrown = outgrown || sc[x][y] - ref[y >> 1] > kOutgrown;  // (the first: infinity)
+                }
+            if (__any_sync(0xffffffffu, outgrown)) {
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    float mx = fmaxf(fmaxf(sc[0][2 * r], sc[0][2 * r + 1]), fmaxf(sc[1][2 * r], sc[1][2 * r + 1]));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+                    const float now = fmaxf(ref[r], mx), f = now == -CUDART_INF_F ? 1.f : fast_exp2(ref[r] - now);
+                    ref[r] = now;
+                    l[r] *= f;
+#pragma unroll
+                    for (int x = 0; x < D / 8; ++x) { o[x][2 * r] *= f; o[x][2 * r + 1] *= f; }
+                }
+            }
+            unsigned pa[4];
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const float base = ref[r] == -CUDART_INF_F ? 0.f : ref[r];
+                    const float p0 = fast_exp2(sc[x][2 * r] - base), p1 = fast_exp2(sc[x][2 * r + 1] - base);
+                    l[r] += p0 + p1;
+                    const __nv_bfloat162 pk = __floats2bfloat162_rn(p0, p1);
+                    pa[2 * x + r] = *reinterpret_cast<const unsigned *>(&pk);
+                }
+#pragma unroll
+            for (int x = 0; x < D / 16; ++x) {
+                unsigned b[4];
+                ldmatrix4_t(vt + piece_at<D>(v_row, 2 * x + v_half), b[0], b[1], b[2], b[3]);
+                wp::mma_bf16(o[2 * x], pa[0], pa[1], pa[2], pa[3], b[0], b[1]);
+                wp::mma_bf16(o[2 * x + 1], pa[0], pa[1], pa[2], pa[3], b[2], b[3]);
+            }
+        };
+        // (the ring's places by name, so that what is there of each stays in registers)
+        for (int n0 = 0; n0 < n_steps; n0 += F::kStages) {
+#pragma unroll
+            for (int x = 0; x < F::kStages; ++x) {
+                const int n = n0 + x;
+                if (n < n_steps) {
+                    const int ahead = n + F::kStages - 1, next = page_of(ahead + 1);
+                    there[(x + F::kStages - 1) % F::kStages] = ahead < n_steps ? fetch(ahead, page) : 0u;
+                    cp_commit();
+                    page = next;
+                    cp_wait<F::kStages - 1>();
+                    __syncwarp();
+                    step(n, there[x]);
+                    __syncwarp();  // (the tile is read before its place is filled again)
+                }
+            }
+        }
+        cp_wait<0>();
+        __syncwarp();
+        // the four warps' m, l and O meet
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
+            l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
+            if ((lane & 3) == 0) { sm.m[warp][quad + 8 * r] = ref[r]; sm.l[warp][quad + 8 * r] = l[r]; }
+        }
+        float *const own = reinterpret_cast<float *>(sm.ring[warp]);
+#pragma unroll
+        for (int x = 0; x < D / 8; ++x) {
+            *reinterpret_cast<float2 *>(own + quad * D + x * 8 + (lane & 3) * 2) = make_float2(o[x][0], o[x][1]);
+            *reinterpret_cast<float2 *>(own + (quad + 8) * D + x * 8 + (lane & 3) * 2) = make_float2(o[x][2], o[x][3]);
+        }
+        __syncthreads();
+        float *const part = part_of(A, (int)blockIdx.x, u == mine.first ? 0 : 1);
+        for (int i = tid; i < sg.heads * (D / 4); i += kThreads) {
+            const int h = i / (D / 4), x = (i % (D / 4)) * 4;
+            float m = sm.m[0][h];
+#pragma unroll
+            for (int w = 1; w < kThreads / 32; ++w) m = fmaxf(m, sm.m[w][h]);
+            const float base = m == -CUDART_INF_F ? 0.f : m;
+            float sum = 0.f;
+            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < kThreads / 32; ++w) {
+                const float f = fast_exp2(sm.m[w][h] - base);
+                const float4 z = *reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(sm.ring[w]) + h * D + x);
+                sum = fmaf(f, sm.l[w][h], sum);
+                y.x = fmaf(f, z.x, y.x); y.y = fmaf(f, z.y, y.y); y.z = fmaf(f, z.z, y.z); y.w = fmaf(f, z.w, y.w);
+            }
+            if (sg.whole) {
+                const float inv = sum > 0.f ? 1.f / sum : 0.f;
+                __nv_bfloat16 *const to = out + ((long long)s * A.a.H + sg.h0 + h) * D + x;
+                to[0] = __float2bfloat16_rn(y.x * inv); to[1] = __float2bfloat16_rn(y.y * inv);
+                to[2] = __float2bfloat16_rn(y.z * inv); to[3] = __float2bfloat16_rn(y.w * inv);
+                if (x == 0 && A.a.lse != nullptr) A.a.lse[(long long)s * A.a.H + sg.h0 + h] = sum > 0.f ? (m + log2f(sum)) * kLn2 : -CUDART_INF_F;
+            } else {
+                *reinterpret_cast<float4 *>(part + 2 * kMaxHeads + h * D + x) = y;
+                if (x == 0) { part[h] = m; part[kMaxHeads + h] = sum; }
+            }
+        }
+        __syncthreads();  // (the rings are filled again)
+        u += sg.units;
+    }
+    record_bad(A, bad);
+}
+
+template <int D>
+cudaError_t launch(Args &A, int n_sm, cudaStream_t st) {
+    const int smem = (int)sizeof(Smem<D>);
+    cudaError_t e = cudaFuncSetAttribute(decode_mma_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    const int most = Form<D>::kCtas * n_sm;
+    if (A.grid > most) A.grid = most;
+    return launch_early(decode_mma_kernel<D>, (unsigned)A.grid, kThreads, smem, st, A);
+}
+
+}  // namespace
+
+namespace decode {
+
+bool mma_supported(const DecodeCall &a, int dtype) {
+    if (dtype != STREAM_BF16 || (a.c.d != 64 && a.c.d != 128 && a.c.d != 256)) return false;
+    return (((uintptr_t)a.k | (uintptr_t)a.v) & 15) == 0 && ((a.c.s_p | a.c.s_t | a.c.s_h) & 7) == 0;
+}
+
+cudaError_t launch_mma(Args &A, int n_sm, cudaStream_t st) {
+    A.q_vec = ((uintptr_t)A.a.q & 15) == 0 && ((A.a.qs_s | A.a.qs_h) & 7) == 0 ? 1 : 0;
+    return A.a.c.d == 64 ? launch<64>(A, n_sm, st) : A.a.c.d == 128 ? launch<128>(A, n_sm, st) : launch<256>(A, n_sm, st);
+}
+
+}  // namespace decode
+}  // namespace stream

@@ -1,0 +1,133 @@
+"""Dense attention and the paged cache: what the library and the binding refuse, without a GPU."""
+import os
+import re
+
+import pytest
+import torch
+
+import paper_2510_19875_b200
+from test_api_cpu import S  # noqa: F401  (fixture)
+
+CSRC = os.path.join(os.path.dirname(paper_2510_19875_b200.__file__), "csrc")
+A = 4096  # an address that nothing is read from: the calls below are refused before anything is launched
+
+
+def prompt(S, **kw):
+    base = dict(n_seqs=2, n_q_heads=4, n_kv_heads=2, d=64, total_q=100, total_k=100, causal=1, dtype=S.STREAM_BF16, q_stride_t=256,
+                q_stride_h=64, kv_stride_t=128, kv_stride_h=64)
+    base.update(kw)
+    return S.StreamPrompt(**base)
+
+
+def cache(S, **kw):
+    base = dict(n_slots=4, n_pages=20, page_size=16, max_pages=8, n_kv_heads=2, d=64, n_layers=3, dtype=S.STREAM_BF16,
+                stride_l=20 * 16 * 128, stride_p=16 * 128, stride_t=128, stride_h=64)
+    base.update(kw)
+    return S.StreamCache(**base)
+
+
+def refused(S, status, call, *args):
+    with pytest.raises(S.StreamError) as e:
+        call(*args)
+    assert e.value.status == status
+    assert S.stream_last_error() != ""
+
+
+@pytest.mark.parametrize("kw", [dict(n_seqs=0), dict(n_q_heads=3), dict(n_kv_heads=0), dict(dtype=5), dict(causal=2), dict(total_q=-1), dict(total_k=-1),
+                                dict(q_stride_t=63), dict(q_stride_h=1), dict(kv_stride_t=0), dict(kv_stride_h=-64), dict(d=0), dict(d=-64)])
+def test_invalid_prompts(S, kw):
+    refused(S, S.STREAM_ERR_INVALID_ARG, S.stream_prompt_attention, prompt(S, **kw), A, A, A, A, A, 0.0, A, None, 0)
+
+
+@pytest.mark.parametrize("kw", [dict(d=96, q_stride_h=96, kv_stride_h=96), dict(total_q=2 ** 31), dict(total_k=2 ** 31), dict(n_seqs=2 ** 25), dict(n_q_heads=2 ** 18)])
+def test_unsupported_prompts(S, kw):
+    refused(S, S.STREAM_ERR_UNSUPPORTED, S.stream_prompt_attention, prompt(S, **kw), A, A, A, A, A, 0.0, A, None, 0)
+
+
+def test_prompt_pointers(S):
+    good = [A, A, A, A, A, 0.0, A, None]
+    for i in (0, 1, 2, 3, 4, 6):
+        refused(S, S.STREAM_ERR_INVALID_ARG, S.stream_prompt_attention, prompt(S), *(None if j == i else x for j, x in enumerate(good)), 0)
+        refused(S, S.STREAM_ERR_INVALID_ARG, S.stream_prompt_attention, prompt(S), *(A + 1 if j == i else x for j, x in enumerate(good)), 0)
+    for scale in (float("inf"),):
+        refused(S, S.STREAM_ERR_INVALID_ARG, S.stream_prompt_attention, prompt(S), A, A, A, A, A, scale, A, None, 0)
+    S.stream_prompt_attention(prompt(S, total_q=0), None, None, None, A, A, 0.0, None, None, 0)  # nothing to do
+    # a stride that separates nothing does not matter
+    S.stream_prompt_attention(prompt(S, total_q=0, q_stride_t=0, n_kv_heads=1, kv_stride_h=0, total_k=1, kv_stride_t=0), None, None, None, A, A, 0.0, None, None, 0)
+
+
+BAD_CACHES = [dict(n_slots=0), dict(n_pages=0), dict(page_size=0), dict(max_pages=-1), dict(n_kv_heads=0), dict(n_layers=0), dict(d=0), dict(dtype=2),
+              dict(stride_l=0), dict(stride_p=-1), dict(stride_t=63), dict(stride_h=0)]
+LARGE_CACHES = [dict(d=48), dict(n_slots=2 ** 20, max_pages=2 ** 12), dict(page_size=2 ** 20, max_pages=2 ** 12), dict(n_pages=2 ** 30 + 1), dict(page_size=2 ** 24, max_pages=1)]
+
+
+def every_call(S, c):
+    n = 1 << 40
+    return [(S.stream_cache_reserve, (c, A, A, A, A, A, A, n, 0)), (S.stream_cache_fork, (c, A, A, A, A, A, A, A, n, 0)),
+            (S.stream_cache_free, (c, A, A, A, A, A, A, n, 0)), (S.stream_cache_compact, (c, A, A, A, A, A, A, n, 0)),
+            (S.stream_cache_copy_pages, (c, A, A, A, A, 3, 0)), (S.stream_cache_write, (c, 0, A, A, 5, 128, 64, A, A, A, A, A, 0)),
+            (S.stream_decode_attention, (c, 0, 4, A, 256, 64, A, A, A, A, 0.0, A, None, A, n, 0))]
+
+
+@pytest.mark.parametrize("kw", BAD_CACHES)
+def test_invalid_caches(S, kw):
+    c = cache(S, **kw)
+    assert S.stream_cache_workspace_bytes(c) == 0 and S.stream_decode_workspace_bytes(c, 4) == 0
+    for call, args in every_call(S, c):
+        refused(S, S.STREAM_ERR_INVALID_ARG, call, *args)
+
+
+@pytest.mark.parametrize("kw", LARGE_CACHES)
+def test_unsupported_caches(S, kw):
+    c = cache(S, **kw)
+    assert S.stream_cache_workspace_bytes(c) == 0 and S.stream_decode_workspace_bytes(c, 4) == 0
+    for call, args in every_call(S, c):
+        refused(S, S.STREAM_ERR_UNSUPPORTED, call, *args)
+
+
+def test_pointers_and_workspaces(S):
+    c = cache(S)
+    assert S.stream_cache_workspace_bytes(c) >= 4 * (4 + 20) and S.stream_decode_workspace_bytes(c, 4) > 256
+    for call, args in every_call(S, c):
+        name = call.__name__
+        for i, x in enumerate(args):
+            if x == A and not isinstance(x, bool):
+                last = call in (S.stream_cache_reserve, S.stream_cache_fork, S.stream_cache_free, S.stream_cache_compact, S.stream_decode_attention) and i == len(args) - 3
+                for bad in (None, A + 1):  # missing; aligned to nothing
+                    refused(S, S.STREAM_ERR_WORKSPACE if last else S.STREAM_ERR_INVALID_ARG, call, *(bad if j == i else y for j, y in enumerate(args)))
+                if last:
+                    for n in (0, 64):
+                        refused(S, S.STREAM_ERR_WORKSPACE, call, *(n if j == i + 1 else y for j, y in enumerate(args)))
+        assert name.startswith("stream_")
+    refused(S, S.STREAM_ERR_INVALID_ARG, S.stream_cache_copy_pages, c, A, A, A, A, -1, 0)
+    S.stream_cache_copy_pages(c, None, None, None, None, 0, 0)
+    for layer in (-1, 3):
+        refused(S, S.STREAM_ERR_INVALID_ARG, S.stream_cache_write, c, layer, A, A, 5, 128, 64, A, A, A, A, A, 0)
+        refused(S, S.STREAM_ERR_INVALID_ARG, S.stream_decode_attention, c, layer, 4, A, 256, 64, A, A, A, A, 0.0, A, None, A, 1 << 40, 0)
+    for total, st, sh in ((-1, 128, 64), (2 ** 31, 128, 64), (5, 63, 64), (5, 128, 0)):
+        refused(S, S.STREAM_ERR_INVALID_ARG, S.stream_cache_write, c, 0, A, A, total, st, sh, A, A, A, A, A, 0)
+    S.stream_cache_write(c, 0, None, None, 0, 128, 64, A, A, A, None, None, 0)
+    for heads, st, sh, scale in ((3, 256, 64, 0.0), (0, 256, 64, 0.0), (4, 63, 64, 0.0), (4, 256, 63, 0.0), (4, 256, 64, float("inf"))):
+        refused(S, S.STREAM_ERR_INVALID_ARG, S.stream_decode_attention, c, 0, heads, A, st, sh, A, A, A, A, scale, A, None, A, 1 << 40, 0)
+    assert S.stream_decode_workspace_bytes(c, 3) == 0 and S.stream_decode_workspace_bytes(c, 0) == 0
+
+
+def test_cpu_tensors_are_refused(S):
+    q, cu = torch.zeros(4, 2, 64), torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(ValueError):
+        S.prompt_attention(q, q, q, cu)
+    k = torch.zeros(1, 2, 4, 2, 64)
+    with pytest.raises(ValueError):
+        S.PagedCache(k, k, torch.zeros(1, 1, dtype=torch.int32), torch.zeros(1, dtype=torch.int32), torch.zeros(2, dtype=torch.int32))
+
+
+EARLY = sorted(f for f in os.listdir(CSRC) if f.endswith(".cu") and "launch_early(" in open(os.path.join(CSRC, f)).read())
+
+
+@pytest.mark.parametrize("name", EARLY + ["serve_common.cuh", "decode.cuh"])
+def test_kernels_that_begin_early_read_no_memory_as_constant(name):
+    """As the other programmatic dependents: they live while the kernel before them still writes."""
+    assert {"prompt_tc.cu", "prompt_generic.cu", "decode.cu", "decode_mma.cu", "cache_ledger.cu", "cache_copy.cu"} <= set(EARLY)
+    text = re.sub(r"//.*", "", open(os.path.join(CSRC, name)).read())
+    assert not re.findall(r"__ldg\s*\(|ld\.global\.nc", text)
+    assert not re.findall(r"const [\w: ]+\*\s*__restrict__", text)
