@@ -112,10 +112,10 @@ __device__ __forceinline__ void after_previous_kernel() {
 // heads in blocks of 32, 41.0 -> 38.9; 4 heads in fp32, 700 tokens, 40.9 -> 37.8; 32 / 8 heads, 4000 tokens, k = 8, 141 -> 136).
 // Clusters (cluster > 1) start as before, after the kernel before: one of them launched early began a microsecond later (18.4 -> 19.5).
 template <class... K, class... A>
-cudaError_t launch_kernel(void (*kern)(K...), unsigned grid, unsigned threads, size_t smem, cudaStream_t st, unsigned cluster, A &&...args) {
+cudaError_t launch_kernel(void (*kern)(K...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st, unsigned cluster, A &&...args) {
     cudaLaunchAttribute at[1] = {};
     cudaLaunchConfig_t c = {};
-    c.gridDim = dim3(grid);
+    c.gridDim = grid;
     c.blockDim = dim3(threads);
     c.dynamicSmemBytes = smem;
     c.stream = st;

@@ -4,7 +4,7 @@
 // head, as many to each CTA: whatever the slots' lengths, every SM reads as much of the cache as any other, which is all there is to
 // be fast at (a key and its value are read once, 4 d FLOP a query head). A CTA walks its stretch segment by segment, a segment
 // being what it has of one slot's head, with the running maximum and sum of a softmax. A segment that holds all of its head's keys
-// is written out; of the others m, l and O go to the workspace (a CTA has two at most, its first and its last), and a second
+// is written out; of the others m, l and O go to the workspace (a CTA has two at most), and a second
 // kernel, launched beside the first one's end, joins the pieces of a head in the order of its keys: no atomics, the
 // same bits every time.
 #include "decode.cuh"
@@ -55,13 +55,13 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(Args A, int vec) {
     after_previous_kernel();
     T *const out = (T *)A.a.out;
     write_empty_slots<T>(A);
-    const Share mine = share_of(A, all_units(c, lane) * A.per_slot, (int)blockIdx.x);
+    const Share mine = share_of(A, all_places(A, lane), (int)blockIdx.x);
     unsigned bad = 0;
-    Place at = {0, 0, 0};
-    for (long long u = mine.first; u < mine.end;) {
-        at = place_of(c, A.per_slot, u, lane, at);
-        const Segment sg = segment_of(A, at, u, mine.end);
-        const int s = at.slot, nh = sg.heads, h0 = sg.h0, key0 = sg.key0, key_end = sg.key_end;
+    Place pl = {0, 0, 0};
+    int n_parts = 0;
+    Left left = {};
+    for (Segment sg = open_segment(A, mine.first, mine.end, lane, pl); sg.next >= 0; sg = open_segment(A, sg.next, mine.end, lane, pl)) {
+        const int s = sg.slot, nh = sg.heads, h0 = sg.h0, key0 = sg.key0, key_end = sg.key_end;
         const int n_tiles = (key_end - key0 + F::kKeys - 1) / F::kKeys;
         const int32_t *const row = c.table + (long long)s * c.max_pages;
         auto page_of = [&](int tile) -> int {  // of this thread's key
@@ -199,7 +199,11 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(Args A, int vec) {
             if (tid < F::kKeys) sm.page[(t + 2) % 3][tid] = next_page;
             __syncthreads();  // (the buffers and the pages of the tile after next)
         }
-        float *const part = part_of(A, (int)blockIdx.x, u == mine.first ? 0 : 1);
+        float *const part = part_of(A, (int)blockIdx.x, n_parts);
+        if (!sg.whole) {
+            if (sg.key0 == 0) left = {pieces_of(sg, mine), n_parts, sg.heads, 0u, (long long)sg.slot * A.a.H + sg.h0, 0ll};
+            ++n_parts;
+        }
 #pragma unroll
         for (int i = 0; i < kHeads; ++i) {
             const int h = i * F::kGroups + group;
@@ -216,61 +220,72 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(Args A, int vec) {
             if (!sg.whole) { part[tid] = sm.m[tid]; part[kMaxHeads + tid] = sm.l[tid]; }
             else if (A.a.lse != nullptr) A.a.lse[(long long)s * A.a.H + h0 + tid] = sm.l[tid] > 0.f ? (sm.m[tid] + log2f(sm.l[tid])) * kLn2 : -CUDART_INF_F;
         }
-        u += sg.units;
     }
-    record_bad(A, bad);
+    leave_to_joins(A, left, bad);
 }
 
 // ----------------------------------------------------------------------------------------------
-// The pieces of a head joined. CTA c stands for the border between the shares c and c + 1: the first border within an
-// owner's units has the join of all of them. One more CTA writes the header.
+// The pieces of an owner joined, a query head a CTA: column c of the grid has what CTA c of the first kernel left. One more column
+// writes the header. Its time is that of loads that wait for one another (what is left; m, l and the first of O), and of its launch.
 // ----------------------------------------------------------------------------------------------
 template <class T>
-__global__ void __launch_bounds__(kThreads) join_kernel(Args A) {
-    const CacheGeom &c = A.a.c;
-    const int tid = threadIdx.x, lane = tid & 31;
+__global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ Args A) {
+    const int tid = threadIdx.x, lane = tid & 31, h = blockIdx.y, d = A.a.c.d;
+    __shared__ unsigned any;
+    __shared__ float f[kMaxGrid];
+    __shared__ float wm[kThreads / 32], wl[kThreads / 32];
+    if (tid == 0) any = 0;
     after_previous_kernel();
-    if ((int)blockIdx.x == A.grid - 1) {
-        __shared__ unsigned any;
-        if (tid == 0) any = 0;
+    if ((int)blockIdx.x == A.grid) {
+        if (h != 0) return;
         __syncthreads();
         for (int i = tid; i < A.grid; i += kThreads)
-            if (A.bad[i] != 0) atomicMax(&any, A.bad[i]);
+            if (A.left[i].bad != 0) atomicMax(&any, A.left[i].bad);
         for (int i = tid; i < (int)sizeof(WorkspaceHeader) / 4; i += kThreads) reinterpret_cast<unsigned *>(A.header)[i] = 0;
         __syncthreads();
         if (tid == 0) {
-            A.header->rows = (unsigned long long)c.n_slots * A.a.H;
+            A.header->rows = (unsigned long long)A.a.c.n_slots * A.a.H;
             if (any != 0) { A.header->error = 701; A.header->error_info = any - 1; }
         }
         return;
     }
-    const long long all = all_units(c, lane) * A.per_slot;
-    const Share left = share_of(A, all, (int)blockIdx.x);
-    const long long border = left.end;
-    if (border >= all || left.first >= border) return;
-    const Place at = place_of(c, A.per_slot, border, lane, {0, 0, 0});
-    const int owner = (int)((border - at.first) / at.units);
-    const long long first = at.first + (long long)owner * at.units, end = first + at.units;
-    if (border == first || left.first > first) return;  // (no owner is cut here, or not for the first time)
-    const int cta0 = (int)blockIdx.x, cta1 = (int)((end - 1) / left.per);  // all that have some of it
-    const int s = at.slot, kvh = owner / A.chunks, h0 = kvh * A.a.hpg + owner % A.chunks * kMaxHeads;
-    const int nh = min(kMaxHeads, A.a.hpg - owner % A.chunks * kMaxHeads), d = c.d;
-    auto piece = [&](int x) { return part_of(A, x, x == cta0 && left.first != first ? 1 : 0); };
-    T *const out = (T *)A.a.out;
-    for (int i = tid; i < nh * d; i += kThreads) {
-        const int h = i / d;
-        float m = -CUDART_INF_F, l = 0.f, o = 0.f;
-        for (int x = cta0; x <= cta1; ++x) m = fmaxf(m, piece(x)[h]);
-        const float base = m == -CUDART_INF_F ? 0.f : m;
-        for (int x = cta0; x <= cta1; ++x) {
-            const float *const p = piece(x);
-            const float f = fast_exp2(p[h] - base);
-            l = fmaf(f, p[kMaxHeads + h], l);
-            o = fmaf(f, p[2 * kMaxHeads + i], o);
-        }
-        out[((long long)s * A.a.H + h0) * d + i] = (T)(l > 0.f ? o / l : 0.f);
-        if (A.a.lse != nullptr && i % d == 0) A.a.lse[(long long)s * A.a.H + h0 + h] = l > 0.f ? (m + log2f(l)) * kLn2 : -CUDART_INF_F;
+    const Left left = A.left[blockIdx.x];
+    if (h >= left.heads || left.n == 0) return;
+    const int n = left.n;
+    auto piece = [&](int x) { return part_of(A, (int)blockIdx.x + x, x == 0 ? left.which : 0); };
+    constexpr int kFirst = 8;
+    float first[kFirst], ls = 0.f, m = -CUDART_INF_F;  // O of the first pieces (this thread's channel); l of piece tid
+#pragma unroll
+    for (int x = 0; x < kFirst; ++x) first[x] = x < n && tid < d ? piece(x)[2 * kMaxHeads + h * d + tid] : 0.f;
+    for (int x = tid; x < n; x += kThreads) m = fmaxf(m, f[x] = piece(x)[h]);
+    if (tid < n) ls = piece(tid)[kMaxHeads + h];
+    m = warp_maximum(m);
+    if (lane == 0) wm[tid >> 5] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(wm[0], wm[1]), fmaxf(wm[2], wm[3]));
+    const float base = m == -CUDART_INF_F ? 0.f : m;
+    float l = 0.f;
+    for (int x = tid; x < n; x += kThreads) {
+        f[x] = fast_exp2(f[x] - base);
+        l = fmaf(f[x], x < kThreads ? ls : piece(x)[kMaxHeads + h], l);
     }
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
+    if (lane == 0) wl[tid >> 5] = l;
+    __syncthreads();
+    l = (wl[0] + wl[1]) + (wl[2] + wl[3]);
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const long long to = left.to + h;
+    for (int i = tid; i < d; i += kThreads) {
+        float o = 0.f;
+#pragma unroll
+        for (int x = 0; x < kFirst; ++x)
+            if (x < n) o = fmaf(f[x], i == tid ? first[x] : piece(x)[2 * kMaxHeads + h * d + i], o);
+#pragma unroll 8
+        for (int x = kFirst; x < n; ++x) o = fmaf(f[x], piece(x)[2 * kMaxHeads + h * d + i], o);
+        ((T *)A.a.out)[to * d + i] = (T)(o * inv);
+    }
+    if (A.a.lse != nullptr && tid == 0) A.a.lse[to] = l > 0.f ? (m + log2f(l)) * kLn2 : -CUDART_INF_F;
 }
 
 template <class T, int D>
@@ -291,12 +306,12 @@ cudaError_t launch_fma_d(const Args &A, int vec, cudaStream_t st) {
     }
 }
 
-constexpr size_t kFlagBytes = (kMaxGrid * sizeof(unsigned) + 255) & ~(size_t)255;
+constexpr size_t kLeftBytes = (kMaxGrid * sizeof(Left) + 255) & ~(size_t)255;
 
 }  // namespace
 
 size_t decode_workspace_bytes(const CacheGeom &c) {
-    return sizeof(WorkspaceHeader) + kFlagBytes + (size_t)kMaxGrid * 2 * kMaxHeads * (c.d + 2) * sizeof(float);
+    return sizeof(WorkspaceHeader) + kLeftBytes + (size_t)kMaxGrid * 2 * kMaxHeads * (c.d + 2) * sizeof(float);
 }
 
 stream_status launch_decode(const DecodeCall &a, int dtype, void *workspace, cudaStream_t st) {
@@ -308,9 +323,9 @@ stream_status launch_decode(const DecodeCall &a, int dtype, void *workspace, cud
     A.chunks = (a.hpg + kMaxHeads - 1) / kMaxHeads;
     A.per_slot = a.c.G * A.chunks;
     A.header = (WorkspaceHeader *)workspace;
-    A.bad = (unsigned *)((char *)workspace + sizeof(WorkspaceHeader));
-    A.parts = (float *)((char *)A.bad + kFlagBytes);
-    const long long most = (long long)a.c.n_slots * A.per_slot * (((long long)a.c.max_pages * a.c.page + kUnit - 1) / kUnit);
+    A.left = (Left *)((char *)workspace + sizeof(WorkspaceHeader));
+    A.parts = (float *)((char *)A.left + kLeftBytes);
+    const long long most = (long long)a.c.n_slots * A.per_slot * (((long long)a.c.max_pages * a.c.page + kUnit - 1) / kUnit + kOpen);
     const int want = 2 * n_sm < kMaxGrid ? 2 * n_sm : kMaxGrid;
     A.grid = (int)(most < want ? most : want);
     const long long any = (long long)(uintptr_t)a.k | (long long)(uintptr_t)a.v | a.c.s_p * e | a.c.s_t * e | a.c.s_h * e;
@@ -319,8 +334,8 @@ stream_status launch_decode(const DecodeCall &a, int dtype, void *workspace, cud
                      : dtype == STREAM_F32   ? launch_fma_d<float>(A, vec, st)
                                              : launch_fma_d<__nv_bfloat16>(A, vec, st);
     if (rc != cudaSuccess) return cuda_fail(rc, "decode attention launch");
-    rc = dtype == STREAM_F32 ? launch_early(join_kernel<float>, (unsigned)A.grid, kThreads, 0, st, A)
-                             : launch_early(join_kernel<__nv_bfloat16>, (unsigned)A.grid, kThreads, 0, st, A);
+    const dim3 joins(A.grid + 1, a.hpg < kMaxHeads ? a.hpg : kMaxHeads);
+    rc = dtype == STREAM_F32 ? launch_early(join_kernel<float>, joins, kThreads, 0, st, A) : launch_early(join_kernel<__nv_bfloat16>, joins, kThreads, 0, st, A);
     return rc == cudaSuccess ? STREAM_OK : cuda_fail(rc, "decode join launch");
 }
 

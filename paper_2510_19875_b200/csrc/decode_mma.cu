@@ -21,17 +21,18 @@ template <int D>
 struct Form {
     static constexpr int kRow = D * 2;                         // bytes
     static constexpr int kTile = kStep * kRow;
-    static constexpr int kStages = D == 64 ? 6 : 3;
-    static constexpr int kWarp = kStages * 2 * kTile;          // bytes of a warp's ring; in the end its O, fp32
+    static constexpr int kStages = D == 64 ? 4 : 3;              // steps in the ring (their keys' flags fit 64 bits)
+    static constexpr int kWarp = kStages * 2 * kTile;          // bytes of a warp's ring
     static constexpr bool kQInRegs = D <= 128;
     static constexpr int kCtas = D <= 128 ? 2 : 1;             // of an SM
-    static_assert(kMaxHeads * D * 4 <= kWarp, "O over the ring");
+    static_assert(kMaxHeads * D * 4 <= 2 * kTile && kStages <= 4, "O in the place of a step");
 };
 template <int D>
 struct Smem {
     unsigned char ring[kThreads / 32][Form<D>::kWarp];
     unsigned char q[kMaxHeads * Form<D>::kRow];
     float m[kThreads / 32][kMaxHeads], l[kThreads / 32][kMaxHeads];
+    unsigned o_at[kThreads / 32];  // where in its ring a warp has left its O
 };
 
 __device__ __forceinline__ void ldmatrix4(unsigned addr, unsigned &a, unsigned &b, unsigned &c, unsigned &d) {
@@ -54,77 +55,100 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas) decode_mma_kernel(co
     after_previous_kernel();
     __nv_bfloat16 *const out = (__nv_bfloat16 *)A.a.out;
     write_empty_slots<__nv_bfloat16>(A);
-    const Share mine = share_of(A, all_units(c, lane) * A.per_slot, (int)blockIdx.x);
-    const unsigned ring = wp::smem_addr(sm.ring[warp]), q_smem = wp::smem_addr(sm.q);
+    const Share mine = share_of(A, all_places(A, lane), (int)blockIdx.x);
+    unsigned char *const ring_ptr = sm.ring[warp];
+    const unsigned ring = wp::smem_addr(ring_ptr), q_smem = wp::smem_addr(sm.q);
     const bool one_page = c.page % kStep == 0;  // a tile's keys lie side by side
-    constexpr int kPieces = D / 8, kRowsAtOnce = kPieces >= 32 ? 1 : 32 / kPieces;  // of a row; rows that 32 lanes fetch at once
-    constexpr int kPerRow = kPieces > 32 ? kPieces / 32 : 1;
-    static_assert(kPerRow == 1, "a row is at most 512 bytes");
+    constexpr int kPieces = D / 8, kRowsAtOnce = 32 / kPieces;  // of a row; rows that 32 lanes fetch at once
     const int row_l = lane / kPieces, piece_l = lane % kPieces;
     // ldmatrix rows of this lane
     const int k_row = (lane >> 4) * 8 + (lane & 7), k_half = (lane >> 3) & 1, v_row = ((lane >> 3) & 1) * 8 + (lane & 7), v_half = lane >> 4;
     unsigned bad = 0;
-    Place at = {0, 0, 0};
-    for (long long u = mine.first; u < mine.end;) {
-        at = place_of(c, A.per_slot, u, lane, at);
-        const Segment sg = segment_of(A, at, u, mine.end);
-        const int s = at.slot;
-        const int32_t *const table = c.table + (long long)s * c.max_pages;
-        const __nv_bfloat16 *const ks = (const __nv_bfloat16 *)A.a.k + (long long)sg.kvh * c.s_h, *const vs = (const __nv_bfloat16 *)A.a.v + (long long)sg.kvh * c.s_h;
-        const int n_steps = (sg.key_end - sg.key0 - warp * kStep + 4 * kStep - 1) / (4 * kStep);  // of this warp (0 or fewer: none)
-        // Lane i < 16: the page of key i of the warp's step n, -1: none
-        auto page_of = [&](int n) -> int {
-            const int key = sg.key0 + (4 * n + warp) * kStep + lane;
-            if (n >= n_steps || lane >= kStep || key >= sg.key_end) return -1;
-            const int page = table[key / c.page];
-            if ((unsigned)page < (unsigned)c.n_pages) return page;
-            bad = (unsigned)s + 1u;
-            return -1;
-        };
-        auto fetch = [&](int n, int page) -> unsigned {  // the step's tiles; which of its keys are there
-            const unsigned there = __ballot_sync(0xffffffffu, page >= 0);
-            const int key = sg.key0 + (4 * n + warp) * kStep + lane;
-            const long long own = page >= 0 ? (long long)page * c.s_p + (long long)(key % c.page) * c.s_t : 0;
-            const unsigned dst = ring + (n % F::kStages) * 2 * F::kTile;
-            const long long base = __shfl_sync(0xffffffffu, own, 0);
+    // What this warp fetches: its steps of the segment that is open, step n in the ring's place (at + n) % kStages
+    const int32_t *table = nullptr;
+    const __nv_bfloat16 *ks = nullptr, *vs = nullptr;
+    int slot = 0, key_w = 0, key_end = 0, n_steps = 0;
+    unsigned at = 0;
+    unsigned long long keys_there = 0;  // 16 flags a place of the ring
+    int page = -1;                      // lane i < 16: the page of key i of the next step to be fetched, -1: none
+    auto page_of = [&](int n) -> int {
+        const int key = key_w + 4 * n * kStep + lane;
+        if (n >= n_steps || lane >= kStep || key >= key_end) return -1;
+        const int x = table[key / c.page];
+        if ((unsigned)x < (unsigned)c.n_pages) return x;
+        bad = (unsigned)slot + 1u;
+        return -1;
+    };
+    auto fetch = [&](int n) {  // step n, and the pages of the one after it are looked up
+        const int own_page = page;
+        page = page_of(n + 1);
+        if (n < n_steps) {
+            const unsigned place = (at + (unsigned)n) % F::kStages, there = __ballot_sync(0xffffffffu, own_page >= 0);
+            keys_there = (keys_there & ~(0xffffull << (16 * place))) | (unsigned long long)there << (16 * place);
+            const int key = key_w + 4 * n * kStep + lane;
+            const long long own = own_page >= 0 ? (long long)own_page * c.s_p + (long long)(key % c.page) * c.s_t : 0;
+            const unsigned dst = ring + place * 2 * F::kTile;
+            const long long base = __shfl_sync(0xffffffffu, own, 0) + row_l * c.s_t;
 #pragma unroll
             for (int r0 = 0; r0 < kStep; r0 += kRowsAtOnce) {
                 const int r = r0 + row_l;
                 const bool is = (there >> r) & 1u;
-                long long e = one_page ? base + r * c.s_t : 0;
+                long long e = base + r0 * c.s_t;
                 if (!one_page) e = __shfl_sync(0xffffffffu, own, r);
                 e = (is ? e : 0) + piece_l * 8;
                 const unsigned to = dst + piece_at<D>(r, piece_l);
                 cp_async16(to, ks + e, is);
                 cp_async16(to + F::kTile, vs + e, is);
             }
-            return there;
-        };
-        // the first tiles are on their way before anything else
-        unsigned there[F::kStages];  // of the steps in the ring
-        int page = page_of(0);
-#pragma unroll
-        for (int n = 0; n < F::kStages - 1; ++n) {
-            const int next = page_of(n + 1);
-            there[n] = n < n_steps ? fetch(n, page) : 0u;
-            cp_commit();
-            page = next;
         }
-        for (int i = tid; i < kMaxHeads * kPieces; i += kThreads) {
-            const int h = i / kPieces, x = i % kPieces;
-            const __nv_bfloat16 *const src = (const __nv_bfloat16 *)A.a.q + (long long)s * A.a.qs_s + (long long)(sg.h0 + h) * A.a.qs_h + x * 8;
-            uint4 w = make_uint4(0, 0, 0, 0);
+        cp_commit();
+    };
+    constexpr int kQ = kMaxHeads * kPieces / kThreads;  // pieces of Q a thread
+    uint4 qr[kQ];
+    // The first steps of a segment are on their way before the one before it is written out, and so is its Q
+    auto open = [&](const Segment &sg) {
+        at += (unsigned)n_steps;
+        slot = sg.slot;
+        table = c.table + (long long)slot * c.max_pages;
+        ks = (const __nv_bfloat16 *)A.a.k + (long long)sg.kvh * c.s_h;
+        vs = (const __nv_bfloat16 *)A.a.v + (long long)sg.kvh * c.s_h;
+        key_w = sg.key0 + warp * kStep;
+        key_end = sg.key_end;
+        n_steps = key_end > key_w ? (key_end - key_w + 4 * kStep - 1) / (4 * kStep) : 0;
+        page = page_of(0);
+#pragma unroll
+        for (int i = 0; i < kQ; ++i) {
+            const int h = (tid + i * kThreads) / kPieces, x = (tid + i * kThreads) % kPieces;
+            const __nv_bfloat16 *const src = (const __nv_bfloat16 *)A.a.q + (long long)slot * A.a.qs_s + (long long)(sg.h0 + h) * A.a.qs_h + x * 8;
+            qr[i] = make_uint4(0, 0, 0, 0);
             if (h < sg.heads) {
                 if (A.q_vec) {
-                    w = *reinterpret_cast<const uint4 *>(src);
+                    qr[i] = *reinterpret_cast<const uint4 *>(src);
                 } else {
-                    __nv_bfloat16 y[8];
+                    unsigned y[4];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) y[e] = src[e];
-                    w = *reinterpret_cast<const uint4 *>(y);
+                    for (int e = 0; e < 4; ++e) {
+                        const __nv_bfloat162 two = __halves2bfloat162(src[2 * e], src[2 * e + 1]);
+                        y[e] = *reinterpret_cast<const unsigned *>(&two);
+                    }
+                    qr[i] = make_uint4(y[0], y[1], y[2], y[3]);
                 }
             }
-            *reinterpret_cast<uint4 *>(sm.q + piece_at<D>(h, x)) = w;
+        }
+#pragma unroll
+        for (int n = 0; n < F::kStages - 1; ++n) fetch(n);
+    };
+    Place pl = {0, 0, 0};
+    int n_parts = 0;
+    Left left = {};
+    Segment sg = open_segment(A, mine.first, mine.end, lane, pl);
+    if (sg.next >= 0) open(sg);
+    while (sg.next >= 0) {
+        const int s = sg.slot;
+#pragma unroll
+        for (int i = 0; i < kQ; ++i) {
+            const int h = (tid + i * kThreads) / kPieces, x = (tid + i * kThreads) % kPieces;
+            *reinterpret_cast<uint4 *>(sm.q + piece_at<D>(h, x)) = qr[i];
         }
         __syncthreads();
         const unsigned q_addr = q_smem + (lane & 15) * F::kRow;
@@ -139,8 +163,12 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas) decode_mma_kernel(co
 #pragma unroll
             for (int y = 0; y < 4; ++y) o[x][y] = 0.f;
         float ref[2] = {-CUDART_INF_F, -CUDART_INF_F}, l[2] = {0.f, 0.f};  // of rows quad and quad + 8, in units of log2
-        auto step = [&](int n, unsigned keys) {
-            const unsigned kt = ring + (n % F::kStages) * 2 * F::kTile, vt = kt + F::kTile;
+        for (int n = 0; n < n_steps; ++n) {
+            fetch(n + F::kStages - 1);
+            cp_wait<F::kStages - 1>();
+            __syncwarp();
+            const unsigned place = (at + (unsigned)n) % F::kStages, keys = (unsigned)(keys_there >> (16 * place)) & 0xffffu;
+            const unsigned kt = ring + place * 2 * F::kTile, vt = kt + F::kTile;
             float sc[2][4];
 #pragma unroll
             for (int x = 0; x < 2; ++x)
@@ -199,26 +227,17 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas) decode_mma_kernel(co
                 wp::mma_bf16(o[2 * x], pa[0], pa[1], pa[2], pa[3], b[0], b[1]);
                 wp::mma_bf16(o[2 * x + 1], pa[0], pa[1], pa[2], pa[3], b[2], b[3]);
             }
-        };
-        // (the ring's places by name, so that what is there of each stays in registers)
-        for (int n0 = 0; n0 < n_steps; n0 += F::kStages) {
-#pragma unroll
-            for (int x = 0; x < F::kStages; ++x) {
-                const int n = n0 + x;
-                if (n < n_steps) {
-                    const int ahead = n + F::kStages - 1, next = page_of(ahead + 1);
-                    there[(x + F::kStages - 1) % F::kStages] = ahead < n_steps ? fetch(ahead, page) : 0u;
-                    cp_commit();
-                    page = next;
-                    cp_wait<F::kStages - 1>();
-                    __syncwarp();
-                    step(n, there[x]);
-                    __syncwarp();  // (the tile is read before its place is filled again)
-                }
-            }
+            __syncwarp();  // (the tile is read before its place is filled again)
         }
-        cp_wait<0>();
-        __syncwarp();
+        const Segment next = open_segment(A, sg.next, mine.end, lane, pl);
+        if (next.next >= 0) {
+            open(next);
+        } else {
+            at += (unsigned)n_steps;
+            cp_wait<0>();
+        }
+        // the place behind the first steps of the next segment is free: for O
+        const unsigned o_place = (at + F::kStages - 1) % F::kStages * 2 * F::kTile;
         // the four warps' m, l and O meet
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
@@ -226,14 +245,19 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas) decode_mma_kernel(co
             l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
             if ((lane & 3) == 0) { sm.m[warp][quad + 8 * r] = ref[r]; sm.l[warp][quad + 8 * r] = l[r]; }
         }
-        float *const own = reinterpret_cast<float *>(sm.ring[warp]);
+        float *const own = reinterpret_cast<float *>(ring_ptr + o_place);
+        if (lane == 0) sm.o_at[warp] = o_place;
 #pragma unroll
         for (int x = 0; x < D / 8; ++x) {
             *reinterpret_cast<float2 *>(own + quad * D + x * 8 + (lane & 3) * 2) = make_float2(o[x][0], o[x][1]);
             *reinterpret_cast<float2 *>(own + (quad + 8) * D + x * 8 + (lane & 3) * 2) = make_float2(o[x][2], o[x][3]);
         }
         __syncthreads();
-        float *const part = part_of(A, (int)blockIdx.x, u == mine.first ? 0 : 1);
+        float *const part = part_of(A, (int)blockIdx.x, n_parts);
+        if (!sg.whole) {
+            if (sg.key0 == 0) left = {pieces_of(sg, mine), n_parts, sg.heads, 0u, (long long)sg.slot * A.a.H + sg.h0, 0ll};
+            ++n_parts;
+        }
         for (int i = tid; i < sg.heads * (D / 4); i += kThreads) {
             const int h = i / (D / 4), x = (i % (D / 4)) * 4;
             float m = sm.m[0][h];
@@ -245,7 +269,7 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas) decode_mma_kernel(co
 #pragma unroll
             for (int w = 0; w < kThreads / 32; ++w) {
                 const float f = fast_exp2(sm.m[w][h] - base);
-                const float4 z = *reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(sm.ring[w]) + h * D + x);
+                const float4 z = *reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(sm.ring[w] + sm.o_at[w]) + h * D + x);
                 sum = fmaf(f, sm.l[w][h], sum);
                 y.x = fmaf(f, z.x, y.x); y.y = fmaf(f, z.y, y.y); y.z = fmaf(f, z.z, y.z); y.w = fmaf(f, z.w, y.w);
             }
@@ -260,10 +284,10 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas) decode_mma_kernel(co
                 if (x == 0) { part[h] = m; part[kMaxHeads + h] = sum; }
             }
         }
-        __syncthreads();  // (the rings are filled again)
-        u += sg.units;
+        __syncthreads();  // (the places of O are filled again)
+        sg = next;
     }
-    record_bad(A, bad);
+    leave_to_joins(A, left, bad);
 }
 
 template <int D>

@@ -39,7 +39,7 @@ __host__ __device__ __forceinline__ int ceil_div(int a, int b) { return (int)(((
 
 // A programmatic dependent (see after_previous_kernel), and clusters of CTAs.
 template <class... K, class... A>
-cudaError_t launch_early(void (*kern)(K...), unsigned grid, unsigned threads, size_t smem, cudaStream_t st, A &&...args) {
+cudaError_t launch_early(void (*kern)(K...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st, A &&...args) {
     return launch_kernel(kern, grid, threads, smem, st, 1u, std::forward<A>(args)...);
 }
 template <class... K, class... A>
