@@ -291,7 +291,8 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ 
 template <class T, int D>
 cudaError_t launch_fma(const Args &A, int vec, cudaStream_t st) {
     const int smem = (int)sizeof(Smem<T, D>);
-    cudaError_t e = cudaFuncSetAttribute(decode_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    static DeviceFlags done;
+    cudaError_t e = allow_smem(decode_kernel<T, D>, smem, done);
     if (e != cudaSuccess) return e;
     return launch_early(decode_kernel<T, D>, (unsigned)A.grid, kThreads, smem, st, A, vec);
 }

@@ -293,7 +293,8 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas) decode_mma_kernel(co
 template <int D>
 cudaError_t launch(Args &A, int n_sm, cudaStream_t st) {
     const int smem = (int)sizeof(Smem<D>);
-    cudaError_t e = cudaFuncSetAttribute(decode_mma_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    static DeviceFlags done;
+    cudaError_t e = allow_smem(decode_mma_kernel<D>, smem, done);
     if (e != cudaSuccess) return e;
     const int most = Form<D>::kCtas * n_sm;
     if (A.grid > most) A.grid = most;

@@ -264,7 +264,8 @@ __global__ void __launch_bounds__(kThreads) prompt_kernel(PromptGeom g, const T 
 template <class T, int D>
 stream_status launch(const PromptGeom &g, const void *q, const void *k, const void *v, cudaStream_t st) {
     const int smem = (int)sizeof(Smem<D>);
-    cudaError_t e = cudaFuncSetAttribute(prompt_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    static DeviceFlags done;
+    cudaError_t e = allow_smem(prompt_kernel<T, D>, smem, done);
     if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(prompt)");
     // no more row tiles than this, however the rows are dealt to the sequences
     const long long tiles = ((long long)g.total_q * g.hpg / kRows + (g.n_seqs < g.total_q ? g.n_seqs : g.total_q)) * g.G;

@@ -520,7 +520,8 @@ stream_status launch(const PromptGeom &g, const void *q, const void *k, const vo
     if (rc != STREAM_OK) return rc;
     const int smem = (2 + F::kStages) * F::kTile + (int)sizeof(Tail<F>) + 1024;
     static_assert((2 + F::kStages) * F::kTile + (int)sizeof(Tail<F>) + 1024 <= 232448, "what a CTA may have");
-    cudaError_t e = cudaFuncSetAttribute(prompt_tc_kernel<F>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    static DeviceFlags done;
+    cudaError_t e = allow_smem(prompt_tc_kernel<F>, smem, done);
     if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(prompt_tc)");
     const int n_sm = current_sm_count();
     if (n_sm <= 0) { set_error("cannot read the SM count of the current device"); return STREAM_ERR_CUDA; }

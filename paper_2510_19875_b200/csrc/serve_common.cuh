@@ -2,6 +2,8 @@
 #pragma once
 #include <math_constants.h>
 
+#include <atomic>
+
 #include "common.cuh"
 
 namespace stream {
@@ -47,14 +49,37 @@ cudaError_t launch_clusters(void (*kern)(K...), unsigned grid, unsigned threads,
     return launch_kernel(kern, grid, threads, smem, st, cluster, std::forward<A>(args)...);
 }
 
-// SMs of the current device (devices of one machine may differ, and a process may use several).
+// What a short call need not ask the runtime every time, by device (a process may use several, and they may differ).
+constexpr int kMaxDevices = 64;
+inline int current_device() {
+    int dev = -1;
+    if (cudaGetDevice(&dev) == cudaSuccess) return dev;
+    (void)cudaGetLastError();
+    return -1;
+}
 inline int current_sm_count() {
-    int dev = 0, n = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+    static std::atomic<int> known[kMaxDevices];
+    const int dev = current_device();
+    if (dev < 0) return 0;
+    int n = dev < kMaxDevices ? known[dev].load(std::memory_order_relaxed) : 0;
+    if (n > 0) return n;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
         (void)cudaGetLastError();
         return 0;
     }
+    if (dev < kMaxDevices) known[dev].store(n, std::memory_order_relaxed);
     return n;
+}
+// Dynamic shared memory of a kernel beyond 48 KB; `done`: of that kernel.
+typedef std::atomic<unsigned long long> DeviceFlags;
+template <class... K>
+cudaError_t allow_smem(void (*kern)(K...), int bytes, DeviceFlags &done) {
+    const int dev = current_device();
+    const unsigned long long bit = dev >= 0 && dev < kMaxDevices ? 1ull << dev : 0ull;
+    if ((done.load(std::memory_order_relaxed) & bit) != 0) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+    return e;
 }
 
 bool prompt_tc_supported(const PromptGeom &g, int dtype, const void *q, const void *k, const void *v);

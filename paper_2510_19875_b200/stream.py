@@ -143,9 +143,10 @@ def _load():
     lib.stream_run_host.argtypes = [P, vp, vp, vp, vp, vp, ctypes.c_float, vp, sz, vp]
     lib.stream_run_host_var.restype = ctypes.c_int
     lib.stream_run_host_var.argtypes = [P, vp, vp, vp, vp, vp, vp, ctypes.c_float, vp, sz, vp]
-    PP, PC, i32, i64 = ctypes.POINTER(StreamPrompt), ctypes.POINTER(StreamCache), ctypes.c_int32, ctypes.c_int64
+    PC, i32, i64 = ctypes.POINTER(StreamCache), ctypes.c_int32, ctypes.c_int64
     lib.stream_prompt_attention.restype = ctypes.c_int
-    lib.stream_prompt_attention.argtypes = [PP, vp, vp, vp, vp, vp, ctypes.c_float, vp, vp, vp]
+    lib.stream_prompt_attention.argtypes = [vp, vp,  # (the struct, or its bytes)
+                                             vp, vp, vp, vp, ctypes.c_float, vp, vp, vp]
     lib.stream_cache_workspace_bytes.restype = sz
     lib.stream_cache_workspace_bytes.argtypes = [PC]
     lib.stream_cache_reserve.restype = ctypes.c_int
@@ -579,27 +580,25 @@ _DTYPES = {torch.float32: STREAM_F32, torch.bfloat16: STREAM_BF16}
 
 
 def _checked(x: torch.Tensor, dtype, shape, what: str, device) -> torch.Tensor:
-    if x.dtype is not dtype or not x.is_contiguous() or tuple(x.shape) != tuple(shape) or x.device != device:
+    if x.dtype is not dtype or not x.is_contiguous() or x.shape != shape or x.device != device:
         raise ValueError(f"{what} must be a contiguous {str(dtype)[6:]} tensor of shape {tuple(shape)} on {device}")
     return x
 
 
-class _Here:
-    def __enter__(self):
-        return None
+def _launch(device: torch.device, call, args, stream) -> None:
+    """``call(*args, stream)`` with the tensors' device as the current one (the way to another device and back is taken
+    only where it is another; of the host's time a short call takes, half is argument handling)."""
+    if device.index == (torch.cuda.current_device() if _raw_stream is None else _current_device()):
+        status = call(*args, _stream_handle(stream))
+    else:
+        with torch.cuda.device(device):
+            status = call(*args, _stream_handle(stream))
+    if status:
+        _raise(status)
 
-    def __exit__(self, *exc):
-        return False
 
-
-_HERE_ALREADY = _Here()
-
-
-def _on(device: torch.device):
-    """The tensors' device as the current one, for a launch."""
-    if device.index is None or device.index == torch.cuda.current_device():
-        return _HERE_ALREADY
-    return torch.cuda.device(device)
+_PROMPT = struct.Struct("@iiiiqqiiqqqq")  # StreamPrompt's fields
+assert _PROMPT.size == ctypes.sizeof(StreamPrompt)
 
 
 def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor, cu_k: torch.Tensor | None = None, *,
@@ -611,31 +610,42 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: to
     ``lse_out``) also the logarithms of the softmax sums, float32 ``[H, total_q]``. Rows of no sequence are left as they are."""
     if not (q.is_cuda and k.is_cuda and v.is_cuda and cu_q.is_cuda):
         raise ValueError("q, k, v and cu_q must be CUDA tensors (there is no CPU path)")
-    if q.dim() != 3 or k.dim() != 3 or q.shape[2] != k.shape[2]:
+    qs, ks, q_strides, k_strides, dtype, device = q.shape, k.shape, q.stride(), k.stride(), q.dtype, q.device
+    if len(qs) != 3 or len(ks) != 3 or qs[2] != ks[2]:
         raise ValueError("q must be [total_q, H, d] and k [total_k, G, d]")
-    if v.shape != k.shape or v.stride() != k.stride():
+    if v.shape != ks or v.stride() != k_strides:
         raise ValueError("v must have k's shape and strides")
-    if q.dtype not in _DTYPES or k.dtype is not q.dtype or v.dtype is not q.dtype:
+    if dtype not in _DTYPES or k.dtype is not dtype or v.dtype is not dtype:
         raise ValueError("q, k and v must all be float32 or all bfloat16")
-    if q.stride(2) != 1 or k.stride(2) != 1:
+    if q_strides[2] != 1 or k_strides[2] != 1:
         raise ValueError("innermost stride must be 1")
-    device = q.device
     if k.device != device or v.device != device:
         raise ValueError("q, k and v must be on one device")
-    if cu_q.dim() != 1 or cu_q.shape[0] < 2:
+    n = cu_q.shape
+    if len(n) != 1 or n[0] < 2:
         raise ValueError("cu_q must be [n_seqs + 1]")
-    _checked(cu_q, torch.int32, cu_q.shape, "cu_q", device)
-    cu_k = cu_q if cu_k is None else _checked(cu_k, torch.int32, cu_q.shape, "cu_k", device)
-    total, H, d = q.shape
-    p = StreamPrompt(cu_q.shape[0] - 1, H, k.shape[1], d, total, k.shape[0], int(causal), _DTYPES[q.dtype], q.stride(0), q.stride(1),
-                     k.stride(0), k.stride(1))
-    out = _empty((total, H, d), q.dtype, device) if out is None else _checked(out, q.dtype, (total, H, d), "out", device)
+    _checked(cu_q, torch.int32, n, "cu_q", device)
+    if cu_k is None:
+        cu_k = cu_q
+    elif cu_k is not cu_q:
+        _checked(cu_k, torch.int32, n, "cu_k", device)
+    total, H, d = qs
+    fields = (n[0] - 1, H, ks[1], d, total, ks[0], int(causal), _DTYPES[dtype], q_strides[0], q_strides[1], k_strides[0], k_strides[1])
+    try:
+        p = _PROMPT.pack(*fields)
+    except struct.error:  # sizes beyond 32 bits: the library's to refuse
+        p = ctypes.byref(StreamPrompt(*fields))
+    if out is None:
+        out = torch.empty_strided(qs, (H * d, d, 1), dtype=dtype, device=device)
+    else:
+        _checked(out, dtype, qs, "out", device)
     if lse_out is not None:
         _checked(lse_out, torch.float32, (H, total), "lse_out", device)
     elif want_lse:
-        lse_out = _empty((H, total), torch.float32, device)
-    with _on(device):
-        stream_prompt_attention(p, q, k, v, cu_q, cu_k, scale, out, lse_out, stream)
+        lse_out = torch.empty_strided((H, total), (total, 1), dtype=torch.float32, device=device)
+    _launch(device, (_lib or _load()).stream_prompt_attention,
+            (p, q.data_ptr(), k.data_ptr(), v.data_ptr(), cu_q.data_ptr(), cu_k.data_ptr(), scale, out.data_ptr(),
+             None if lse_out is None else lse_out.data_ptr()), stream)
     return out if lse_out is None else (out, lse_out)
 
 
@@ -679,9 +689,16 @@ class PagedCache:
         if n == 0:
             raise StreamError(STREAM_ERR_INVALID_ARG, stream_last_error())
         self.workspace = _empty((n,), torch.uint8, self.device)
+        self._p = ctypes.byref(self.struct)
+        self._decode_bytes = {}  # workspace of decode_attention by query heads
 
-    def _ledger(self):
-        return self.page_table.data_ptr(), self.seq_len.data_ptr(), self.ref_count.data_ptr()
+    def _ledger(self, call, first, *rest, stream):
+        """One of the ledger calls: what it is asked, the ledger, what it gives back, the workspace."""
+        table, length, count, ws = self.page_table, self.seq_len, self.ref_count, self.workspace
+        _launch(self.device, call, (self._p, *first, table.data_ptr(), length.data_ptr(), count.data_ptr(), *rest, ws.data_ptr(), ws.numel()), stream)
+
+    def _info(self):
+        return torch.empty_strided((4,), (1,), dtype=torch.int32, device=self.device)
 
 
 def new_cache(n_slots: int, n_pages: int, page_size: int, max_pages: int, n_kv_heads: int, d: int, *, n_layers: int = 1,
@@ -697,9 +714,8 @@ def cache_reserve(cache: PagedCache, n_new: torch.Tensor, stream=None) -> torch.
     the info ``[done, pages taken, free pages, refusals]`` (int32, on the device)."""
     c = cache
     _checked(n_new, torch.int32, (c.n_slots,), "n_new", c.device)
-    info = _empty((4,), torch.int32, c.device)
-    with _on(c.device):
-        stream_cache_reserve(c.struct, n_new, *c._ledger(), info, c.workspace, c.workspace.numel(), stream)
+    info = c._info()
+    c._ledger((_lib or _load()).stream_cache_reserve, (n_new.data_ptr(),), info.data_ptr(), stream=stream)
     return info
 
 
@@ -708,9 +724,8 @@ def cache_fork(cache: PagedCache, parent: torch.Tensor, stream=None) -> CacheMov
     ``parent[s]``. Full pages are shared; the copies of the others are due: hand the result to :func:`cache_copy_pages`."""
     c = cache
     _checked(parent, torch.int32, (c.n_slots,), "parent", c.device)
-    info, pairs = _empty((4,), torch.int32, c.device), _empty((c.n_slots, 2), torch.int32, c.device)
-    with _on(c.device):
-        stream_cache_fork(c.struct, parent, *c._ledger(), pairs, info, c.workspace, c.workspace.numel(), stream)
+    info, pairs = c._info(), torch.empty_strided((c.n_slots, 2), (2, 1), dtype=torch.int32, device=c.device)
+    c._ledger((_lib or _load()).stream_cache_fork, (parent.data_ptr(),), pairs.data_ptr(), info.data_ptr(), stream=stream)
     return CacheMoves(pairs, info)
 
 
@@ -718,43 +733,43 @@ def cache_free(cache: PagedCache, done: torch.Tensor, stream=None) -> torch.Tens
     """Empties every slot with ``done[s] != 0`` (int32 ``[n_slots]``). Returns ``[1, pages freed, free pages, impossible entries]``."""
     c = cache
     _checked(done, torch.int32, (c.n_slots,), "done", c.device)
-    info = _empty((4,), torch.int32, c.device)
-    with _on(c.device):
-        stream_cache_free(c.struct, done, *c._ledger(), info, c.workspace, c.workspace.numel(), stream)
+    info = c._info()
+    c._ledger((_lib or _load()).stream_cache_free, (done.data_ptr(),), info.data_ptr(), stream=stream)
     return info
 
 
 def cache_compact(cache: PagedCache, stream=None) -> CacheMoves:
     """Moves the pages in use to the lowest numbers; the copies are due (:func:`cache_copy_pages`)."""
     c = cache
-    info, pairs = _empty((4,), torch.int32, c.device), _empty((c.n_pages // 2, 2), torch.int32, c.device)
-    with _on(c.device):
-        stream_cache_compact(c.struct, *c._ledger(), pairs, info, c.workspace, c.workspace.numel(), stream)
+    info, pairs = c._info(), torch.empty_strided((c.n_pages // 2, 2), (2, 1), dtype=torch.int32, device=c.device)
+    c._ledger((_lib or _load()).stream_cache_compact, (), pairs.data_ptr(), info.data_ptr(), stream=stream)
     return CacheMoves(pairs, info)
 
 
 def cache_copy_pages(cache: PagedCache, moves: CacheMoves, stream=None) -> None:
     """Makes the copies that :func:`cache_fork` or :func:`cache_compact` asks for, in all layers."""
-    c = cache
-    _checked(moves.pairs, torch.int32, (moves.pairs.shape[0], 2), "pairs", c.device)
-    _checked(moves.info, torch.int32, (4,), "info", c.device)
-    with _on(c.device):
-        stream_cache_copy_pages(c.struct, c.k, c.v, moves.pairs, moves.info.data_ptr() + 4, moves.pairs.shape[0], stream)
+    c, pairs, info = cache, moves.pairs, moves.info
+    n = pairs.shape[0]
+    _checked(pairs, torch.int32, (n, 2), "pairs", c.device)
+    _checked(info, torch.int32, (4,), "info", c.device)
+    _launch(c.device, (_lib or _load()).stream_cache_copy_pages,
+            (c._p, c.k.data_ptr(), c.v.data_ptr(), pairs.data_ptr(), info.data_ptr() + 4, n), stream)
 
 
 def cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, cu_new: torch.Tensor, *, layer: int = 0, stream=None) -> None:
     """Writes new tokens' keys and values (``[total, n_kv_heads, d]``, rows ``cu_new[s] .. cu_new[s + 1]`` being slot s's
     last tokens) to the pages of one layer, after :func:`cache_reserve`."""
-    c = cache
-    if k.dim() != 3 or tuple(k.shape[1:]) != (c.n_kv_heads, c.d) or v.shape != k.shape or v.stride() != k.stride():
+    c, shape, strides = cache, k.shape, k.stride()
+    if len(shape) != 3 or shape[1] != c.n_kv_heads or shape[2] != c.d or v.shape != shape or v.stride() != strides:
         raise ValueError("k and v must be [total, n_kv_heads, d], alike in strides")
     if k.dtype is not c.k.dtype or v.dtype is not c.k.dtype or k.device != c.device or v.device != c.device:
         raise ValueError("k and v must have the cache's dtype and device")
-    if k.stride(2) != 1:
+    if strides[2] != 1:
         raise ValueError("innermost stride must be 1")
     _checked(cu_new, torch.int32, (c.n_slots + 1,), "cu_new", c.device)
-    with _on(c.device):
-        stream_cache_write(c.struct, layer, k, v, k.shape[0], k.stride(0), k.stride(1), cu_new, c.page_table, c.seq_len, c.k, c.v, stream)
+    _launch(c.device, (_lib or _load()).stream_cache_write,
+            (c._p, layer, k.data_ptr(), v.data_ptr(), shape[0], strides[0], strides[1], cu_new.data_ptr(), c.page_table.data_ptr(),
+             c.seq_len.data_ptr(), c.k.data_ptr(), c.v.data_ptr()), stream)
 
 
 def decode_attention(q: torch.Tensor, cache: PagedCache, *, layer: int = 0, scale: float = 0.0, want_lse: bool = False,
@@ -763,25 +778,31 @@ def decode_attention(q: torch.Tensor, cache: PagedCache, *, layer: int = 0, scal
     """Attention of one new token of every slot, q ``[n_slots, H, d]``, over its cached tokens. Returns the output
     ``[n_slots, H, d]``, with ``want_lse`` (or ``lse_out``) also the logarithms of the softmax sums, float32
     ``[n_slots, H]``. ``workspace``: uint8, at least :func:`stream_decode_workspace_bytes`, one per call that can overlap."""
-    c = cache
-    if q.dim() != 3 or q.shape[0] != c.n_slots or q.shape[2] != c.d or q.dtype is not c.k.dtype or q.device != c.device:
+    c, shape, strides = cache, q.shape, q.stride()
+    if len(shape) != 3 or shape[0] != c.n_slots or shape[2] != c.d or q.dtype is not c.k.dtype or q.device != c.device:
         raise ValueError("q must be [n_slots, H, d] with the cache's dtype and device")
-    if q.stride(2) != 1:
+    if strides[2] != 1:
         raise ValueError("innermost stride must be 1")
-    H = q.shape[1]
-    out = _empty(tuple(q.shape), q.dtype, c.device) if out is None else _checked(out, q.dtype, q.shape, "out", c.device)
+    n, H, d = shape
+    if out is None:
+        out = torch.empty_strided(shape, (H * d, d, 1), dtype=q.dtype, device=c.device)
+    else:
+        _checked(out, q.dtype, shape, "out", c.device)
     if lse_out is not None:
-        _checked(lse_out, torch.float32, (c.n_slots, H), "lse_out", c.device)
+        _checked(lse_out, torch.float32, (n, H), "lse_out", c.device)
     elif want_lse:
-        lse_out = _empty((c.n_slots, H), torch.float32, c.device)
+        lse_out = torch.empty_strided((n, H), (H, 1), dtype=torch.float32, device=c.device)
     if workspace is None:
-        n = stream_decode_workspace_bytes(c.struct, H)
-        if n == 0:
+        need = c._decode_bytes.get(H) or stream_decode_workspace_bytes(c.struct, H)
+        if need == 0:
             raise StreamError(STREAM_ERR_INVALID_ARG, stream_last_error())
-        workspace = _empty((n,), torch.uint8, c.device)
-    elif workspace.dtype is not torch.uint8 or not workspace.is_contiguous() or workspace.device != c.device:
-        raise ValueError("workspace must be a contiguous uint8 tensor on the cache's device")
-    with _on(c.device):
-        stream_decode_attention(c.struct, layer, H, q, q.stride(0), q.stride(1), c.k, c.v, c.page_table, c.seq_len, scale, out, lse_out,
-                                workspace, workspace.numel(), stream)
+        c._decode_bytes[H] = need
+        workspace = torch.empty_strided((need,), (1,), dtype=torch.uint8, device=c.device)
+    else:
+        need = workspace.numel()
+        if workspace.dtype is not torch.uint8 or not workspace.is_contiguous() or workspace.device != c.device:
+            raise ValueError("workspace must be a contiguous uint8 tensor on the cache's device")
+    _launch(c.device, (_lib or _load()).stream_decode_attention,
+            (c._p, layer, H, q.data_ptr(), strides[0], strides[1], c.k.data_ptr(), c.v.data_ptr(), c.page_table.data_ptr(),
+             c.seq_len.data_ptr(), scale, out.data_ptr(), None if lse_out is None else lse_out.data_ptr(), workspace.data_ptr(), need), stream)
     return out if lse_out is None else (out, lse_out)
