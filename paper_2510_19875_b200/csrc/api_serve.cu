@@ -110,6 +110,7 @@ stream_status stream_prompt_attention(const stream_prompt *p, const void *q, con
     g.cu_q = cu_q; g.cu_k = cu_k; g.scale_log2 = scale * 1.4426950408889634f; g.out = out; g.lse = lse_out;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (prompt_tc_supported(g, p->dtype, q, k, v)) return launch_prompt_tc(g, q, k, v, st);
+    if (prompt_mma_supported(g, p->dtype, q, k, v)) return launch_prompt_mma(g, q, k, v, st);
     return launch_prompt_generic(g, p->dtype, q, k, v, st);
 }
 

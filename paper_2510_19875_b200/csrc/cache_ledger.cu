@@ -6,6 +6,7 @@
 // launches. Every thread owns a run of consecutive slots and one of consecutive pages; prefix sums over the threads give each
 // its place among the pages taken, in ascending order. Bound by latency: the loads of one phase and three or four barriers.
 #include "serve_common.cuh"
+#include "warp_common.cuh"
 
 namespace stream {
 namespace {
@@ -26,24 +27,15 @@ struct Shared {
     int cta_sums[3];   // read by the cluster's other CTAs
 };
 
-__device__ __forceinline__ unsigned cluster_size() { unsigned x; asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(x)); return x; }
-__device__ __forceinline__ unsigned cluster_rank() { unsigned x; asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(x)); return x; }
 // All threads of all CTAs; what they wrote before, in global and in shared memory, is there behind it.
 __device__ __forceinline__ void sync_all() {
-    if (cluster_size() == 1) {
+    if (wp::cluster_size() == 1) {
         __syncthreads();
         return;
     }
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    wp::cluster_arrive();
+    wp::cluster_wait();
 }
-__device__ __forceinline__ int read_peer(const int *p, unsigned rank) {
-    unsigned r;
-    int v;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"((unsigned)__cvta_generic_to_shared(p)), "r"(rank));
-    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(r) : "memory");
-    return v;
-}
-
 // before[i]: the sum of x[i] over the threads in front of this one, all CTAs counted; total[i]: over all.
 template <int n>
 __device__ void scan(Shared &sh, const int (&x)[n], int (&before)[n], int (&total)[n]) {
@@ -75,13 +67,13 @@ __device__ void scan(Shared &sh, const int (&x)[n], int (&before)[n], int (&tota
         }
     }
     sync_all();
-    const unsigned ctas = cluster_size(), rank = cluster_rank();
+    const unsigned ctas = wp::cluster_size(), rank = wp::cluster_rank();
 #pragma unroll
     for (int i = 0; i < n; ++i) {
         before[i] = sh.warp_sums[i][warp] + incl[i] - x[i];
         total[i] = 0;
         for (unsigned r = 0; r < ctas; ++r) {
-            const int s = ctas == 1 ? sh.cta_sums[i] : read_peer(&sh.cta_sums[i], r);
+            const int s = ctas == 1 ? sh.cta_sums[i] : __float_as_int(wp::load_in_cluster(reinterpret_cast<const float *>(&sh.cta_sums[i]), r));
             if (r < rank) before[i] += s;
             total[i] += s;
         }
@@ -92,8 +84,8 @@ __device__ void scan(Shared &sh, const int (&x)[n], int (&before)[n], int (&tota
 struct Run { int first, end; };
 // This thread's run of n things.
 __device__ __forceinline__ Run own_run(int n) {
-    const int threads = (int)cluster_size() * kThreads, per = (n + threads - 1) / threads;
-    const long long me = (long long)cluster_rank() * kThreads + threadIdx.x;
+    const int threads = (int)wp::cluster_size() * kThreads, per = (n + threads - 1) / threads;
+    const long long me = (long long)wp::cluster_rank() * kThreads + threadIdx.x;
     return {(int)min((long long)n, me * per), (int)min((long long)n, (me + 1) * per)};
 }
 __device__ __forceinline__ int free_in(const CacheGeom &c, Run r) {
@@ -103,7 +95,7 @@ __device__ __forceinline__ int free_in(const CacheGeom &c, Run r) {
 }
 __device__ __forceinline__ bool in_cache(const CacheGeom &c, int page) { return (unsigned)page < (unsigned)c.n_pages; }
 __device__ __forceinline__ void say(const Args &a, int done, int moved, int free, int bad) {
-    if (threadIdx.x == 0 && cluster_rank() == 0) *reinterpret_cast<int4 *>(a.info) = make_int4(done, moved, free, bad);
+    if (threadIdx.x == 0 && wp::cluster_rank() == 0) *reinterpret_cast<int4 *>(a.info) = make_int4(done, moved, free, bad);
 }
 // The free pages of this thread's run, the first of them being the before-th of all, take their places among the `total` taken ones.
 __device__ __forceinline__ void take_pages(const Args &a, Run r, int before, int total) {
@@ -115,7 +107,7 @@ __device__ __forceinline__ void take_pages(const Args &a, Run r, int before, int
 }
 // Warps of all CTAs take the slots in turn.
 struct Warps { int first, step; };
-__device__ __forceinline__ Warps all_warps() { return {(int)(cluster_rank() * (kThreads / 32) + (threadIdx.x >> 5)), (int)cluster_size() * (kThreads / 32)}; }
+__device__ __forceinline__ Warps all_warps() { return {(int)(wp::cluster_rank() * (kThreads / 32) + (threadIdx.x >> 5)), (int)wp::cluster_size() * (kThreads / 32)}; }
 
 __global__ void __launch_bounds__(kThreads, 1) reserve_kernel(Args a) {
     __shared__ Shared sh;
@@ -269,7 +261,7 @@ __global__ void __launch_bounds__(kThreads, 1) compact_kernel(Args a) {
         if (!is_free && p >= n_used) a.pairs[2ll * at[0]++] = p;
         if (is_free && p < n_used) a.pairs[2ll * at[1]++ + 1] = p;
     }
-    const int threads = (int)cluster_size() * kThreads, me = (int)cluster_rank() * kThreads + threadIdx.x;
+    const int threads = (int)wp::cluster_size() * kThreads, me = (int)wp::cluster_rank() * kThreads + threadIdx.x;
     for (int i = moves + me; i < c.n_pages / 2; i += threads) *reinterpret_cast<int2 *>(a.pairs + 2ll * i) = make_int2(-1, -1);
     sync_all();
     for (int i = me; i < moves; i += threads) {

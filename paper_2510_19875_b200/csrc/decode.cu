@@ -81,8 +81,8 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(Args A, int vec) {
                 const T *const ks = (const T *)A.a.k + e, *const vs = (const T *)A.a.v + e;
                 unsigned char *const kd = sm.k[buf] + r * F::kRow + x * 16, *const vd = sm.v[buf] + r * F::kRow + x * 16;
                 if (vec) {
-                    cp_async16((unsigned)__cvta_generic_to_shared(kd), ks, page >= 0);
-                    cp_async16((unsigned)__cvta_generic_to_shared(vd), vs, page >= 0);
+                    wp::cp_async16((unsigned)__cvta_generic_to_shared(kd), ks, page >= 0 ? 16 : 0);
+                    wp::cp_async16((unsigned)__cvta_generic_to_shared(vd), vs, page >= 0 ? 16 : 0);
                 } else {
 #pragma unroll
                     for (int y = 0; y < 16 / (int)sizeof(T); ++y) {
@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(Args A, int vec) {
                     }
                 }
             }
-            cp_commit();
+            wp::cp_async_commit();
         };
         __syncthreads();  // (the segment before has been read)
         if (tid < F::kKeys) {
@@ -115,9 +115,9 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(Args A, int vec) {
             if (t + 2 < n_tiles && tid < F::kKeys) next_page = page_of(t + 2);
             if (t + 1 < n_tiles) {
                 fetch(t + 1, (t + 1) & 1);
-                cp_wait<1>();
+                wp::cp_async_wait<1>();
             } else {
-                cp_wait<0>();
+                wp::cp_async_wait<0>();
             }
             __syncthreads();
             {  // logits: a key and every kSplit-th query head a thread

@@ -1,6 +1,7 @@
 // How the keys of a paged cache are dealt to the CTAs of decode attention, for its kernels.
 #pragma once
 #include "serve_common.cuh"
+#include "warp_common.cuh"
 
 namespace stream {
 namespace decode {
@@ -157,13 +158,6 @@ __device__ __forceinline__ float warp_maximum(float x) {
     for (int d = 16; d > 0; d >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
     return x;
 }
-
-__device__ __forceinline__ void cp_async16(unsigned dst, const void *src, bool there) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int n>
-__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(n) : "memory"); }
 
 }  // namespace decode
 }  // namespace stream

@@ -7,7 +7,6 @@
 // (ref is moved only when a logit has outgrown it by 2^30: fp32 sums and bf16 weights keep their relative precision), and its own O in
 // registers; at the end the four meet in shared memory. Keys behind the slot's last one, or without a page, are zeros there.
 #include "decode.cuh"
-#include "warp_common.cuh"
 
 namespace stream {
 namespace {
@@ -97,11 +96,11 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas) decode_mma_kernel(co
                 if (!one_page) e = __shfl_sync(0xffffffffu, own, r);
                 e = (is ? e : 0) + piece_l * 8;
                 const unsigned to = dst + piece_at<D>(r, piece_l);
-                cp_async16(to, ks + e, is);
-                cp_async16(to + F::kTile, vs + e, is);
+                wp::cp_async16(to, ks + e, is ? 16 : 0);
+                wp::cp_async16(to + F::kTile, vs + e, is ? 16 : 0);
             }
         }
-        cp_commit();
+        wp::cp_async_commit();
     };
     constexpr int kQ = kMaxHeads * kPieces / kThreads;  // pieces of Q a thread
     uint4 qr[kQ];
@@ -165,7 +164,7 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas) decode_mma_kernel(co
         float ref[2] = {-CUDART_INF_F, -CUDART_INF_F}, l[2] = {0.f, 0.f};  // of rows quad and quad + 8, in units of log2
         for (int n = 0; n < n_steps; ++n) {
             fetch(n + F::kStages - 1);
-            cp_wait<F::kStages - 1>();
+            wp::cp_async_wait<F::kStages - 1>();
             __syncwarp();
             const unsigned place = (at + (unsigned)n) % F::kStages, keys = (unsigned)(keys_there >> (16 * place)) & 0xffffu;
             const unsigned kt = ring + place * 2 * F::kTile, vt = kt + F::kTile;
@@ -234,7 +233,7 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas) decode_mma_kernel(co
             open(next);
         } else {
             at += (unsigned)n_steps;
-            cp_wait<0>();
+            wp::cp_async_wait<0>();
         }
         // the place behind the first steps of the next segment is free: for O
         const unsigned o_place = (at + F::kStages - 1) % F::kStages * 2 * F::kTile;

@@ -7,6 +7,7 @@
 // the SMs, a cluster of up to eight CTAs has the tile: each walks every n-th key tile, and their m, l and O meet
 // through shared memory, in a fixed order, every CTA joining its share of the rows.
 #include "serve_common.cuh"
+#include "warp_common.cuh"
 
 namespace stream {
 namespace {
@@ -23,17 +24,6 @@ struct Smem {
     float p[kRows * (kKeys + 4)];
     float m[kRows], l[kRows];
 };
-
-__device__ __forceinline__ unsigned cluster_size() { unsigned x; asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(x)); return x; }
-__device__ __forceinline__ unsigned cluster_rank() { unsigned x; asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(x)); return x; }
-__device__ __forceinline__ void cluster_sync() { asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-__device__ __forceinline__ float read_peer(const float *p, unsigned rank) {
-    unsigned r;
-    float v;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"((unsigned)__cvta_generic_to_shared(p)), "r"(rank));
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(r) : "memory");
-    return v;
-}
 
 // Four channels of a row.
 template <class T>
@@ -57,33 +47,16 @@ __global__ void __launch_bounds__(kThreads) prompt_kernel(PromptGeom g, const T 
     Smem<D> &sm = *reinterpret_cast<Smem<D> *>(smem_raw);
     constexpr int kPad = Smem<D>::kPad, kCols = D >= 64 ? 4 : D / 16;  // channels side by side of a thread's O, in D / (16 * kCols) places
     constexpr int kParts = D / (16 * kCols);
-    const unsigned ctas = cluster_size(), rank = cluster_rank();
+    const unsigned ctas = wp::cluster_size(), rank = wp::cluster_rank();
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, lane = tid & 31;
     if (ctas == 1) after_previous_kernel();
     // which rows: kv head fastest, then the sequences' row tiles one after the other
     const int tile = (int)(blockIdx.x / ctas), kvh = tile % g.G, nth = tile / g.G;
-    int seq = -1, first = 0;  // sequence of the nth row tile, row tiles before it
-    for (int s0 = 0, sum = 0; s0 < g.n_seqs; s0 += 32) {
-        const int s = s0 + lane;
-        const int tiles = s < g.n_seqs ? (int)(((long long)span_of(g.cu_q, s, g.total_q).n * g.hpg + kRows - 1) / kRows) : 0;
-        int incl = tiles;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int y = __shfl_up_sync(0xffffffffu, incl, d);
-            if (lane >= d) incl += y;
-        }
-        const unsigned past = __ballot_sync(0xffffffffu, nth < sum + incl);
-        if (past != 0) {
-            const int at = __ffs(past) - 1;
-            seq = s0 + at;
-            first = sum + __shfl_sync(0xffffffffu, incl - tiles, at);
-            break;
-        }
-        sum += __shfl_sync(0xffffffffu, incl, 31);
-    }
-    if (seq < 0) return;  // (the whole cluster)
+    const RowTile rt = row_tile(g, nth, kRows, lane);
+    if (rt.seq < 0) return;  // (the whole cluster)
+    const int seq = rt.seq;
     const Span sq = span_of(g.cu_q, seq, g.total_q), sk = span_of(g.cu_k, seq, g.total_k);
-    const long long row_base = (long long)(nth - first) * kRows;  // (a sequence's rows may be more than 32 bits count)
+    const long long row_base = (long long)rt.nth * kRows;  // (a sequence's rows may be more than 32 bits count)
     const int n_rows = (int)min((long long)sq.n * g.hpg - row_base, (long long)kRows);
     const int shift = sk.n - sq.n;  // query i sees the keys up to i + shift
     auto keys_of = [&](int r) -> int {  // keys that row r of the tile sees
@@ -216,21 +189,22 @@ __global__ void __launch_bounds__(kThreads) prompt_kernel(PromptGeom g, const T 
             for (int part = 0; part < kParts; ++part)
 #pragma unroll
                 for (int c = 0; c < kCols; ++c) acc[(ty * 4 + i) * D + part * 64 + tx * kCols + c] = o[i][part * kCols + c];
-        cluster_sync();
+        wp::cluster_arrive();
+        wp::cluster_wait();
         for (int r = (int)rank + (int)ctas * ty; r < n_rows; r += (int)ctas * 16) {  // a row per 16 threads and step
             float mx = -CUDART_INF_F;
-            for (unsigned x = 0; x < ctas; ++x) mx = fmaxf(mx, read_peer(&sm.m[r], x));
+            for (unsigned x = 0; x < ctas; ++x) mx = fmaxf(mx, wp::load_in_cluster(&sm.m[r], x));
             const float base = mx == -CUDART_INF_F ? 0.f : mx;
             float sum = 0.f, w[kParts * kCols];
 #pragma unroll
             for (int c = 0; c < kParts * kCols; ++c) w[c] = 0.f;
             for (unsigned x = 0; x < ctas; ++x) {
-                const float f = fast_exp2(read_peer(&sm.m[r], x) - base);
-                sum = fmaf(f, read_peer(&sm.l[r], x), sum);
+                const float f = fast_exp2(wp::load_in_cluster(&sm.m[r], x) - base);
+                sum = fmaf(f, wp::load_in_cluster(&sm.l[r], x), sum);
 #pragma unroll
                 for (int part = 0; part < kParts; ++part)
 #pragma unroll
-                    for (int c = 0; c < kCols; ++c) w[part * kCols + c] = fmaf(f, read_peer(&acc[r * D + part * 64 + tx * kCols + c], x), w[part * kCols + c]);
+                    for (int c = 0; c < kCols; ++c) w[part * kCols + c] = fmaf(f, wp::load_in_cluster(&acc[r * D + part * 64 + tx * kCols + c], x), w[part * kCols + c]);
             }
             const float inv = sum > 0.f ? 1.f / sum : 0.f;
             const long long row = row_base + r, tok = sq.first + row / g.hpg;
@@ -242,7 +216,8 @@ __global__ void __launch_bounds__(kThreads) prompt_kernel(PromptGeom g, const T 
                 for (int c = 0; c < kCols; ++c) to[part * 64 + tx * kCols + c] = (T)(w[part * kCols + c] * inv);
             if (g.lse != nullptr && tx == 0) g.lse[(long long)h * g.total_q + tok] = sum > 0.f ? (mx + log2f(sum)) * kLn2 : -CUDART_INF_F;
         }
-        cluster_sync();  // (nobody leaves while its shared memory is read)
+        wp::cluster_arrive();
+        wp::cluster_wait();  // (nobody leaves while its shared memory is read)
         return;
     }
 #pragma unroll
@@ -267,8 +242,7 @@ stream_status launch(const PromptGeom &g, const void *q, const void *k, const vo
     static DeviceFlags done;
     cudaError_t e = allow_smem(prompt_kernel<T, D>, smem, done);
     if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(prompt)");
-    // no more row tiles than this, however the rows are dealt to the sequences
-    const long long tiles = ((long long)g.total_q * g.hpg / kRows + (g.n_seqs < g.total_q ? g.n_seqs : g.total_q)) * g.G;
+    const long long tiles = most_row_tiles(g, kRows);
     const int n_sm = current_sm_count();
     if (n_sm <= 0) { set_error("cannot read the SM count of the current device"); return STREAM_ERR_CUDA; }
     // several CTAs a tile where one each leaves SMs without, as long as there are keys for all

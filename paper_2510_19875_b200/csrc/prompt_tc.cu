@@ -34,7 +34,8 @@ using namespace tc;
 
 constexpr int kThreads = 384;
 constexpr int kRows = 128, kKeys = 128;  // of a tile
-constexpr int kMaxSeqs = 512;            // of a launch
+constexpr int kMaxSeqs = 256;            // of a launch
+constexpr int kMaxLevels = 2048;         // items of a kv head that are put in order
 constexpr float kOutgrown = 30.f;        // log2
 
 template <int D_>
@@ -60,9 +61,11 @@ struct Tail {
     unsigned int tmem_base;
     int abort_flag;
     int n_items;
-    int warp_sum[kThreads / 32];
+    int sorted;                                          // `order` holds the items of a kv head
+    unsigned order[kMaxLevels];                          // sequence << 12 | level, the most keys first
     Seq seq[kMaxSeqs];                                   // the longest first
     int item_end[kMaxSeqs];                              // items of the sequences up to and with this one
+    uint4 stage[8][128];                                 // of each softmax warp: 32 rows x 32 channels of the output
 };
 
 struct Params {
@@ -81,17 +84,26 @@ struct Item {
 template <class F>
 __device__ __forceinline__ Item item_at(const Params &P, const Tail<F> *tl, int id) {
     const PromptGeom &g = P.g;
-    int lo = 0, hi = g.n_seqs - 1;  // the first sequence whose items end behind id
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (tl->item_end[mid] > id) hi = mid;
-        else lo = mid + 1;
-    }
     Item it;
+    int lo = 0, level;
+    if (tl->sorted) {
+        const int nth = id / g.G;
+        lo = (int)(tl->order[nth] >> 12);
+        level = (int)(tl->order[nth] & 4095u);
+        it.kvh = id - nth * g.G;
+    } else {
+        int hi = g.n_seqs - 1;  // the first sequence whose items end behind id
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (tl->item_end[mid] > id) hi = mid;
+            else lo = mid + 1;
+        }
+        const int rem = id - (lo > 0 ? tl->item_end[lo - 1] : 0);
+        level = rem / g.G;
+        it.kvh = rem - level * g.G;
+    }
     it.s = tl->seq[lo];
-    const int first = lo > 0 ? tl->item_end[lo - 1] : 0, rem = id - first;
-    const int level = rem / g.G, pairs = (tl->item_end[lo] - first) / g.G;
-    it.kvh = rem - level * g.G;
+    const int pairs = ceil_div(it.s.q_n, 2 * P.per_tile);
     it.tok0 = (pairs - 1 - level) * 2 * P.per_tile;  // late tokens, with the most keys, first
     it.most = 0;
 #pragma unroll
@@ -191,7 +203,7 @@ __device__ void mma_role(const Params &P, Tail<F> *tl, unsigned q_smem, unsigned
     Use<F> use;
     unsigned n_q[2] = {0, 0}, n_p[2] = {0, 0};
     const unsigned q_lo = desc_lo_sw128(q_smem, 16), k_lo = desc_lo_sw128(ring, 16), v_lo = desc_lo_sw128(ring, F::kHalf);
-    auto scores = [&](int x, unsigned stage) {  // S_x = Q_x K^T
+    auto scores = [&](int x, unsigned stage, bool last) {  // S_x = Q_x K^T; last: Q_x has been read
         if (elect_one()) {
 #pragma unroll
             for (int c = 0; c < F::kHalves; ++c)
@@ -200,6 +212,7 @@ __device__ void mma_role(const Params &P, Tail<F> *tl, unsigned q_smem, unsigned
                     tc_mma_bf16_split(tmem + F::kSCol + x * 128, q_lo + ((x * F::kTile + c * F::kHalf + k4 * 32) >> 4), kHi,
                                       k_lo + stage * (F::kTile >> 4) + ((c * F::kHalf + k4 * 32) >> 4), kHi, F::kIdescQK, (c | k4) != 0);
             tc_commit(smem_u32(&tl->s_full[x]));
+            if (last) tc_commit(smem_u32(&tl->q_free[x]));
         }
         __syncwarp();
     };
@@ -225,7 +238,7 @@ __device__ void mma_role(const Params &P, Tail<F> *tl, unsigned q_smem, unsigned
             if (it.n[x] <= 0) continue;
             if (!wait_w(&tl->q_full[x], n_q[x] & 1u, tl, 1012)) return;
             tc_fence_after();
-            scores(x, use.stage());
+            scores(x, use.stage(), it.n[x] == 1);
         }
         release(use.stage());
         ++use.u;
@@ -249,7 +262,7 @@ __device__ void mma_role(const Params &P, Tail<F> *tl, unsigned q_smem, unsigned
                     if (!k_there && !wait_w(&tl->full[k.stage()], k.phase(), tl, 1017)) return;
                     k_there = true;
                     tc_fence_after();
-                    scores(x, k.stage());
+                    scores(x, k.stage(), j + 2 == it.n[x]);
                 } else {
                     if (elect_one()) tc_commit(smem_u32(&tl->o_done[x]));
                     __syncwarp();
@@ -264,10 +277,14 @@ __device__ void mma_role(const Params &P, Tail<F> *tl, unsigned q_smem, unsigned
             }
         }
     }
-    for (unsigned i = 0; i < F::kStages && use.u > 0; ++i) {  // no arrival is on its way when the CTA leaves
+    // no arrival is on its way when the CTA leaves
+    for (unsigned i = 0; i < F::kStages && use.u > 0; ++i) {
         --use.u;
         if (!wait_w(&tl->empty[use.stage()], use.phase(), tl, 1018)) return;
     }
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+        if (n_q[x] > 0 && !wait_w(&tl->q_free[x], (n_q[x] - 1) & 1u, tl, 1019)) return;
 }
 
 // Multiplies fp32 columns of this thread's TMEM lane by f (eight at a time: the logits are in registers beside them).
@@ -288,13 +305,21 @@ __device__ __forceinline__ void rescale(unsigned taddr, float f) {
 }
 
 template <class F>
-__device__ void softmax_role(const Params &P, Tail<F> *tl, unsigned char *q_ptr, unsigned tmem, int t) {
+__device__ void softmax_role(const Params &P, Tail<F> *tl, unsigned tmem, int t) {
     const PromptGeom &g = P.g;
     const int x = t >> 7, row = t & 127, lane = t & 31, wq = row >> 5;
     const int tok_r = row / g.hpg, head_r = row - tok_r * g.hpg;  // within the tile
     const unsigned lanes = tmem + ((unsigned)(row & ~31) << 16), s_addr = lanes + F::kSCol + x * 128, o_addr = lanes + F::kOCol + x * 128;
     const unsigned long long scale2 = pack_f32x2(g.scale_log2, g.scale_log2);
-    unsigned char *const stage = q_ptr + x * F::kTile + wq * 32 * F::D * 2;  // this warp's rows of the output, over the tile's Q
+    uint4 *const stage = tl->stage[t >> 5];
+    int out_tok[4];        // of the four output rows that this lane stores a piece of: the token within the tile, and where
+    long long out_at[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int rr = wq * 32 + i * 8 + (lane >> 2);
+        out_tok[i] = rr / g.hpg;
+        out_at[i] = ((long long)out_tok[i] * g.H + (rr - out_tok[i] * g.hpg)) * F::D;
+    }
     unsigned n_s = 0, n_o = 0;
     __nv_bfloat16 *const out = (__nv_bfloat16 *)g.out;
     for (int round = 0, id; (id = nth_item(round)) < tl->n_items; ++round) {
@@ -364,48 +389,47 @@ __device__ void softmax_role(const Params &P, Tail<F> *tl, unsigned char *q_ptr,
         const int head = it.kvh * g.hpg + head_r;
         if (mine && g.lse != nullptr)
             g.lse[(long long)head * g.total_q + it.s.q_first + tok] = l > 0.f ? (ref * g.scale_log2 + log2f(l)) * kLn2 : -CUDART_INF_F;
-        // 32 channels at a time to shared memory, the 16-byte pieces of a row turned so that eight rows touch every bank
+        // 32 channels at a time through shared memory, where a row's 16-byte pieces are turned so that eight rows touch every bank, and
+        // from there four lanes a row: whole sectors
         const float inv = l > 0.f ? 1.f / l : 0.f;
-        unsigned char *const own = stage + lane * 128;
+        const int n_tok = min(P.per_tile, it.s.q_n - tok0);
+        __nv_bfloat16 *const to = out + ((long long)(it.s.q_first + tok0) * g.H + it.kvh * g.hpg) * F::D + (lane & 3) * 8;
         if (n_tiles > 0) {
             if (!wait_w(&tl->o_done[x], n_o++ & 1u, tl, 1022)) return;
             tc_fence_after();
+        }
 #pragma unroll 1
-            for (int c = 0; c < F::D / 32; ++c) {
-                unsigned r[32];
+        for (int c = 0; c < F::D / 32; ++c) {
+            unsigned r[32];
+            if (n_tiles > 0) {
                 tmem_ld_32x32_issue(o_addr + c * 32, r);
                 tmem_ld_wait();
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    unsigned w[4];
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-                        const __nv_bfloat162 pk = __floats2bfloat162_rn(__uint_as_float(r[8 * u + 2 * y]) * inv, __uint_as_float(r[8 * u + 2 * y + 1]) * inv);
-                        w[y] = *reinterpret_cast<const unsigned *>(&pk);
-                    }
-                    *reinterpret_cast<uint4 *>(own + (c >> 1) * 32 * 128 + (((((c & 1) << 2) + u) ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                if (c == F::D / 32 - 1) {
+                    tc_fence_before();
+                    mbar_arrive_if(smem_u32(&tl->o_free[x]), lane == 0);
                 }
+            } else {  // (no key for any row)
+#pragma unroll
+                for (int i = 0; i < 32; ++i) r[i] = 0u;
             }
-            tc_fence_before();
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                unsigned w[4];
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    const __nv_bfloat162 pk = __floats2bfloat162_rn(__uint_as_float(r[8 * u + 2 * y]) * inv, __uint_as_float(r[8 * u + 2 * y + 1]) * inv);
+                    w[y] = *reinterpret_cast<const unsigned *>(&pk);
+                }
+                stage[lane * 4 + (u ^ ((lane >> 1) & 3))] = make_uint4(w[0], w[1], w[2], w[3]);
+            }
             __syncwarp();
-            mbar_arrive_if(smem_u32(&tl->o_free[x]), lane == 0);
-        }
-        // and from there in whole rows: a row's D channels by D / 8 lanes
-        constexpr int kLanes = F::D / 8, kAtOnce = 32 / kLanes;
-        const int piece = lane % kLanes;
-#pragma unroll 4
-        for (int r0 = 0; r0 < 32; r0 += kAtOnce) {
-            const int r = r0 + lane / kLanes, rr = wq * 32 + r, tr = rr / g.hpg, hr = rr - tr * g.hpg;
-            uint4 w = make_uint4(0, 0, 0, 0);  // (no key for any row)
-            if (n_tiles > 0) w = *reinterpret_cast<const uint4 *>(stage + ((piece >> 3) * 32 + r) * 128 + (((piece & 7) ^ (r & 7)) << 4));
-            if (tr < P.per_tile && tok0 + tr < it.s.q_n)
-                *reinterpret_cast<uint4 *>(out + ((long long)(it.s.q_first + tok0 + tr) * g.H + it.kvh * g.hpg + hr) * F::D + piece * 8) = w;
-        }
-        __syncwarp();
-        if (n_tiles > 0) {
-            fence_async_smem();  // (the next Q is written by the copy engine)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int rr = i * 8 + (lane >> 2);
+                const uint4 w = stage[rr * 4 + ((lane & 3) ^ ((rr >> 1) & 3))];
+                if (out_tok[i] < n_tok) *reinterpret_cast<uint4 *>(to + out_at[i] + c * 32) = w;
+            }
             __syncwarp();
-            mbar_arrive_if(smem_u32(&tl->q_free[x]), lane == 0);
         }
     }
 }
@@ -424,7 +448,7 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
         for (int i = 0; i < F::kStages; ++i) { mbar_init(smem_u32(&tl->full[i]), 1); mbar_init(smem_u32(&tl->empty[i]), 1); mbar_init(smem_u32(&tl->v_raw[i]), 1); }
         for (int x = 0; x < 2; ++x) {
             mbar_init(smem_u32(&tl->q_full[x]), 1);
-            mbar_init(smem_u32(&tl->q_free[x]), 4);
+            mbar_init(smem_u32(&tl->q_free[x]), 1);
             mbar_init(smem_u32(&tl->s_full[x]), 1);
             mbar_init(smem_u32(&tl->p_half[x][0]), 4);
             mbar_init(smem_u32(&tl->p_half[x][1]), 4);
@@ -482,12 +506,47 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
     __syncthreads();
     tc_fence_after();
     const unsigned tmem = tl->tmem_base;
+    // Items in the order of their key tiles, over all sequences (in the sequences' order the last CTA was 9 % behind the mean: 12 prompts of up to 4500
+    // tokens; in this one 2 %). An item's place is how many stand in front of it, which each sequence says in closed form. Not where every
+    // item has a CTA of its own, nor where there is too much to count (16 terms a thread take 2 us): the items are many and
+    // small against a CTA's sum then.
+    const int n_levels = tl->n_items / g.G;
+    const bool sorted = g.n_seqs > 1 && tl->n_items > (int)gridDim.x && n_levels <= kMaxLevels && n_levels * g.n_seqs <= 16 * kThreads;
+    if (tid == 0) tl->sorted = sorted ? 1 : 0;
+    for (int i = tid; sorted && i < n_levels; i += kThreads) {
+        int own = 0, hi = g.n_seqs - 1;
+        while (own < hi) {
+            const int mid = (own + hi) >> 1;
+            if (tl->item_end[mid] > i * g.G) hi = mid;
+            else own = mid + 1;
+        }
+        const int level = i - (own > 0 ? tl->item_end[own - 1] / g.G : 0), span2 = 2 * P.per_tile;
+        // key tiles of a sequence's item at `level`; its items with more than v of them
+        auto tiles = [&](const Seq &q, int lv) {
+            const int end = min((ceil_div(q.q_n, span2) - lv) * span2, q.q_n);
+            return ceil_div(g.causal ? max(0, end + q.k_n - q.q_n) : q.k_n, kKeys);
+        };
+        auto above = [&](const Seq &q, int v) {
+            const int n = ceil_div(q.q_n, span2);
+            if (v < 0) return n;
+            if ((long long)q.k_n <= (long long)v * kKeys) return 0;
+            if (!g.causal) return n;
+            const long long need = (long long)v * kKeys - q.k_n + q.q_n;  // queries up to there see no more
+            return need < span2 ? n : n - (int)(need / span2);
+        };
+        const int v = tiles(tl->seq[own], level);
+        int place = level;
+        for (int o = 0; o < g.n_seqs; ++o)
+            if (o != own) place += above(tl->seq[o], o < own ? v - 1 : v);
+        tl->order[place] = (unsigned)own << 12 | (unsigned)level;
+    }
+    __syncthreads();
     if (warp < 4) {
         if (warp == 0) load_role<F>(P, &tmap_q, &tmap_k, &tmap_v, tl, smem_u32(smem), smem_u32(ring));
         else if (warp == 1) mma_role<F>(P, tl, smem_u32(smem), smem_u32(ring), tmem);
         else if (warp == 2) zero_role<F>(P, tl, ring, lane);
     } else {
-        softmax_role<F>(P, tl, smem, tmem, tid - 128);
+        softmax_role<F>(P, tl, tmem, tid - 128);
     }
     __syncwarp();
     leave(&tl->abort_flag, tmem, warp == 1);

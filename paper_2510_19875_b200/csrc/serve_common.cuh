@@ -39,6 +39,33 @@ __device__ __forceinline__ Span span_of(const int32_t *cu, int s, int total) {
 __device__ __forceinline__ int tokens_of(const CacheGeom &c, int s) { return min(max(c.len[s], 0), c.max_pages * c.page); }
 __host__ __device__ __forceinline__ int ceil_div(int a, int b) { return (int)(((long long)a + b - 1) / b); }
 
+// The kernels that give every tile of `rows` rows of a kv head's queries a CTA: which sequence the nth one lies in, and its number
+// there. By a whole warp. seq < 0: there are fewer.
+struct RowTile { int seq, nth; };
+__device__ __forceinline__ RowTile row_tile(const PromptGeom &g, int nth, int rows, int lane) {
+    for (int s0 = 0, sum = 0; s0 < g.n_seqs; s0 += 32) {
+        const int s = s0 + lane;
+        const int tiles = s < g.n_seqs ? (int)(((long long)span_of(g.cu_q, s, g.total_q).n * g.hpg + rows - 1) / rows) : 0;
+        int incl = tiles;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, incl, d);
+            if (lane >= d) incl += y;
+        }
+        const unsigned past = __ballot_sync(0xffffffffu, nth < sum + incl);
+        if (past != 0) {
+            const int at = __ffs(past) - 1;
+            return {s0 + at, nth - sum - __shfl_sync(0xffffffffu, incl - tiles, at)};
+        }
+        sum += __shfl_sync(0xffffffffu, incl, 31);
+    }
+    return {-1, 0};
+}
+// No more tiles than this, of all kv heads, however the rows are dealt to the sequences.
+inline long long most_row_tiles(const PromptGeom &g, int rows) {
+    return ((long long)g.total_q * g.hpg / rows + (g.n_seqs < g.total_q ? g.n_seqs : g.total_q)) * g.G;
+}
+
 // A programmatic dependent (see after_previous_kernel), and clusters of CTAs.
 template <class... K, class... A>
 cudaError_t launch_early(void (*kern)(K...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st, A &&...args) {
@@ -84,6 +111,8 @@ cudaError_t allow_smem(void (*kern)(K...), int bytes, DeviceFlags &done) {
 
 bool prompt_tc_supported(const PromptGeom &g, int dtype, const void *q, const void *k, const void *v);
 stream_status launch_prompt_tc(const PromptGeom &g, const void *q, const void *k, const void *v, cudaStream_t st);
+bool prompt_mma_supported(const PromptGeom &g, int dtype, const void *q, const void *k, const void *v);
+stream_status launch_prompt_mma(const PromptGeom &g, const void *q, const void *k, const void *v, cudaStream_t st);
 stream_status launch_prompt_generic(const PromptGeom &g, int dtype, const void *q, const void *k, const void *v, cudaStream_t st);
 
 struct DecodeCall {
