@@ -331,7 +331,7 @@ stream_status launch_decode(const DecodeCall &a, int dtype, void *workspace, cud
     A.grid = (int)(most < want ? most : want);
     const long long any = (long long)(uintptr_t)a.k | (long long)(uintptr_t)a.v | a.c.s_p * e | a.c.s_t * e | a.c.s_h * e;
     const int vec = any % 16 == 0 ? 1 : 0;
-    cudaError_t rc = mma_supported(a, dtype) ? launch_mma(A, n_sm, st)
+    cudaError_t rc = warp_supported(a, dtype) ? launch_warp(A, dtype, n_sm, st)
                      : dtype == STREAM_F32   ? launch_fma_d<float>(A, vec, st)
                                              : launch_fma_d<__nv_bfloat16>(A, vec, st);
     if (rc != cudaSuccess) return cuda_fail(rc, "decode attention launch");

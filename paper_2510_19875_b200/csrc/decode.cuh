@@ -29,12 +29,12 @@ struct Args {
     float *parts;                // [grid][2][kMaxHeads * (d + 2)]: m, l, O
     struct Left *left;           // [grid]
     WorkspaceHeader *header;
-    int q_vec;                   // (mma.sync) q is read in pieces of 16 bytes
+    int q_vec;                   // (decode_warp.cu) q is read in pieces of 16 bytes
 };
 
-// bf16 on mma.sync. May lower A.grid.
-bool mma_supported(const DecodeCall &a, int dtype);
-cudaError_t launch_mma(Args &A, int n_sm, cudaStream_t st);
+// Rows of 16-byte pieces, up to 512 bytes. May lower A.grid.
+bool warp_supported(const DecodeCall &a, int dtype);
+cudaError_t launch_warp(Args &A, int dtype, int n_sm, cudaStream_t st);
 
 // A segment costs a CTA kOpen units beside its own: the way from one owner's last key to the next one's first, the warps' meeting and
 // the output. So an owner takes up as many places more in the row that is dealt out, in front of its units. (Without them a CTA with
