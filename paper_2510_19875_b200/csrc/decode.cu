@@ -226,22 +226,26 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(Args A, int vec) {
 
 // ----------------------------------------------------------------------------------------------
 // The pieces of an owner joined, a query head a CTA: column c of the grid has what CTA c of the first kernel left. One more column
-// writes the header. Its time is that of loads that wait for one another (what is left; m, l and the first of O), and of its launch.
+// writes the header. A thread has four channels of every n-th piece, so that the pieces of a long slot (up to all CTAs' of the first
+// kernel: one slot, one head, 32954 keys, 258 pieces) are read 16 to 64 side by side. Its time is that of loads that wait for
+// one another (what is left; m, l and the first of O), and of its launch.
 // ----------------------------------------------------------------------------------------------
+constexpr int kJoinThreads = 256;
 template <class T>
-__global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ Args A) {
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ Args A) {
     const int tid = threadIdx.x, lane = tid & 31, h = blockIdx.y, d = A.a.c.d;
     __shared__ unsigned any;
     __shared__ float f[kMaxGrid];
-    __shared__ float wm[kThreads / 32], wl[kThreads / 32];
+    __shared__ float wm[kJoinThreads / 32], wl[kJoinThreads / 32];
+    __shared__ float4 sums[kJoinThreads];
     if (tid == 0) any = 0;
     after_previous_kernel();
     if ((int)blockIdx.x == A.grid) {
         if (h != 0) return;
         __syncthreads();
-        for (int i = tid; i < A.grid; i += kThreads)
+        for (int i = tid; i < A.grid; i += kJoinThreads)
             if (A.left[i].bad != 0) atomicMax(&any, A.left[i].bad);
-        for (int i = tid; i < (int)sizeof(WorkspaceHeader) / 4; i += kThreads) reinterpret_cast<unsigned *>(A.header)[i] = 0;
+        for (int i = tid; i < (int)sizeof(WorkspaceHeader) / 4; i += kJoinThreads) reinterpret_cast<unsigned *>(A.header)[i] = 0;
         __syncthreads();
         if (tid == 0) {
             A.header->rows = (unsigned long long)A.a.c.n_slots * A.a.H;
@@ -251,40 +255,61 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ 
     }
     const Left left = A.left[blockIdx.x];
     if (h >= left.heads || left.n == 0) return;
-    const int n = left.n;
+    const int n = left.n, quads = d / 4, groups = kJoinThreads / quads, group = tid / quads, at = (tid - group * quads) * 4;
     auto piece = [&](int x) { return part_of(A, (int)blockIdx.x + x, x == 0 ? left.which : 0); };
-    constexpr int kFirst = 8;
-    float first[kFirst], ls = 0.f, m = -CUDART_INF_F;  // O of the first pieces (this thread's channel); l of piece tid
+    auto o_of = [&](int x) { return *reinterpret_cast<const float4 *>(piece(x) + 2 * kMaxHeads + h * d + at); };
+    constexpr int kFirst = 4;
+    float4 first[kFirst];  // of O, before its weights are known
+    float ls[2] = {0.f, 0.f}, m = -CUDART_INF_F;
+    static_assert(kMaxGrid <= 2 * kJoinThreads, "two pieces' m and l a thread");
 #pragma unroll
-    for (int x = 0; x < kFirst; ++x) first[x] = x < n && tid < d ? piece(x)[2 * kMaxHeads + h * d + tid] : 0.f;
-    for (int x = tid; x < n; x += kThreads) m = fmaxf(m, f[x] = piece(x)[h]);
-    if (tid < n) ls = piece(tid)[kMaxHeads + h];
+    for (int i = 0; i < kFirst; ++i) first[i] = group + i * groups < n ? o_of(group + i * groups) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int x = tid + i * kJoinThreads;
+        if (x < n) {
+            m = fmaxf(m, f[x] = piece(x)[h]);
+            ls[i] = piece(x)[kMaxHeads + h];
+        }
+    }
     m = warp_maximum(m);
     if (lane == 0) wm[tid >> 5] = m;
     __syncthreads();
-    m = fmaxf(fmaxf(wm[0], wm[1]), fmaxf(wm[2], wm[3]));
+    m = wm[0];
+#pragma unroll
+    for (int i = 1; i < kJoinThreads / 32; ++i) m = fmaxf(m, wm[i]);
     const float base = m == -CUDART_INF_F ? 0.f : m;
     float l = 0.f;
-    for (int x = tid; x < n; x += kThreads) {
-        f[x] = fast_exp2(f[x] - base);
-        l = fmaf(f[x], x < kThreads ? ls : piece(x)[kMaxHeads + h], l);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int x = tid + i * kJoinThreads;
+        if (x < n) {
+            f[x] = fast_exp2(f[x] - base);
+            l = fmaf(f[x], ls[i], l);
+        }
     }
 #pragma unroll
     for (int x = 16; x > 0; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
     if (lane == 0) wl[tid >> 5] = l;
     __syncthreads();
-    l = (wl[0] + wl[1]) + (wl[2] + wl[3]);
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](float w, const float4 &y) { o.x = fmaf(w, y.x, o.x); o.y = fmaf(w, y.y, o.y); o.z = fmaf(w, y.z, o.z); o.w = fmaf(w, y.w, o.w); };
+#pragma unroll
+    for (int i = 0; i < kFirst; ++i)
+        if (group + i * groups < n) add(f[group + i * groups], first[i]);
+#pragma unroll 4
+    for (int x = group + kFirst * groups; x < n; x += groups) add(f[x], o_of(x));
+    sums[tid] = o;
+    __syncthreads();
+    if (group > 0) return;
+    l = 0.f;
+#pragma unroll
+    for (int i = 0; i < kJoinThreads / 32; ++i) l += wl[i];
+    for (int i = 1; i < groups && i < n; ++i) add(1.f, sums[i * quads + tid]);
     const float inv = l > 0.f ? 1.f / l : 0.f;
     const long long to = left.to + h;
-    for (int i = tid; i < d; i += kThreads) {
-        float o = 0.f;
-#pragma unroll
-        for (int x = 0; x < kFirst; ++x)
-            if (x < n) o = fmaf(f[x], i == tid ? first[x] : piece(x)[2 * kMaxHeads + h * d + i], o);
-#pragma unroll 8
-        for (int x = kFirst; x < n; ++x) o = fmaf(f[x], piece(x)[2 * kMaxHeads + h * d + i], o);
-        ((T *)A.a.out)[to * d + i] = (T)(o * inv);
-    }
+    T *const out = (T *)A.a.out + to * d + at;
+    out[0] = (T)(o.x * inv); out[1] = (T)(o.y * inv); out[2] = (T)(o.z * inv); out[3] = (T)(o.w * inv);
     if (A.a.lse != nullptr && tid == 0) A.a.lse[to] = l > 0.f ? (m + log2f(l)) * kLn2 : -CUDART_INF_F;
 }
 
@@ -336,7 +361,7 @@ stream_status launch_decode(const DecodeCall &a, int dtype, void *workspace, cud
                                              : launch_fma_d<__nv_bfloat16>(A, vec, st);
     if (rc != cudaSuccess) return cuda_fail(rc, "decode attention launch");
     const dim3 joins(A.grid + 1, a.hpg < kMaxHeads ? a.hpg : kMaxHeads);
-    rc = dtype == STREAM_F32 ? launch_early(join_kernel<float>, joins, kThreads, 0, st, A) : launch_early(join_kernel<__nv_bfloat16>, joins, kThreads, 0, st, A);
+    rc = dtype == STREAM_F32 ? launch_early(join_kernel<float>, joins, kJoinThreads, 0, st, A) : launch_early(join_kernel<__nv_bfloat16>, joins, kJoinThreads, 0, st, A);
     return rc == cudaSuccess ? STREAM_OK : cuda_fail(rc, "decode join launch");
 }
 
