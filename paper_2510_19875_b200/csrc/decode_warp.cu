@@ -265,7 +265,7 @@ __global__ void __launch_bounds__(kThreads, Form<T, D>::kCtas) decode_warp_kerne
     extern __shared__ __align__(128) unsigned char smem_raw[];
     Smem<T, D> &sm = *reinterpret_cast<Smem<T, D> *>(smem_raw);
     const CacheGeom &c = A.a.c;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, quad = lane >> 2;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     after_previous_kernel();
     T *const out = (T *)A.a.out;
     write_empty_slots<T>(A);
@@ -275,8 +275,6 @@ __global__ void __launch_bounds__(kThreads, Form<T, D>::kCtas) decode_warp_kerne
     const bool one_page = c.page % kStep == 0;  // a tile's keys lie side by side
     constexpr int kPieces = F::kPieces, kRowsAtOnce = 32 / kPieces;  // rows that 32 lanes fetch at once
     const int row_l = lane / kPieces, piece_l = lane % kPieces;
-    // ldmatrix rows of this lane
-    const int k_row = (lane >> 4) * 8 + (lane & 7), k_half = (lane >> 3) & 1, v_row = ((lane >> 3) & 1) * 8 + (lane & 7), v_half = lane >> 4;
     unsigned bad = 0;
     // What this warp fetches: its steps of the segment that is open, step n in the ring's place (at + n) % kStages
     const int32_t *table = nullptr;

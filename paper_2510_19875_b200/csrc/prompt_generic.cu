@@ -18,9 +18,10 @@ constexpr int kRows = 64, kKeys = 64;
 template <int D>
 struct Smem {
     static constexpr int kPad = D + 4;        // (16-byte reads of eight rows side by side touch every bank once)
+    static constexpr int kBufs = D <= 128 ? 2 : 1;  // key tiles in shared memory
     float q[kRows * kPad];
-    float k[kKeys * kPad];
-    float v[kKeys * D];
+    float k[kBufs][kKeys * kPad];
+    float v[kBufs][kKeys * D];
     float p[kRows * (kKeys + 4)];
     float m[kRows], l[kRows];
 };
@@ -56,7 +57,7 @@ __global__ void __launch_bounds__(kThreads) prompt_kernel(PromptGeom g, const T 
     if (rt.seq < 0) return;  // (the whole cluster)
     const int seq = rt.seq;
     const Span sq = span_of(g.cu_q, seq, g.total_q), sk = span_of(g.cu_k, seq, g.total_k);
-    const long long row_base = (long long)rt.nth * kRows;  // (a sequence's rows may be more than 32 bits count)
+    const long long row_base = ((long long)sq.n * g.hpg - 1) / kRows * kRows - (long long)rt.nth * kRows;  // late tokens, with the most keys, first  // (a sequence's rows may be more than 32 bits count)
     const int n_rows = (int)min((long long)sq.n * g.hpg - row_base, (long long)kRows);
     const int shift = sk.n - sq.n;  // query i sees the keys up to i + shift
     auto keys_of = [&](int r) -> int {  // keys that row r of the tile sees
@@ -88,18 +89,38 @@ __global__ void __launch_bounds__(kThreads) prompt_kernel(PromptGeom g, const T 
 #pragma unroll
         for (int c = 0; c < kParts * kCols; ++c) o[i][c] = 0.f;
     }
-    for (long long j0 = (long long)rank * kKeys; j0 < most; j0 += (long long)ctas * kKeys) {
-        __syncthreads();
-        for (int i = tid; i < kKeys * (D / 4); i += kThreads) {
-            const int r = i / (D / 4), c = (i % (D / 4)) * 4;
-            const long long key = j0 + r;
-            float4 x = make_float4(0.f, 0.f, 0.f, 0.f), y = x;
-            if (key < sk.n) {
-                x = load4(ks + key * g.ks_t + c, vec);
-                y = load4(vs + key * g.ks_t + c, vec);
+    constexpr int kBufs = Smem<D>::kBufs;
+    const long long step = (long long)ctas * kKeys;
+    auto fetch = [&](long long j0, int buf) {
+        if (j0 < most) {
+            for (int i = tid; i < kKeys * (D / 4); i += kThreads) {
+                const int r = i / (D / 4), c = (i % (D / 4)) * 4;
+                const long long key = j0 + r;
+                const bool there = key < sk.n;
+                const T *const kp = ks + (there ? key * g.ks_t : 0) + c, *const vp = vs + (there ? key * g.ks_t : 0) + c;
+                float *const kd = &sm.k[buf][r * kPad + c], *const vd = &sm.v[buf][r * D + c];
+                if (sizeof(T) == 4 && vec) {
+                    wp::cp_async16(wp::smem_addr(kd), kp, there ? 16 : 0);
+                    wp::cp_async16(wp::smem_addr(vd), vp, there ? 16 : 0);
+                } else {
+                    *reinterpret_cast<float4 *>(kd) = there ? load4(kp, vec) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    *reinterpret_cast<float4 *>(vd) = there ? load4(vp, vec) : make_float4(0.f, 0.f, 0.f, 0.f);
+                }
             }
-            *reinterpret_cast<float4 *>(&sm.k[r * kPad + c]) = x;
-            *reinterpret_cast<float4 *>(&sm.v[r * D + c]) = y;
+        }
+        wp::cp_async_commit();
+    };
+    const long long j_first = (long long)rank * kKeys;
+    if (kBufs == 2) fetch(j_first, 0);
+    int buf = 0;
+    for (long long j0 = j_first; j0 < most; j0 += step, buf ^= kBufs - 1) {
+        if (kBufs == 2) {
+            fetch(j0 + step, buf ^ 1);
+            wp::cp_async_wait<1>();
+        } else {
+            __syncthreads();
+            fetch(j0, 0);
+            wp::cp_async_wait<0>();
         }
         __syncthreads();
         float s[4][4];  // rows ty * 4 + i, keys tx + 16 * j
@@ -113,7 +134,7 @@ __global__ void __launch_bounds__(kThreads) prompt_kernel(PromptGeom g, const T 
 #pragma unroll
             for (int i = 0; i < 4; ++i) a[i] = *reinterpret_cast<const float4 *>(&sm.q[(ty * 4 + i) * kPad + c]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) b[j] = *reinterpret_cast<const float4 *>(&sm.k[(tx + 16 * j) * kPad + c]);
+            for (int j = 0; j < 4; ++j) b[j] = *reinterpret_cast<const float4 *>(&sm.k[buf][(tx + 16 * j) * kPad + c]);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -153,7 +174,7 @@ __global__ void __launch_bounds__(kThreads) prompt_kernel(PromptGeom g, const T 
                 float w[kParts * kCols];
 #pragma unroll
                 for (int part = 0; part < kParts; ++part) {
-                    const float *at = &sm.v[(j + x) * D + part * 64 + tx * kCols];
+                    const float *at = &sm.v[buf][(j + x) * D + part * 64 + tx * kCols];
                     if constexpr (kCols == 4) {
                         const float4 y = *reinterpret_cast<const float4 *>(at);
                         w[part * 4] = y.x; w[part * 4 + 1] = y.y; w[part * 4 + 2] = y.z; w[part * 4 + 3] = y.w;
@@ -170,7 +191,9 @@ __global__ void __launch_bounds__(kThreads) prompt_kernel(PromptGeom g, const T 
                 }
             }
         }
+        if (kBufs == 2) __syncthreads();  // (the buffer of the tile after next)
     }
+    wp::cp_async_wait<0>();
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -178,7 +201,7 @@ __global__ void __launch_bounds__(kThreads) prompt_kernel(PromptGeom g, const T 
     if (ctas > 1) {
         // every CTA leaves its m, l and O (over its key tiles, no longer needed); the rows are then dealt out to the CTAs
         __syncthreads();
-        float *const acc = sm.k;  // [kRows][D]
+        float *const acc = sm.k[0];  // [kRows][D]
         if (tx == 0) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) { sm.m[ty * 4 + i] = m[i]; sm.l[ty * 4 + i] = l[i]; }
