@@ -410,7 +410,8 @@ typedef struct {
  *   cu_q, cu_k  device int32 [n_seqs + 1], ascending; an entry outside 0 .. total_q (total_k) counts as the nearest
  *               inside, and a sequence whose end lies before its beginning is empty
  *   scale       logit scale; <= 0 selects 1/sqrt(d)
- *   out         device, dtype of the problem, contiguous [total_q, n_q_heads, d]; rows of no sequence stay as they are
+ *   out         device, dtype of the problem, contiguous [total_q, n_q_heads, d]; rows of no sequence stay as they are. Must
+ *               not overlap an input
  *   lse_out     device float32 [n_q_heads, total_q] or NULL; likewise
  * Softmax statistics and the output accumulate in fp32.
  */
@@ -498,11 +499,13 @@ stream_status stream_cache_copy_pages(const stream_cache *c, void *k_pages, void
  * position or page cannot be, are passed over.
  *   k, v     device, [total, n_kv_heads, d] with the strides given (elements, innermost 1); read only
  *   cu_new   device int32 [n_slots + 1], ascending, clamped like cu_q
+ *   done     device int32, or NULL: nothing is written where it is 0. The first word of reserve's info_out: a reserve that was
+ *            refused has left the lengths as they were, and the last tokens that there are would be overwritten
  *   k_pages, v_pages  the caches' first elements (layer 0); written: layer `layer`
  */
 stream_status stream_cache_write(const stream_cache *c, int32_t layer, const void *k, const void *v, int64_t total,
                                  int64_t stride_t, int64_t stride_h, const int32_t *cu_new, const int32_t *page_table,
-                                 const int32_t *seq_len, void *k_pages, void *v_pages, void *cuda_stream);
+                                 const int32_t *seq_len, const int32_t *done, void *k_pages, void *v_pages, void *cuda_stream);
 
 /*
  * Attention of one new token of every slot over its cached tokens (its own among them, if it has been written):
@@ -516,7 +519,7 @@ stream_status stream_cache_write(const stream_cache *c, int32_t layer, const voi
  *   n_q_heads   a multiple of n_kv_heads
  *   q           device [n_slots, n_q_heads, d] with the strides given (elements, innermost 1); read only
  *   scale       logit scale; <= 0 selects 1/sqrt(d)
- *   out         device, dtype of the cache, contiguous [n_slots, n_q_heads, d]; overwritten
+ *   out         device, dtype of the cache, contiguous [n_slots, n_q_heads, d]; overwritten. Must not overlap an input
  *   lse_out     device float32 [n_slots, n_q_heads] or NULL
  *   workspace   device, 256-byte aligned, >= stream_decode_workspace_bytes(c, n_q_heads); overwritten, nothing is kept
  *               in it but the record. Calls that can overlap on the GPU need one each.

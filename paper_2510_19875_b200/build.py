@@ -16,7 +16,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libstream.so")
 SOURCES = ["api.cu", "mask_generic.cu", "attn_generic.cu", "attn_mma.cu", "attn_tok.cu", "mask_tc.cu", "attn_tc.cu", "mask_tok.cu",
-           "static_scratch.cu", "vertical.cu", "mask_diff.cu", "selftest.cu", "api_serve.cu", "prompt_tc.cu", "prompt_generic.cu", "prompt_mma.cu",
+           "static_scratch.cu", "vertical.cu", "mask_diff.cu", "selftest.cu", "api_serve.cu", "prompt_tc.cu", "prompt_generic.cu", "prompt_mma.cu", "prompt_f32.cu",
            "decode.cu", "decode_warp.cu", "cache_ledger.cu", "cache_copy.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

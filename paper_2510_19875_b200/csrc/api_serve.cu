@@ -111,6 +111,7 @@ stream_status stream_prompt_attention(const stream_prompt *p, const void *q, con
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (prompt_tc_supported(g, p->dtype, q, k, v)) return launch_prompt_tc(g, q, k, v, st);
     if (prompt_mma_supported(g, p->dtype, q, k, v)) return launch_prompt_mma(g, q, k, v, st);
+    if (prompt_f32_supported(g, p->dtype, q, k, v)) return launch_prompt_f32(g, q, k, v, st);
     return launch_prompt_generic(g, p->dtype, q, k, v, st);
 }
 
@@ -173,7 +174,7 @@ stream_status stream_cache_copy_pages(const stream_cache *c, void *k_pages, void
 
 stream_status stream_cache_write(const stream_cache *c, int32_t layer, const void *k, const void *v, int64_t total,
                                  int64_t stride_t, int64_t stride_h, const int32_t *cu_new, const int32_t *page_table,
-                                 const int32_t *seq_len, void *k_pages, void *v_pages, void *cuda_stream) {
+                                 const int32_t *seq_len, const int32_t *done, void *k_pages, void *v_pages, void *cuda_stream) {
     CacheGeom g;
     stream_status rc = make_cache(c, &g);
     if (rc != STREAM_OK) return rc;
@@ -184,12 +185,12 @@ stream_status stream_cache_write(const stream_cache *c, int32_t layer, const voi
     if (total == 0) return STREAM_OK;
     if (k == nullptr || v == nullptr || k_pages == nullptr || v_pages == nullptr) return invalid("k, v, k_pages and v_pages must not be NULL");
     const int e = elem_bytes(c->dtype);
-    if (!natural(k, e) || !natural(v, e) || !natural(k_pages, e) || !natural(v_pages, e) || !natural(cu_new, 4) || !natural(page_table, 4) || !natural(seq_len, 4))
+    if (!natural(k, e) || !natural(v, e) || !natural(k_pages, e) || !natural(v_pages, e) || !natural(cu_new, 4) || !natural(page_table, 4) || !natural(seq_len, 4) || !natural(done, 4))
         return invalid("a pointer is not aligned to its elements");
     g.table = const_cast<int32_t *>(page_table);
     g.len = const_cast<int32_t *>(seq_len);
     const long long at = (long long)layer * g.s_l * e;
-    return launch_write(g, e, k, v, (int)total, total > 1 ? stride_t : (long long)g.G * g.d, g.G > 1 ? stride_h : g.d, cu_new,
+    return launch_write(g, e, k, v, (int)total, total > 1 ? stride_t : (long long)g.G * g.d, g.G > 1 ? stride_h : g.d, cu_new, done,
                         (char *)k_pages + at, (char *)v_pages + at, (cudaStream_t)cuda_stream);
 }
 

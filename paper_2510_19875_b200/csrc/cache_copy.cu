@@ -65,16 +65,17 @@ struct WriteArgs {
     CacheGeom c;
     const char *k, *v;
     char *k_pages, *v_pages;
-    const int32_t *cu;
+    const int32_t *cu, *done;
     int total, elem;
     long long s_t, s_h;          // bytes, of k and v
     int run, per_token;          // units of a head's row (of all heads where they lie side by side on both sides); of a token
 };
 
 template <class Unit>
-__global__ void __launch_bounds__(kThreads) write_kernel(WriteArgs a) {
+__global__ void __launch_bounds__(kThreads) write_kernel(const __grid_constant__ WriteArgs a) {
     after_previous_kernel();
     const CacheGeom &c = a.c;
+    if (a.done != nullptr && *a.done == 0) return;
     const int lane = threadIdx.x & 31;
     for (long long t = (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); t < a.total; t += (long long)gridDim.x * (kThreads / 32)) {
         // the slot whose rows hold t: the last one that begins at or before it (32 candidates a step)
@@ -145,10 +146,10 @@ stream_status launch_copy_pages(const CacheGeom &c, int elem, void *k, void *v, 
 }
 
 stream_status launch_write(const CacheGeom &c, int elem, const void *k, const void *v, int total, long long s_t, long long s_h,
-                           const int32_t *cu_new, void *k_pages, void *v_pages, cudaStream_t st) {
+                           const int32_t *cu_new, const int32_t *done, void *k_pages, void *v_pages, cudaStream_t st) {
     WriteArgs a = {};
     a.c = c; a.k = (const char *)k; a.v = (const char *)v; a.k_pages = (char *)k_pages; a.v_pages = (char *)v_pages;
-    a.cu = cu_new; a.total = total; a.elem = elem; a.s_t = s_t * elem; a.s_h = s_h * elem;
+    a.cu = cu_new; a.done = done; a.total = total; a.elem = elem; a.s_t = s_t * elem; a.s_h = s_h * elem;
     const long long row = (long long)c.d * elem, all = row * c.G;
     const bool side_by_side = c.G == 1 || (s_h == c.d && c.s_h == c.d);
     const int unit = unit_of({(long long)(uintptr_t)k, (long long)(uintptr_t)v, (long long)(uintptr_t)k_pages, (long long)(uintptr_t)v_pages,

@@ -113,6 +113,8 @@ bool prompt_tc_supported(const PromptGeom &g, int dtype, const void *q, const vo
 stream_status launch_prompt_tc(const PromptGeom &g, const void *q, const void *k, const void *v, cudaStream_t st);
 bool prompt_mma_supported(const PromptGeom &g, int dtype, const void *q, const void *k, const void *v);
 stream_status launch_prompt_mma(const PromptGeom &g, const void *q, const void *k, const void *v, cudaStream_t st);
+bool prompt_f32_supported(const PromptGeom &g, int dtype, const void *q, const void *k, const void *v);
+stream_status launch_prompt_f32(const PromptGeom &g, const void *q, const void *k, const void *v, cudaStream_t st);
 stream_status launch_prompt_generic(const PromptGeom &g, int dtype, const void *q, const void *k, const void *v, cudaStream_t st);
 
 struct DecodeCall {
@@ -134,6 +136,6 @@ stream_status launch_free(const CacheGeom &c, const int32_t *done, int32_t *info
 stream_status launch_compact(const CacheGeom &c, int32_t *pairs, int32_t *info, void *ws, cudaStream_t st);
 stream_status launch_copy_pages(const CacheGeom &c, int elem, void *k, void *v, const int32_t *pairs, const int32_t *count, int n_pairs, cudaStream_t st);
 stream_status launch_write(const CacheGeom &c, int elem, const void *k, const void *v, int total, long long s_t, long long s_h,
-                           const int32_t *cu_new, void *k_pages, void *v_pages, cudaStream_t st);
+                           const int32_t *cu_new, const int32_t *done, void *k_pages, void *v_pages, cudaStream_t st);
 
 }  // namespace stream

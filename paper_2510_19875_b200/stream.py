@@ -160,7 +160,7 @@ def _load():
     lib.stream_cache_copy_pages.restype = ctypes.c_int
     lib.stream_cache_copy_pages.argtypes = [PC, vp, vp, vp, vp, i32, vp]
     lib.stream_cache_write.restype = ctypes.c_int
-    lib.stream_cache_write.argtypes = [PC, i32, vp, vp, i64, i64, i64, vp, vp, vp, vp, vp, vp]
+    lib.stream_cache_write.argtypes = [PC, i32, vp, vp, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp]
     lib.stream_decode_workspace_bytes.restype = sz
     lib.stream_decode_workspace_bytes.argtypes = [PC, i32]
     lib.stream_decode_attention.restype = ctypes.c_int
@@ -352,9 +352,9 @@ def stream_cache_copy_pages(c: StreamCache, k_pages, v_pages, pairs, count, n_pa
 
 
 def stream_cache_write(c: StreamCache, layer: int, k, v, total: int, stride_t: int, stride_h: int, cu_new, page_table, seq_len,
-                       k_pages, v_pages, stream=None) -> None:
+                       done, k_pages, v_pages, stream=None) -> None:
     _raise(_load().stream_cache_write(ctypes.byref(c), int(layer), _addr(k), _addr(v), int(total), int(stride_t), int(stride_h),
-                                      _addr(cu_new), _addr(page_table), _addr(seq_len), _addr(k_pages), _addr(v_pages),
+                                      _addr(cu_new), _addr(page_table), _addr(seq_len), _addr(done), _addr(k_pages), _addr(v_pages),
                                       _stream_handle(stream)))
 
 
@@ -756,9 +756,12 @@ def cache_copy_pages(cache: PagedCache, moves: CacheMoves, stream=None) -> None:
             (c._p, c.k.data_ptr(), c.v.data_ptr(), pairs.data_ptr(), info.data_ptr() + 4, n), stream)
 
 
-def cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, cu_new: torch.Tensor, *, layer: int = 0, stream=None) -> None:
+def cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, cu_new: torch.Tensor, *, layer: int = 0,
+                info: torch.Tensor | None = None, stream=None) -> None:
     """Writes new tokens' keys and values (``[total, n_kv_heads, d]``, rows ``cu_new[s] .. cu_new[s + 1]`` being slot s's
-    last tokens) to the pages of one layer, after :func:`cache_reserve`."""
+    last tokens) to the pages of one layer, after :func:`cache_reserve`. With its ``info`` nothing is written if it was
+    refused; a caller that has not looked at the info passes it on (the lengths are then as they were, and the last
+    tokens there would be overwritten)."""
     c, shape, strides = cache, k.shape, k.stride()
     if len(shape) != 3 or shape[1] != c.n_kv_heads or shape[2] != c.d or v.shape != shape or v.stride() != strides:
         raise ValueError("k and v must be [total, n_kv_heads, d], alike in strides")
@@ -767,9 +770,11 @@ def cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, cu_new: tor
     if strides[2] != 1:
         raise ValueError("innermost stride must be 1")
     _checked(cu_new, torch.int32, (c.n_slots + 1,), "cu_new", c.device)
+    if info is not None:
+        _checked(info, torch.int32, (4,), "info", c.device)
     _launch(c.device, (_lib or _load()).stream_cache_write,
             (c._p, layer, k.data_ptr(), v.data_ptr(), shape[0], strides[0], strides[1], cu_new.data_ptr(), c.page_table.data_ptr(),
-             c.seq_len.data_ptr(), c.k.data_ptr(), c.v.data_ptr()), stream)
+             c.seq_len.data_ptr(), None if info is None else info.data_ptr(), c.k.data_ptr(), c.v.data_ptr()), stream)
 
 
 def decode_attention(q: torch.Tensor, cache: PagedCache, *, layer: int = 0, scale: float = 0.0, want_lse: bool = False,

@@ -281,6 +281,22 @@ def test_writes_that_cannot_be_are_passed_over(S):
     S.cache_write(cache, k[:0], k[:0], ints([0, 0, 0, 0]))
 
 
+@pytest.mark.parametrize("n_slots", [3, 40])
+def test_nothing_is_written_after_a_refused_reserve(S, n_slots):
+    cache = S.new_cache(n_slots, 4, 4, 400, 2, 16, dtype=F32)  # (by one CTA, by eight)
+    cache.k.zero_(), cache.v.zero_()
+    cu = ints([0] + [8] * n_slots)
+    k = torch.ones(8, 2, 16, device="cuda")
+    for new, done in ((8, 1), (16, 0), (8, 1)):
+        info = S.cache_reserve(cache, ints([new] + [0] * (n_slots - 1)))
+        before = cache.k.clone(), cache.v.clone()
+        S.cache_write(cache, k * new, k * new, cu, info=info)
+        assert info[0] == done
+        if not done:
+            assert torch.equal(cache.k, before[0]) and torch.equal(cache.v, before[1])
+    assert cache.seq_len[0] == 16 and cache.k.min() == 8
+
+
 def test_many_slots(S):
     n = 3000
     cache = S.new_cache(n, 2 * n, 8, 4, 1, 16, dtype=F32)

@@ -65,7 +65,7 @@ def every_call(S, c):
     n = 1 << 40
     return [(S.stream_cache_reserve, (c, A, A, A, A, A, A, n, 0)), (S.stream_cache_fork, (c, A, A, A, A, A, A, A, n, 0)),
             (S.stream_cache_free, (c, A, A, A, A, A, A, n, 0)), (S.stream_cache_compact, (c, A, A, A, A, A, A, n, 0)),
-            (S.stream_cache_copy_pages, (c, A, A, A, A, 3, 0)), (S.stream_cache_write, (c, 0, A, A, 5, 128, 64, A, A, A, A, A, 0)),
+            (S.stream_cache_copy_pages, (c, A, A, A, A, 3, 0)), (S.stream_cache_write, (c, 0, A, A, 5, 128, 64, A, A, A, None, A, A, 0)),
             (S.stream_decode_attention, (c, 0, 4, A, 256, 64, A, A, A, A, 0.0, A, None, A, n, 0))]
 
 
@@ -102,11 +102,12 @@ def test_pointers_and_workspaces(S):
     refused(S, S.STREAM_ERR_INVALID_ARG, S.stream_cache_copy_pages, c, A, A, A, A, -1, 0)
     S.stream_cache_copy_pages(c, None, None, None, None, 0, 0)
     for layer in (-1, 3):
-        refused(S, S.STREAM_ERR_INVALID_ARG, S.stream_cache_write, c, layer, A, A, 5, 128, 64, A, A, A, A, A, 0)
+        refused(S, S.STREAM_ERR_INVALID_ARG, S.stream_cache_write, c, layer, A, A, 5, 128, 64, A, A, A, A, A, A, 0)
         refused(S, S.STREAM_ERR_INVALID_ARG, S.stream_decode_attention, c, layer, 4, A, 256, 64, A, A, A, A, 0.0, A, None, A, 1 << 40, 0)
     for total, st, sh in ((-1, 128, 64), (2 ** 31, 128, 64), (5, 63, 64), (5, 128, 0)):
-        refused(S, S.STREAM_ERR_INVALID_ARG, S.stream_cache_write, c, 0, A, A, total, st, sh, A, A, A, A, A, 0)
-    S.stream_cache_write(c, 0, None, None, 0, 128, 64, A, A, A, None, None, 0)
+        refused(S, S.STREAM_ERR_INVALID_ARG, S.stream_cache_write, c, 0, A, A, total, st, sh, A, A, A, A, A, A, 0)
+    S.stream_cache_write(c, 0, None, None, 0, 128, 64, A, A, A, None, None, None, 0)
+    refused(S, S.STREAM_ERR_INVALID_ARG, S.stream_cache_write, c, 0, A, A, 5, 128, 64, A, A, A, A + 2, A, A, 0)
     for heads, st, sh, scale in ((3, 256, 64, 0.0), (0, 256, 64, 0.0), (4, 63, 64, 0.0), (4, 256, 63, 0.0), (4, 256, 64, float("inf"))):
         refused(S, S.STREAM_ERR_INVALID_ARG, S.stream_decode_attention, c, 0, heads, A, st, sh, A, A, A, A, scale, A, None, A, 1 << 40, 0)
     assert S.stream_decode_workspace_bytes(c, 3) == 0 and S.stream_decode_workspace_bytes(c, 0) == 0
