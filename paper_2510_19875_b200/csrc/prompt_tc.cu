@@ -17,7 +17,7 @@
 // Roles (384 threads): warp 0 loads Q, K and V by TMA (one ring for K and V, in the order of their use); warp 1 issues the MMAs and
 // owns TMEM; warp 2 writes zeros over the rows of a V tile behind the sequence's last key (a weight of zero times what lies
 // there, which may be anything, has to be zero); warps 4..7 and 8..11 are the softmax of the two tiles and store their output.
-// A row's 128 logits stay in registers. Every wait is bounded.
+// A row's 128 logits stay in registers. Every wait is bounded, or for a role whose waits are.
 #include <math_constants.h>
 
 #include "serve_common.cuh"
@@ -118,9 +118,12 @@ __device__ __forceinline__ Item item_at(const Params &P, const Tail<F> *tl, int 
 }
 
 template <class F>
-__device__ __forceinline__ bool wait_w(const void *bar, unsigned parity, Tail<F> *tl, unsigned code) {
-    return mbar_wait_warp(smem_u32(bar), parity, &tl->abort_flag, &g_prompt_status[0], &g_prompt_status[1], code);
+__device__ __forceinline__ bool wait_w(const void *bar, unsigned parity, Tail<F> *tl, unsigned code, long long limit = kWaitCycles) {
+    return mbar_wait_warp(smem_u32(bar), parity, &tl->abort_flag, &g_prompt_status[0], &g_prompt_status[1], code, limit);
 }
+// For the roles that pass over items and may so wait for one that is far ahead, seconds long where the items in front are many and have
+// a million keys: what they wait for comes from roles whose own waits are limited, and ends with their abort.
+constexpr long long kWhileOthersWork = 1ll << 62;
 
 // A place in the ring of K and V tiles: use u of it.
 template <class F>
@@ -184,7 +187,7 @@ __device__ void zero_role(const Params &P, Tail<F> *tl, unsigned char *ring, int
         if ((long long)it.most * kKeys <= it.s.k_n) continue;
         Use<F> last;
         last.u = use.u - 1;
-        if (!wait_w(&tl->v_raw[last.stage()], (parity >> last.stage()) & 1u, tl, 1003)) return;
+        if (!wait_w(&tl->v_raw[last.stage()], (parity >> last.stage()) & 1u, tl, 1003, kWhileOthersWork)) return;
         parity ^= 1u << last.stage();
         const int there = it.s.k_n - (it.most - 1) * kKeys;
         unsigned char *const tile = ring + last.stage() * F::kTile;
@@ -333,7 +336,7 @@ __device__ void softmax_role(const Params &P, Tail<F> *tl, unsigned tmem, int t)
         const bool mine = tok_r < P.per_tile && tok < it.s.q_n;
         float ref = -CUDART_INF_F, l = 0.f;
         for (int j = 0; j < n_tiles; ++j) {
-            if (!wait_w(&tl->s_full[x], n_s++ & 1u, tl, 1021)) return;
+            if (!wait_w(&tl->s_full[x], n_s++ & 1u, tl, 1021, kWhileOthersWork)) return;
             tc_fence_after();
             unsigned sr[2][64];
 #pragma unroll

@@ -772,6 +772,8 @@ def cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, cu_new: tor
     _checked(cu_new, torch.int32, (c.n_slots + 1,), "cu_new", c.device)
     if info is not None:
         _checked(info, torch.int32, (4,), "info", c.device)
+    if not 0 <= layer < c.n_layers:  # (beyond 32 bits too, of which the call would see the lower ones)
+        raise ValueError("no such layer")
     _launch(c.device, (_lib or _load()).stream_cache_write,
             (c._p, layer, k.data_ptr(), v.data_ptr(), shape[0], strides[0], strides[1], cu_new.data_ptr(), c.page_table.data_ptr(),
              c.seq_len.data_ptr(), None if info is None else info.data_ptr(), c.k.data_ptr(), c.v.data_ptr()), stream)
@@ -788,6 +790,8 @@ def decode_attention(q: torch.Tensor, cache: PagedCache, *, layer: int = 0, scal
         raise ValueError("q must be [n_slots, H, d] with the cache's dtype and device")
     if strides[2] != 1:
         raise ValueError("innermost stride must be 1")
+    if not 0 <= layer < c.n_layers:
+        raise ValueError("no such layer")
     n, H, d = shape
     if out is None:
         out = torch.empty_strided(shape, (H * d, d, 1), dtype=q.dtype, device=c.device)

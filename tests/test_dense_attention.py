@@ -77,6 +77,31 @@ def test_long_sequences(S, H, G, d, n, dtype):
     run(S, q, k, v, cu_q, cu_k, True)
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("H,G,d,lens_q,lens_k", [
+    (28, 4, 128, [700, 1500, 0, 333, 64, 2000, 1, 129], [700, 1600, 5, 333, 2000, 2000, 1300, 0]),  # put in the order of their keys
+    (8, 8, 64, [600, 600, 600, 1], [600, 599, 40, 900]),
+    (128, 1, 64, [5000, 300], [5000, 300]),                                                          # too many to be put in order
+])
+def test_more_items_than_ctas(S, H, G, d, lens_q, lens_k, causal):
+    q, k, v, cu_q, cu_k = inputs(H, G, d, lens_q, lens_k, BF16, behind=7, seed=H)
+    run(S, q, k, v, cu_q, cu_k, causal)
+
+
+def test_a_kernel_of_seconds(S):
+    """Waits have a limit of about a second, but some roles of the tensor-core kernel wait for items far ahead: a short prompt behind one
+    of a million tokens and more."""
+    n, m, d = 1_200_000, 77, 128
+    q, k, v = (torch.randn(n + m, h, d, device="cuda", dtype=BF16) for h in (8, 8, 8))
+    out, lse = S.prompt_attention(q, k, v, ints([0, n, n + m]), want_lse=True)
+    torch.cuda.synchronize()
+    S.stream_check_device_status()
+    check(out[n:], lse[:, n:], attention64(q[n:], k[n:], v[n:], 0), m, d, BF16)
+    for at in (0, 1000, 600_001, n - 3):
+        some = attention64(q[at:at + 3], k[:at + 3], v[:at + 3], at)
+        check(out[at:at + 3], lse[:, at:at + 3], some, at + 3, d, BF16)
+
+
 def test_many_sequences(S):
     """More sequences than the tensor-core kernel takes in one launch, of all lengths from none."""
     lens = [i % 23 for i in range(1300)]
