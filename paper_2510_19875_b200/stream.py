@@ -692,10 +692,8 @@ class PagedCache:
         self._p = ctypes.byref(self.struct)
         self._decode_bytes = {}  # workspace of decode_attention by query heads
 
-    def _ledger(self, call, first, *rest, stream):
-        """One of the ledger calls: what it is asked, the ledger, what it gives back, the workspace."""
-        table, length, count, ws = self.page_table, self.seq_len, self.ref_count, self.workspace
-        _launch(self.device, call, (self._p, *first, table.data_ptr(), length.data_ptr(), count.data_ptr(), *rest, ws.data_ptr(), ws.numel()), stream)
+    def _ledger(self):
+        return self.page_table.data_ptr(), self.seq_len.data_ptr(), self.ref_count.data_ptr()
 
     def _info(self):
         return torch.empty_strided((4,), (1,), dtype=torch.int32, device=self.device)
@@ -715,7 +713,8 @@ def cache_reserve(cache: PagedCache, n_new: torch.Tensor, stream=None) -> torch.
     c = cache
     _checked(n_new, torch.int32, (c.n_slots,), "n_new", c.device)
     info = c._info()
-    c._ledger((_lib or _load()).stream_cache_reserve, (n_new.data_ptr(),), info.data_ptr(), stream=stream)
+    _launch(c.device, (_lib or _load()).stream_cache_reserve,
+            (c._p, n_new.data_ptr(), *c._ledger(), info.data_ptr(), c.workspace.data_ptr(), c.workspace.numel()), stream)
     return info
 
 
@@ -725,7 +724,8 @@ def cache_fork(cache: PagedCache, parent: torch.Tensor, stream=None) -> CacheMov
     c = cache
     _checked(parent, torch.int32, (c.n_slots,), "parent", c.device)
     info, pairs = c._info(), torch.empty_strided((c.n_slots, 2), (2, 1), dtype=torch.int32, device=c.device)
-    c._ledger((_lib or _load()).stream_cache_fork, (parent.data_ptr(),), pairs.data_ptr(), info.data_ptr(), stream=stream)
+    _launch(c.device, (_lib or _load()).stream_cache_fork,
+            (c._p, parent.data_ptr(), *c._ledger(), pairs.data_ptr(), info.data_ptr(), c.workspace.data_ptr(), c.workspace.numel()), stream)
     return CacheMoves(pairs, info)
 
 
@@ -734,7 +734,8 @@ def cache_free(cache: PagedCache, done: torch.Tensor, stream=None) -> torch.Tens
     c = cache
     _checked(done, torch.int32, (c.n_slots,), "done", c.device)
     info = c._info()
-    c._ledger((_lib or _load()).stream_cache_free, (done.data_ptr(),), info.data_ptr(), stream=stream)
+    _launch(c.device, (_lib or _load()).stream_cache_free,
+            (c._p, done.data_ptr(), *c._ledger(), info.data_ptr(), c.workspace.data_ptr(), c.workspace.numel()), stream)
     return info
 
 
@@ -742,7 +743,8 @@ def cache_compact(cache: PagedCache, stream=None) -> CacheMoves:
     """Moves the pages in use to the lowest numbers; the copies are due (:func:`cache_copy_pages`)."""
     c = cache
     info, pairs = c._info(), torch.empty_strided((c.n_pages // 2, 2), (2, 1), dtype=torch.int32, device=c.device)
-    c._ledger((_lib or _load()).stream_cache_compact, (), pairs.data_ptr(), info.data_ptr(), stream=stream)
+    _launch(c.device, (_lib or _load()).stream_cache_compact,
+            (c._p, *c._ledger(), pairs.data_ptr(), info.data_ptr(), c.workspace.data_ptr(), c.workspace.numel()), stream)
     return CacheMoves(pairs, info)
 
 
