@@ -8,7 +8,7 @@
 // While the tensor core multiplies for one tile, four warps compute P = 2^(scale (s - ref)) of the other, a thread a row. `ref` is
 // the row's maximum at the first key tile, moved (with O and the sum, which are multiplied by 2^(scale (old - new))) only when a
 // later one has outgrown it by more than 2^30: fp32 sums and bf16 weights keep their relative precision whatever the reference.
-// P is rounded to bf16 for the product (2^-9 of a weight, below the rounding of the bf16 output); the sum l is that of the unrounded
+// P is rounded to bf16 for the product (2^-8 of a weight at most, as the bf16 output is in the end); the sum l is that of the unrounded
 // weights in fp32, and so exact enough for the logarithm that is returned.
 //
 // Order of the issuing warp, per key tile: P_0 V_j, Q_0 K_(j+1), P_1 V_j, Q_1 K_(j+1). MMAs of one thread run in order, so that S_X
@@ -37,6 +37,9 @@ constexpr int kRows = 128, kKeys = 128;  // of a tile
 constexpr int kMaxSeqs = 256;            // of a launch
 constexpr int kMaxLevels = 2048;         // items of a kv head that are put in order
 constexpr float kOutgrown = 30.f;        // log2
+// K and V bytes of the kv heads whose items are walked together, of the 126 MB of L2 (32 / 8 heads, TFLOP/s: 131072 tokens, all heads
+// 1094 to 1117, one at a time 1202 to 1217; 65536, all 1196 to 1219, two 1193 to 1207, three 1250 to 1268; 16384 in halves 1285 for 1372).
+constexpr long long kKvInL2 = 110ll << 20;
 
 template <int D_>
 struct Form {
@@ -60,17 +63,18 @@ struct Tail {
     unsigned long long o_done[2], o_free[2];
     unsigned int tmem_base;
     int abort_flag;
-    int n_items;
+    int n_levels, n_items;                               // items of a kv head; of all
     int sorted;                                          // `order` holds the items of a kv head
     unsigned order[kMaxLevels];                          // sequence << 12 | level, the most keys first
     Seq seq[kMaxSeqs];                                   // the longest first
-    int item_end[kMaxSeqs];                              // items of the sequences up to and with this one
+    int level_end[kMaxSeqs];                             // levels (pairs of tiles, items of a kv head) of the sequences up to and with this one
     uint4 stage[8][128];                                 // of each softmax warp: 32 rows x 32 channels of the output
 };
 
 struct Params {
     PromptGeom g;
     int per_tile;  // tokens of a tile: 128 / hpg
+    int heads;     // kv heads whose items are walked together
 };
 
 // What a CTA works on.
@@ -81,26 +85,33 @@ struct Item {
     int most;             // of both
 };
 
+// The first sequence whose levels end behind the nth.
+template <class F>
+__device__ __forceinline__ int sequence_of(const Tail<F> *tl, int n_seqs, int nth) {
+    int lo = 0, hi = n_seqs - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (tl->level_end[mid] > nth) hi = mid;
+        else lo = mid + 1;
+    }
+    return lo;
+}
+
 template <class F>
 __device__ __forceinline__ Item item_at(const Params &P, const Tail<F> *tl, int id) {
     const PromptGeom &g = P.g;
     Item it;
+    // some kv heads at a time, and of them the sequences' levels (pairs of tiles) in order, head by head
+    const int per_phase = tl->n_levels * P.heads, phase = id / per_phase, rem = id - phase * per_phase;
+    const int heads = min(P.heads, g.G - phase * P.heads), nth = rem / heads;
+    it.kvh = phase * P.heads + rem - nth * heads;
     int lo = 0, level;
     if (tl->sorted) {
-        const int nth = id / g.G;
         lo = (int)(tl->order[nth] >> 12);
         level = (int)(tl->order[nth] & 4095u);
-        it.kvh = id - nth * g.G;
     } else {
-        int hi = g.n_seqs - 1;  // the first sequence whose items end behind id
-        while (lo < hi) {
-            const int mid = (lo + hi) >> 1;
-            if (tl->item_end[mid] > id) hi = mid;
-            else lo = mid + 1;
-        }
-        const int rem = id - (lo > 0 ? tl->item_end[lo - 1] : 0);
-        level = rem / g.G;
-        it.kvh = rem - level * g.G;
+        lo = sequence_of(tl, g.n_seqs, nth);
+        level = nth - (lo > 0 ? tl->level_end[lo - 1] : 0);
     }
     it.s = tl->seq[lo];
     const int pairs = ceil_div(it.s.q_n, 2 * P.per_tile);
@@ -468,7 +479,7 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
         const Span a = span_of(g.cu_q, s, g.total_q), b = span_of(g.cu_k, s, g.total_k);
         return Seq{a.first, a.n, b.first, b.n};
     };
-    for (int s = tid; s < g.n_seqs; s += kThreads) tl->item_end[s] = span(s).k_n;
+    for (int s = tid; s < g.n_seqs; s += kThreads) tl->level_end[s] = span(s).k_n;
     __syncthreads();
     int at[(kMaxSeqs + kThreads - 1) / kThreads];
 #pragma unroll
@@ -476,8 +487,8 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
         const int s = tid + i * kThreads;
         at[i] = 0;
         if (s < g.n_seqs) {
-            const int own = tl->item_end[s];
-            for (int o = 0; o < g.n_seqs; ++o) at[i] += tl->item_end[o] > own || (tl->item_end[o] == own && o < s) ? 1 : 0;
+            const int own = tl->level_end[s];
+            for (int o = 0; o < g.n_seqs; ++o) at[i] += tl->level_end[o] > own || (tl->level_end[o] == own && o < s) ? 1 : 0;
         }
     }
     __syncthreads();
@@ -487,23 +498,26 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
         if (s < g.n_seqs) {
             const Seq q = span(s);
             tl->seq[at[i]] = q;
-            tl->item_end[at[i]] = (int)(((long long)q.q_n + 2 * P.per_tile - 1) / (2 * P.per_tile)) * g.G;
+            tl->level_end[at[i]] = ceil_div(q.q_n, 2 * P.per_tile);
         }
     }
     __syncthreads();
     if (warp == 0) {
         int sum = 0;
         for (int s0 = 0; s0 < g.n_seqs; s0 += 32) {
-            int v = s0 + lane < g.n_seqs ? tl->item_end[s0 + lane] : 0;
+            int v = s0 + lane < g.n_seqs ? tl->level_end[s0 + lane] : 0;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
                 const int y = __shfl_up_sync(0xffffffffu, v, d);
                 if (lane >= d) v += y;
             }
-            if (s0 + lane < g.n_seqs) tl->item_end[s0 + lane] = sum + v;
+            if (s0 + lane < g.n_seqs) tl->level_end[s0 + lane] = sum + v;
             sum += __shfl_sync(0xffffffffu, v, 31);
         }
-        if (lane == 0) tl->n_items = sum;
+        if (lane == 0) {
+            tl->n_levels = sum;
+            tl->n_items = sum * g.G;
+        }
     }
     tc_fence_before();
     __syncthreads();
@@ -513,17 +527,11 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
     // tokens; in this one 2 %). An item's place is how many stand in front of it, which each sequence says in closed form. Not where every
     // item has a CTA of its own, nor where there is too much to count (16 terms a thread take 2 us): the items are many and
     // small against a CTA's sum then.
-    const int n_levels = tl->n_items / g.G;
+    const int n_levels = tl->n_levels;
     const bool sorted = g.n_seqs > 1 && tl->n_items > (int)gridDim.x && n_levels <= kMaxLevels && n_levels * g.n_seqs <= 16 * kThreads;
     if (tid == 0) tl->sorted = sorted ? 1 : 0;
     for (int i = tid; sorted && i < n_levels; i += kThreads) {
-        int own = 0, hi = g.n_seqs - 1;
-        while (own < hi) {
-            const int mid = (own + hi) >> 1;
-            if (tl->item_end[mid] > i * g.G) hi = mid;
-            else own = mid + 1;
-        }
-        const int level = i - (own > 0 ? tl->item_end[own - 1] / g.G : 0), span2 = 2 * P.per_tile;
+        const int own = sequence_of(tl, g.n_seqs, i), level = i - (own > 0 ? tl->level_end[own - 1] : 0), span2 = 2 * P.per_tile;
         // key tiles of a sequence's item at `level`; its items with more than v of them
         auto tiles = [&](const Seq &q, int lv) {
             const int end = min((ceil_div(q.q_n, span2) - lv) * span2, q.q_n);
@@ -573,6 +581,8 @@ stream_status launch(const PromptGeom &g, const void *q, const void *k, const vo
     Params P;
     P.g = g;
     P.per_tile = kRows / g.hpg;
+    const long long fit = kKvInL2 / ((long long)g.total_k * F::D * 4);
+    P.heads = (int)(fit < 1 ? 1 : fit > g.G ? g.G : fit);
     CUtensorMap tq, tk, tv;
     stream_status rc = make_map_q(&tq, g, q, P.per_tile);
     if (rc != STREAM_OK) return rc;

@@ -88,16 +88,17 @@ def test_more_items_than_ctas(S, H, G, d, lens_q, lens_k, causal):
     run(S, q, k, v, cu_q, cu_k, causal)
 
 
-def test_a_kernel_of_seconds(S):
-    """Waits have a limit of about a second, but some roles of the tensor-core kernel wait for items far ahead: a short prompt behind one
-    of a million tokens and more."""
-    n, m, d = 1_200_000, 77, 128
+@pytest.mark.parametrize("n", [70_000, 1_200_000])
+def test_keys_of_more_than_the_cache_holds_and_a_kernel_of_seconds(S, n):
+    """Three kv heads of eight, then one, are walked at a time. Waits have a limit of about a second, but some roles of the tensor-core
+    kernel wait for items far ahead: a short prompt behind one of a million tokens and more."""
+    m, d = 77, 128
     q, k, v = (torch.randn(n + m, h, d, device="cuda", dtype=BF16) for h in (8, 8, 8))
     out, lse = S.prompt_attention(q, k, v, ints([0, n, n + m]), want_lse=True)
     torch.cuda.synchronize()
     S.stream_check_device_status()
     check(out[n:], lse[:, n:], attention64(q[n:], k[n:], v[n:], 0), m, d, BF16)
-    for at in (0, 1000, 600_001, n - 3):
+    for at in (0, 1000, n // 2 + 1, n - 3):
         some = attention64(q[at:at + 3], k[:at + 3], v[:at + 3], at)
         check(out[at:at + 3], lse[:, at:at + 3], some, at + 3, d, BF16)
 
