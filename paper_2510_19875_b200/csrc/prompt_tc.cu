@@ -36,6 +36,7 @@ constexpr int kThreads = 384;
 constexpr int kRows = 128, kKeys = 128;  // of a tile
 constexpr int kMaxSeqs = 256;            // of a launch
 constexpr int kMaxLevels = 2048;         // items of a kv head that are put in order
+constexpr long long kMaxItems = 0x7fffffffll - (1 << 20);
 constexpr float kOutgrown = 30.f;        // log2
 // K and V bytes of the kv heads whose items are walked together, of the 126 MB of L2 (32 / 8 heads, TFLOP/s: 131072 tokens, all heads
 // 1094 to 1117, one at a time 1202 to 1217; 65536, all 1196 to 1219, two 1193 to 1207, three 1250 to 1268; 16384 in halves 1285 for 1372).
@@ -474,49 +475,43 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
     }
     if (warp == 1) tmem_alloc(smem_u32(&tl->tmem_base));  // all columns: one CTA per SM
     after_previous_kernel();
-    // The sequences, those with the most keys first (up to 512: a thread or two each count those in front), and their items
+    // The sequences, those with the most keys first (a thread a sequence counts those in front), and their items
     auto span = [&](int s) {
         const Span a = span_of(g.cu_q, s, g.total_q), b = span_of(g.cu_k, s, g.total_k);
         return Seq{a.first, a.n, b.first, b.n};
     };
-    for (int s = tid; s < g.n_seqs; s += kThreads) tl->level_end[s] = span(s).k_n;
+    if (tid < g.n_seqs) tl->level_end[tid] = span(tid).k_n;
     __syncthreads();
-    int at[(kMaxSeqs + kThreads - 1) / kThreads];
-#pragma unroll
-    for (int i = 0; i < (kMaxSeqs + kThreads - 1) / kThreads; ++i) {
-        const int s = tid + i * kThreads;
-        at[i] = 0;
-        if (s < g.n_seqs) {
-            const int own = tl->level_end[s];
-            for (int o = 0; o < g.n_seqs; ++o) at[i] += tl->level_end[o] > own || (tl->level_end[o] == own && o < s) ? 1 : 0;
-        }
+    static_assert(kMaxSeqs <= kThreads, "a thread a sequence");
+    int at = 0;
+    if (tid < g.n_seqs) {
+        const int own = tl->level_end[tid];
+        for (int o = 0; o < g.n_seqs; ++o) at += tl->level_end[o] > own || (tl->level_end[o] == own && o < tid) ? 1 : 0;
     }
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < (kMaxSeqs + kThreads - 1) / kThreads; ++i) {
-        const int s = tid + i * kThreads;
-        if (s < g.n_seqs) {
-            const Seq q = span(s);
-            tl->seq[at[i]] = q;
-            tl->level_end[at[i]] = ceil_div(q.q_n, 2 * P.per_tile);
-        }
+    if (tid < g.n_seqs) {
+        const Seq q = span(tid);
+        tl->seq[at] = q;
+        tl->level_end[at] = ceil_div(q.q_n, 2 * P.per_tile);
     }
     __syncthreads();
     if (warp == 0) {
-        int sum = 0;
+        long long sum = 0;
         for (int s0 = 0; s0 < g.n_seqs; s0 += 32) {
-            int v = s0 + lane < g.n_seqs ? tl->level_end[s0 + lane] : 0;
+            long long v = s0 + lane < g.n_seqs ? tl->level_end[s0 + lane] : 0;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
-                const int y = __shfl_up_sync(0xffffffffu, v, d);
+                const long long y = __shfl_up_sync(0xffffffffu, v, d);
                 if (lane >= d) v += y;
             }
-            if (s0 + lane < g.n_seqs) tl->level_end[s0 + lane] = sum + v;
+            if (s0 + lane < g.n_seqs) tl->level_end[s0 + lane] = (int)(sum + v);
             sum += __shfl_sync(0xffffffffu, v, 31);
         }
         if (lane == 0) {
-            tl->n_levels = sum;
-            tl->n_items = sum * g.G;
+            // (the host has seen that the sequences' items can be counted, unless their offsets fall and sequences overlap: then nothing is done)
+            const bool fits = sum * g.G <= kMaxItems;
+            tl->n_levels = fits ? (int)sum : 0;
+            tl->n_items = fits ? (int)sum * g.G : 0;
         }
     }
     tc_fence_before();
@@ -614,7 +609,7 @@ bool prompt_tc_supported(const PromptGeom &g, int dtype, const void *q, const vo
     if (dtype != STREAM_BF16 || (g.d != 64 && g.d != 128) || g.hpg > kRows || g.total_k < 1) return false;
     if (g.total_q > 0x7fffff00 || g.total_k > 0x7fffff00) return false;  // (a tile's last row is a coordinate too)
     if ((((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)g.out) & 15) != 0 || ((g.qs_t | g.qs_h | g.ks_t | g.ks_h) & 7) != 0) return false;
-    return ((long long)g.total_q / (2 * (kRows / g.hpg)) + g.n_seqs) * g.G < 0x7fffffffLL - (1 << 20);  // items
+    return ((long long)g.total_q / (2 * (kRows / g.hpg)) + g.n_seqs) * g.G <= kMaxItems;
 }
 
 stream_status launch_prompt_tc(const PromptGeom &g, const void *q, const void *k, const void *v, cudaStream_t st) {

@@ -43,19 +43,20 @@ __host__ __device__ __forceinline__ int ceil_div(int a, int b) { return (int)(((
 // there. By a whole warp. seq < 0: there are fewer.
 struct RowTile { int seq, nth; };
 __device__ __forceinline__ RowTile row_tile(const PromptGeom &g, int nth, int rows, int lane) {
-    for (int s0 = 0, sum = 0; s0 < g.n_seqs; s0 += 32) {
+    long long sum = 0;  // (offsets that fall make sequences overlap: more tiles than 32 bits count)
+    for (int s0 = 0; s0 < g.n_seqs; s0 += 32) {
         const int s = s0 + lane;
-        const int tiles = s < g.n_seqs ? (int)(((long long)span_of(g.cu_q, s, g.total_q).n * g.hpg + rows - 1) / rows) : 0;
-        int incl = tiles;
+        const long long tiles = s < g.n_seqs ? ((long long)span_of(g.cu_q, s, g.total_q).n * g.hpg + rows - 1) / rows : 0;
+        long long incl = tiles;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
-            const int y = __shfl_up_sync(0xffffffffu, incl, d);
+            const long long y = __shfl_up_sync(0xffffffffu, incl, d);
             if (lane >= d) incl += y;
         }
         const unsigned past = __ballot_sync(0xffffffffu, nth < sum + incl);
         if (past != 0) {
             const int at = __ffs(past) - 1;
-            return {s0 + at, nth - sum - __shfl_sync(0xffffffffu, incl - tiles, at)};
+            return {s0 + at, (int)(nth - sum - __shfl_sync(0xffffffffu, incl - tiles, at))};
         }
         sum += __shfl_sync(0xffffffffu, incl, 31);
     }

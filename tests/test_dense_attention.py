@@ -168,6 +168,12 @@ def test_offsets_that_cannot_be_stay_inside(S, dtype, d):
     ref = want(q[50:60], k[100:], v[100:], [0, 10], [0, 100], True)
     check(out[50:60], None, ref, 100, d, dtype)
     assert (out[:50] == 7).all() and (out[60:] == 7).all()
+    # sequences that overlap since the offsets fall: twice the same rows
+    cu = ints([0, 200] * 150)
+    out, lse = S.prompt_attention(q, k, v, cu, want_lse=True)
+    torch.cuda.synchronize()
+    S.stream_check_device_status()
+    check(out, lse, want(q, k, v, [0, 200], [0, 200], True), 200, d, dtype)
 
 
 @pytest.mark.parametrize("dtype,d", [(BF16, 64), (F32, 64)])
