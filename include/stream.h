@@ -391,8 +391,8 @@ typedef struct {
     int32_t n_q_heads;      /* >= 1 */
     int32_t n_kv_heads;     /* >= 1 and divides n_q_heads */
     int32_t d;              /* 16, 32, 64, 128 or 256 */
-    int64_t total_q;        /* rows of Q and of the output, 0 .. 2^31 - 1 */
-    int64_t total_k;        /* rows of K and V, 0 .. 2^31 - 1 */
+    int64_t total_q;        /* rows of Q and of the output, 0 .. 2^31 - 4096 */
+    int64_t total_k;        /* rows of K and V, 0 .. 2^31 - 4096 */
     int32_t causal;         /* 1: a sequence's last query sees all its keys, the one before it all but the last, ...; 0: all see all */
     int32_t dtype;          /* stream_dtype */
     int64_t q_stride_t, q_stride_h, kv_stride_t, kv_stride_h; /* elements; a stride whose extent is 1 does not matter */
@@ -413,7 +413,8 @@ typedef struct {
  *   out         device, dtype of the problem, contiguous [total_q, n_q_heads, d]; rows of no sequence stay as they are. Must
  *               not overlap an input
  *   lse_out     device float32 [n_q_heads, total_q] or NULL; likewise
- * Softmax statistics and the output accumulate in fp32.
+ * Softmax statistics and the output accumulate in fp32, with weights of up to 2^30 before the division by their sum: |V| up to
+ * 2^64 cannot overflow, whatever the logits and the length.
  */
 stream_status stream_prompt_attention(const stream_prompt *p, const void *q, const void *k, const void *v, const int32_t *cu_q,
                                       const int32_t *cu_k, float scale, void *out, float *lse_out, void *cuda_stream);
@@ -429,9 +430,9 @@ stream_status stream_prompt_attention(const stream_prompt *p, const void *q, con
  * A new cache has -1, 0 and 0 everywhere. A page that is not full belongs to one slot alone (a fork copies it);
  * full pages may be shared, and are not written again. The lowest-numbered free pages are taken first. */
 typedef struct {
-    int32_t n_slots;        /* >= 1; n_slots * max_pages < 2^31 */
+    int32_t n_slots;        /* 1 .. 2^30; n_slots * max_pages < 2^31 */
     int32_t n_pages;        /* 1 .. 2^30 */
-    int32_t page_size;      /* tokens; >= 1; max_pages * page_size < 2^31 */
+    int32_t page_size;      /* tokens; >= 1; max_pages * page_size <= 2^31 - 4096 */
     int32_t max_pages;      /* >= 1 */
     int32_t n_kv_heads;     /* >= 1 */
     int32_t d;              /* 16, 32, 64, 128 or 256 */
@@ -510,9 +511,9 @@ stream_status stream_cache_write(const stream_cache *c, int32_t layer, const voi
 /*
  * Attention of one new token of every slot over its cached tokens (its own among them, if it has been written):
  *     out[s, h] = sum_{t < seq_len[s]} softmax_t(scale q_s.k_t) v_t,     lse[s, h] = log sum_t exp(scale q_s.k_t)
- * An empty slot gets zeros and -inf. The tokens of all slots and heads are dealt evenly to the SMs, and pieces of a
- * long slot are joined in a fixed order: the same call gives the same bits. What the pages hold beyond a slot's tokens
- * does not matter (NaN included). Tokens whose page number is outside the cache are left out, and recorded:
+ * An empty slot gets zeros and -inf. Sums as in stream_prompt_attention (|v| up to 2^64). The tokens of all slots and
+ * heads are dealt evenly to the SMs, and pieces of a long slot are joined in a fixed order: the same call gives the same bits.
+ * What the pages hold beyond a slot's tokens does not matter (NaN included). Tokens whose page number is outside the cache are left out, and recorded:
  * stream_read_stats(workspace, ...) then returns STREAM_ERR_DEVICE_CHECK with error = 701 and error_info = such a slot. A seq_len below 0
  * counts as 0, one above max_pages * page_size as that.
  *

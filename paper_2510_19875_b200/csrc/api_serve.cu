@@ -10,6 +10,9 @@ namespace {
 bool known_d(int d) { return d == 16 || d == 32 || d == 64 || d == 128 || d == 256; }
 int elem_bytes(int dtype) { return dtype == STREAM_F32 ? 4 : 2; }
 
+// Tokens of a sequence, of a slot and of all prompts: a tile's last row, counted from its first, stays within 32 bits.
+constexpr long long kMaxTokens = 0x7fffffffLL - 4095;
+
 stream_status invalid(const char *text) {
     set_error("%s", text);
     return STREAM_ERR_INVALID_ARG;
@@ -33,8 +36,8 @@ stream_status make_prompt(const stream_prompt *p, PromptGeom *g) {
         !strides_ok(p->total_k, p->kv_stride_t, p->n_kv_heads, p->kv_stride_h, p->d))
         return invalid("token and head strides must be >= d");
     if (!known_d(p->d)) { set_error("d must be 16, 32, 64, 128 or 256 (got %d)", p->d); return STREAM_ERR_UNSUPPORTED; }
-    if (p->total_q > 0x7fffffffLL || p->total_k > 0x7fffffffLL || p->n_seqs > (1 << 24) || p->n_q_heads > (1 << 16)) {
-        set_error("up to 2^31 - 1 tokens, 2^24 sequences and 2^16 heads");
+    if (p->total_q > kMaxTokens || p->total_k > kMaxTokens || p->n_seqs > (1 << 24) || p->n_q_heads > (1 << 16)) {
+        set_error("up to 2^31 - 4096 tokens, 2^24 sequences and 2^16 heads");
         return STREAM_ERR_UNSUPPORTED;
     }
     *g = PromptGeom{};
@@ -58,8 +61,8 @@ stream_status make_cache(const stream_cache *c, CacheGeom *g) {
         (c->n_kv_heads > 1 && c->stride_h < d))
         return invalid("layer, page, token and head strides must be >= d");
     if (!known_d(d)) { set_error("d must be 16, 32, 64, 128 or 256 (got %d)", d); return STREAM_ERR_UNSUPPORTED; }
-    if ((long long)c->n_slots * c->max_pages > 0x7fffffffLL || (long long)c->max_pages * c->page_size > 0x7fffffffLL ||
-        c->n_pages > (1 << 30) || c->n_kv_heads > (1 << 16) || (long long)c->page_size * c->n_kv_heads * d > 0x3fffffffLL) {
+    if ((long long)c->n_slots * c->max_pages > 0x7fffffffLL || (long long)c->max_pages * c->page_size > kMaxTokens ||
+        c->n_pages > (1 << 30) || c->n_slots > (1 << 30) || c->n_kv_heads > (1 << 16) || (long long)c->page_size * c->n_kv_heads * d > 0x3fffffffLL) {
         set_error("too many slots, pages or tokens for 32-bit indexing");
         return STREAM_ERR_UNSUPPORTED;
     }

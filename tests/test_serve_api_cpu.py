@@ -132,3 +132,18 @@ def test_kernels_that_begin_early_read_no_memory_as_constant(name):
     text = re.sub(r"//.*", "", open(os.path.join(CSRC, name)).read())
     assert not re.findall(r"__ldg\s*\(|ld\.global\.nc", text)
     assert not re.findall(r"const [\w: ]+\*\s*__restrict__", text)
+
+
+def test_largest_sizes(S):
+    """As many tokens and slots as 32 bits count with a tile's rows added, and one more."""
+    most = 2 ** 31 - 4096
+    for kw in (dict(total_q=most + 1), dict(total_k=most + 1)):
+        refused(S, S.STREAM_ERR_UNSUPPORTED, S.stream_prompt_attention, prompt(S, **kw), A, A, A, A, A, 0.0, A, None, 0)
+    S.stream_prompt_attention(prompt(S, total_q=0, total_k=most), None, None, None, A, A, 0.0, None, None, 0)  # nothing to do
+    for good, bad in ((dict(max_pages=most, page_size=1, n_slots=1), dict(max_pages=most + 1, page_size=1, n_slots=1)),
+                      (dict(n_slots=2 ** 30, max_pages=1), dict(n_slots=2 ** 30 + 1, max_pages=1))):
+        assert S.stream_cache_workspace_bytes(cache(S, **good)) > 0
+        c = cache(S, **bad)
+        assert S.stream_cache_workspace_bytes(c) == 0 and S.stream_decode_workspace_bytes(c, 4) == 0
+        for call, args in every_call(S, c):
+            refused(S, S.STREAM_ERR_UNSUPPORTED, call, *args)
