@@ -597,6 +597,18 @@ def _launch(device: torch.device, call, args, stream) -> None:
         _raise(status)
 
 
+def _on_stream(stream, device: torch.device, call, *args, **kwargs):
+    """``call`` with ``stream`` as the current one: what it allocates is then that stream's memory, which nobody on another
+    one is given while the kernels have yet to run (a workspace is let go when the call returns)."""
+    if not isinstance(stream, torch.cuda.Stream):
+        handle = int(stream)
+        stream = torch.cuda.ExternalStream(handle, device=device) if handle > 1 else torch.cuda.default_stream(device)  # (1: cudaStreamLegacy)
+    if stream.device != device:
+        raise ValueError("the stream must be one of the tensors' device")
+    with torch.cuda.stream(stream):
+        return call(*args, **kwargs)
+
+
 _PROMPT = struct.Struct("@iiiiqqiiqqqq")  # StreamPrompt's fields
 assert _PROMPT.size == ctypes.sizeof(StreamPrompt)
 
@@ -607,7 +619,8 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: to
     """Dense attention of packed prompts: q ``[total_q, H, d]``, k and v ``[total_k, G, d]``, ``cu_q`` and ``cu_k``
     int32 CUDA tensors ``[n_seqs + 1]`` with the sequences' first rows (``cu_k``: default ``cu_q``). Under a causal
     mask a sequence's last query sees all its keys. Returns the output ``[total_q, H, d]``, with ``want_lse`` (or
-    ``lse_out``) also the logarithms of the softmax sums, float32 ``[H, total_q]``. Rows of no sequence are left as they are."""
+    ``lse_out``) also the logarithms of the softmax sums, float32 ``[H, total_q]``. Rows of no sequence are left as they are. ``stream``, here and
+    below: the call runs and allocates as under ``torch.cuda.stream(stream)``."""
     if not (q.is_cuda and k.is_cuda and v.is_cuda and cu_q.is_cuda):
         raise ValueError("q, k, v and cu_q must be CUDA tensors (there is no CPU path)")
     qs, ks, q_strides, k_strides, dtype, device = q.shape, k.shape, q.stride(), k.stride(), q.dtype, q.device
@@ -629,6 +642,8 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: to
         cu_k = cu_q
     elif cu_k is not cu_q:
         _checked(cu_k, torch.int32, n, "cu_k", device)
+    if stream is not None:
+        return _on_stream(stream, device, prompt_attention, q, k, v, cu_q, cu_k, causal=causal, scale=scale, want_lse=want_lse, out=out, lse_out=lse_out)
     total, H, d = qs
     fields = (n[0] - 1, H, ks[1], d, total, ks[0], int(causal), _DTYPES[dtype], q_strides[0], q_strides[1], k_strides[0], k_strides[1])
     try:
@@ -645,7 +660,7 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: to
         lse_out = torch.empty_strided((H, total), (total, 1), dtype=torch.float32, device=device)
     _launch(device, (_lib or _load()).stream_prompt_attention,
             (p, q.data_ptr(), k.data_ptr(), v.data_ptr(), cu_q.data_ptr(), cu_k.data_ptr(), scale, out.data_ptr(),
-             None if lse_out is None else lse_out.data_ptr()), stream)
+             None if lse_out is None else lse_out.data_ptr()), None)
     return out if lse_out is None else (out, lse_out)
 
 
@@ -712,9 +727,11 @@ def cache_reserve(cache: PagedCache, n_new: torch.Tensor, stream=None) -> torch.
     the info ``[done, pages taken, free pages, refusals]`` (int32, on the device)."""
     c = cache
     _checked(n_new, torch.int32, (c.n_slots,), "n_new", c.device)
+    if stream is not None:
+        return _on_stream(stream, c.device, cache_reserve, c, n_new)
     info = c._info()
     _launch(c.device, (_lib or _load()).stream_cache_reserve,
-            (c._p, n_new.data_ptr(), *c._ledger(), info.data_ptr(), c.workspace.data_ptr(), c.workspace.numel()), stream)
+            (c._p, n_new.data_ptr(), *c._ledger(), info.data_ptr(), c.workspace.data_ptr(), c.workspace.numel()), None)
     return info
 
 
@@ -723,9 +740,11 @@ def cache_fork(cache: PagedCache, parent: torch.Tensor, stream=None) -> CacheMov
     ``parent[s]``. Full pages are shared; the copies of the others are due: hand the result to :func:`cache_copy_pages`."""
     c = cache
     _checked(parent, torch.int32, (c.n_slots,), "parent", c.device)
+    if stream is not None:
+        return _on_stream(stream, c.device, cache_fork, c, parent)
     info, pairs = c._info(), torch.empty_strided((c.n_slots, 2), (2, 1), dtype=torch.int32, device=c.device)
     _launch(c.device, (_lib or _load()).stream_cache_fork,
-            (c._p, parent.data_ptr(), *c._ledger(), pairs.data_ptr(), info.data_ptr(), c.workspace.data_ptr(), c.workspace.numel()), stream)
+            (c._p, parent.data_ptr(), *c._ledger(), pairs.data_ptr(), info.data_ptr(), c.workspace.data_ptr(), c.workspace.numel()), None)
     return CacheMoves(pairs, info)
 
 
@@ -733,18 +752,22 @@ def cache_free(cache: PagedCache, done: torch.Tensor, stream=None) -> torch.Tens
     """Empties every slot with ``done[s] != 0`` (int32 ``[n_slots]``). Returns ``[1, pages freed, free pages, impossible entries]``."""
     c = cache
     _checked(done, torch.int32, (c.n_slots,), "done", c.device)
+    if stream is not None:
+        return _on_stream(stream, c.device, cache_free, c, done)
     info = c._info()
     _launch(c.device, (_lib or _load()).stream_cache_free,
-            (c._p, done.data_ptr(), *c._ledger(), info.data_ptr(), c.workspace.data_ptr(), c.workspace.numel()), stream)
+            (c._p, done.data_ptr(), *c._ledger(), info.data_ptr(), c.workspace.data_ptr(), c.workspace.numel()), None)
     return info
 
 
 def cache_compact(cache: PagedCache, stream=None) -> CacheMoves:
     """Moves the pages in use to the lowest numbers; the copies are due (:func:`cache_copy_pages`)."""
     c = cache
+    if stream is not None:
+        return _on_stream(stream, c.device, cache_compact, c)
     info, pairs = c._info(), torch.empty_strided((c.n_pages // 2, 2), (2, 1), dtype=torch.int32, device=c.device)
     _launch(c.device, (_lib or _load()).stream_cache_compact,
-            (c._p, *c._ledger(), pairs.data_ptr(), info.data_ptr(), c.workspace.data_ptr(), c.workspace.numel()), stream)
+            (c._p, *c._ledger(), pairs.data_ptr(), info.data_ptr(), c.workspace.data_ptr(), c.workspace.numel()), None)
     return CacheMoves(pairs, info)
 
 
@@ -794,6 +817,8 @@ def decode_attention(q: torch.Tensor, cache: PagedCache, *, layer: int = 0, scal
         raise ValueError("innermost stride must be 1")
     if not 0 <= layer < c.n_layers:
         raise ValueError("no such layer")
+    if stream is not None:
+        return _on_stream(stream, c.device, decode_attention, q, c, layer=layer, scale=scale, want_lse=want_lse, out=out, lse_out=lse_out, workspace=workspace)
     n, H, d = shape
     if out is None:
         out = torch.empty_strided(shape, (H * d, d, 1), dtype=q.dtype, device=c.device)
@@ -815,5 +840,5 @@ def decode_attention(q: torch.Tensor, cache: PagedCache, *, layer: int = 0, scal
             raise ValueError("workspace must be a contiguous uint8 tensor on the cache's device")
     _launch(c.device, (_lib or _load()).stream_decode_attention,
             (c._p, layer, H, q.data_ptr(), strides[0], strides[1], c.k.data_ptr(), c.v.data_ptr(), c.page_table.data_ptr(),
-             c.seq_len.data_ptr(), scale, out.data_ptr(), None if lse_out is None else lse_out.data_ptr(), workspace.data_ptr(), need), stream)
+             c.seq_len.data_ptr(), scale, out.data_ptr(), None if lse_out is None else lse_out.data_ptr(), workspace.data_ptr(), need), None)
     return out if lse_out is None else (out, lse_out)

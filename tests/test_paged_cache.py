@@ -402,3 +402,30 @@ def test_a_step_captured_in_a_graph(S):
         S.cache_write(grown, k, v, cu)
         assert torch.equal(out, S.decode_attention(q, grown))
     assert cache.seq_len.tolist() == [40] * n and torch.equal(cache.page_table, grown.page_table)
+
+
+@pytest.mark.parametrize("handle", [False, True])
+@pytest.mark.parametrize("what", ["prompt", "decode", "reserve", "fork", "free", "compact"])
+def test_memory_of_a_call_on_another_stream(S, what, handle):
+    """What a call on another stream writes to (results, a workspace) is not handed to the current one while the call has yet to run."""
+    q, k = torch.randn(4, 8, 64, device="cuda").to(BF16), torch.randn(4, 2, 64, device="cuda").to(BF16)
+    cu, ones, parent = ints([0, 4]), ints([0, 1, 0, 0]), ints([-1, 0, -1, -1])
+    side = torch.cuda.Stream()
+    for waiting in (False, True):  # (the first time kernels are loaded, which waits for the GPU)
+        cache, _, _ = filled_cache(S, [70, 0, 33, 0], 16, 2, 64, BF16)
+        calls = dict(prompt=lambda: S.prompt_attention(q, k, k, cu, want_lse=True, stream=st), decode=lambda: S.decode_attention(q, cache, want_lse=True, stream=st),
+                     reserve=lambda: S.cache_reserve(cache, ones, stream=st), fork=lambda: S.cache_fork(cache, parent, stream=st),
+                     free=lambda: S.cache_free(cache, ones, stream=st), compact=lambda: S.cache_compact(cache, stream=st))
+        sizes = [16, 32, 2 * 4 * 8 * 64, 4 * 4 * 8, 8 * (cache.n_pages // 2), S.stream_decode_workspace_bytes(cache.struct, 8)]
+        st = side.cuda_stream if handle else side
+        torch.cuda.synchronize()
+        if waiting:
+            with torch.cuda.stream(side):
+                torch.cuda._sleep(400_000_000)  # (a fifth of a second)
+        calls[what]()
+        here = [torch.full((n,), 77, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(4)]
+        torch.cuda.current_stream().synchronize()
+        assert not (waiting and side.query())
+        side.synchronize()
+        for x in here:
+            assert (x == 77).all()
