@@ -173,8 +173,9 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas) prompt_mma_kernel(co
         __syncthreads();  // (the buffers of the tile after next)
     }
     wp::cp_async_wait<0>();
-    __syncwarp();
-    // the output over the warp's own rows of Q, and from there in pieces of 16 bytes
+    // The output over the warp's own rows of Q, and from there in pieces of 16 bytes. Those rows came by copies of other warps' threads, which no
+    // barrier has waited for where no row of the tile sees a key (the loop did not run).
+    __syncthreads();
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
         l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);

@@ -234,3 +234,21 @@ def test_agrees_with_the_sparse_pass_that_keeps_every_block(S):
     w = attention64(*(x[0].transpose(0, 1) for x in (q, k, v)), 0)
     check(dense, None, w, T, d, BF16)
     check(sparse[0].transpose(0, 1), None, w, T, d, BF16)
+
+
+@pytest.mark.parametrize("keys", [0, 40])
+@pytest.mark.parametrize("H,G,d,dtype", [(8, 2, 256, BF16), (8, 2, 128, BF16), (8, 2, 64, BF16), (8, 2, 32, BF16), (7, 1, 16, BF16), (300, 2, 64, BF16),
+                                         (8, 2, 128, F32), (8, 1, 256, F32)])
+def test_tiles_that_see_no_key_are_zeros_every_time(S, H, G, d, dtype, keys):
+    """Thousands of row tiles without any key, of a Q that L2 does not hold: what is stored is never Q, which comes to the place that the output leaves from.
+    Without keys at all, and under a causal mask where the last queries alone see one."""
+    n = 160 * 2 ** 20 // (H * d * (2 if dtype is BF16 else 4))
+    q = torch.full((n, H, d), 3.0, dtype=dtype, device="cuda")
+    k, v = (torch.ones(keys, G, d, dtype=dtype, device="cuda") for _ in range(2))
+    cu_q, cu_k = ints([0, 1, n // 3, n]), ints([0, 0, 0, keys])
+    out, lse = torch.empty_like(q), torch.empty(H, n, device="cuda")
+    for _ in range(10):
+        out.fill_(5), lse.fill_(5)
+        S.prompt_attention(q, k, v, cu_q, cu_k, out=out, lse_out=lse)
+        assert not out[:n - keys].any() and (lse[:, :n - keys] == -float("inf")).all()
+        assert (out[n - keys:] == 1).all()  # (equal logits: weights of 1, and m (1 / m) is 1 in fp32 up to m = 40)

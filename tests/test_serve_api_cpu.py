@@ -147,3 +147,19 @@ def test_largest_sizes(S):
         assert S.stream_cache_workspace_bytes(c) == 0 and S.stream_decode_workspace_bytes(c, 4) == 0
         for call, args in every_call(S, c):
             refused(S, S.STREAM_ERR_UNSUPPORTED, call, *args)
+
+
+@pytest.mark.parametrize("name,threads,rows,per_piece,dims", [("prompt_mma.cu", 256, 128, 8, (16, 32, 64, 128, 256)), ("prompt_f32.cu", 128, 64, 4, (16, 32, 64, 128))])
+def test_output_in_the_place_of_q_waits_for_every_warps_copies(name, threads, rows, per_piece, dims):
+    """A tile without keys runs no barrier in its key loop: one has to stand between the copies of Q, most of which threads of
+    other warps make, and the output that takes Q's place."""
+    others = {}
+    for d in dims:
+        pieces = d // per_piece  # piece i, of row i / pieces, is thread i % threads' to copy; 16 rows are a warp's
+        others[d] = sum(i % threads // 32 != i // pieces // 16 for i in range(rows * pieces))
+    assert max(others.values()) > 0
+    text = re.sub(r"//.*", "", open(os.path.join(CSRC, name)).read())
+    assert re.search(r"i % kPieces.*\n(?:.*\n){1,3}.*cp_async16\(q_s", text)  # (as modelled here)
+    behind = text[text.index("cp_async_wait<0>()"):]  # the first is behind the loop
+    output = re.search(r"sm\.q \+", behind)
+    assert "__syncthreads()" in behind[:output.start()]
