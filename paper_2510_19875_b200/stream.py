@@ -677,8 +677,8 @@ class PagedCache:
 
     ``k`` and ``v`` are ``[n_layers, n_pages, page_size, n_kv_heads, d]`` (views of any stride order, innermost
     stride 1, both alike), ``page_table`` int32 ``[n_slots, max_pages]``, ``seq_len`` int32 ``[n_slots]`` and
-    ``ref_count`` int32 ``[n_pages]``, all on one device. The object keeps them and a workspace for the ledger
-    calls; :func:`new_cache` makes an empty one."""
+    ``ref_count`` int32 ``[n_pages]``, all on one device. The object keeps them and nothing else on the device;
+    :func:`new_cache` makes an empty one."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, seq_len: torch.Tensor, ref_count: torch.Tensor):
         if not k.is_cuda or not v.is_cuda:
@@ -703,7 +703,7 @@ class PagedCache:
         n = stream_cache_workspace_bytes(self.struct)
         if n == 0:
             raise StreamError(STREAM_ERR_INVALID_ARG, stream_last_error())
-        self.workspace = _empty((n,), torch.uint8, self.device)
+        self._ledger_bytes = n
         self._p = ctypes.byref(self.struct)
         self._decode_bytes = {}  # workspace of decode_attention by query heads
 
@@ -712,6 +712,11 @@ class PagedCache:
 
     def _info(self):
         return torch.empty_strided((4,), (1,), dtype=torch.int32, device=self.device)
+
+    def _workspace(self):
+        """For one ledger call: the current stream's memory, as the call's results are. (The handle may be gone before the call has run, and
+        a graph that the call is captured in outlives it.)"""
+        return torch.empty_strided((self._ledger_bytes,), (1,), dtype=torch.uint8, device=self.device)
 
 
 def new_cache(n_slots: int, n_pages: int, page_size: int, max_pages: int, n_kv_heads: int, d: int, *, n_layers: int = 1,
@@ -729,9 +734,9 @@ def cache_reserve(cache: PagedCache, n_new: torch.Tensor, stream=None) -> torch.
     _checked(n_new, torch.int32, (c.n_slots,), "n_new", c.device)
     if stream is not None:
         return _on_stream(stream, c.device, cache_reserve, c, n_new)
-    info = c._info()
+    info, ws = c._info(), c._workspace()
     _launch(c.device, (_lib or _load()).stream_cache_reserve,
-            (c._p, n_new.data_ptr(), *c._ledger(), info.data_ptr(), c.workspace.data_ptr(), c.workspace.numel()), None)
+            (c._p, n_new.data_ptr(), *c._ledger(), info.data_ptr(), ws.data_ptr(), c._ledger_bytes), None)
     return info
 
 
@@ -742,9 +747,9 @@ def cache_fork(cache: PagedCache, parent: torch.Tensor, stream=None) -> CacheMov
     _checked(parent, torch.int32, (c.n_slots,), "parent", c.device)
     if stream is not None:
         return _on_stream(stream, c.device, cache_fork, c, parent)
-    info, pairs = c._info(), torch.empty_strided((c.n_slots, 2), (2, 1), dtype=torch.int32, device=c.device)
+    info, ws, pairs = c._info(), c._workspace(), torch.empty_strided((c.n_slots, 2), (2, 1), dtype=torch.int32, device=c.device)
     _launch(c.device, (_lib or _load()).stream_cache_fork,
-            (c._p, parent.data_ptr(), *c._ledger(), pairs.data_ptr(), info.data_ptr(), c.workspace.data_ptr(), c.workspace.numel()), None)
+            (c._p, parent.data_ptr(), *c._ledger(), pairs.data_ptr(), info.data_ptr(), ws.data_ptr(), c._ledger_bytes), None)
     return CacheMoves(pairs, info)
 
 
@@ -754,9 +759,9 @@ def cache_free(cache: PagedCache, done: torch.Tensor, stream=None) -> torch.Tens
     _checked(done, torch.int32, (c.n_slots,), "done", c.device)
     if stream is not None:
         return _on_stream(stream, c.device, cache_free, c, done)
-    info = c._info()
+    info, ws = c._info(), c._workspace()
     _launch(c.device, (_lib or _load()).stream_cache_free,
-            (c._p, done.data_ptr(), *c._ledger(), info.data_ptr(), c.workspace.data_ptr(), c.workspace.numel()), None)
+            (c._p, done.data_ptr(), *c._ledger(), info.data_ptr(), ws.data_ptr(), c._ledger_bytes), None)
     return info
 
 
@@ -765,9 +770,9 @@ def cache_compact(cache: PagedCache, stream=None) -> CacheMoves:
     c = cache
     if stream is not None:
         return _on_stream(stream, c.device, cache_compact, c)
-    info, pairs = c._info(), torch.empty_strided((c.n_pages // 2, 2), (2, 1), dtype=torch.int32, device=c.device)
+    info, ws, pairs = c._info(), c._workspace(), torch.empty_strided((c.n_pages // 2, 2), (2, 1), dtype=torch.int32, device=c.device)
     _launch(c.device, (_lib or _load()).stream_cache_compact,
-            (c._p, *c._ledger(), pairs.data_ptr(), info.data_ptr(), c.workspace.data_ptr(), c.workspace.numel()), None)
+            (c._p, *c._ledger(), pairs.data_ptr(), info.data_ptr(), ws.data_ptr(), c._ledger_bytes), None)
     return CacheMoves(pairs, info)
 
 

@@ -1,5 +1,6 @@
 """The paged cache: its ledger against plain Python, the copies, and decode attention against 64 bits."""
 import random
+from types import SimpleNamespace
 
 import pytest
 import torch
@@ -429,3 +430,78 @@ def test_memory_of_a_call_on_another_stream(S, what, handle):
         side.synchronize()
         for x in here:
             assert (x == 77).all()
+
+
+LEDGER_CALLS = dict(reserve=lambda S, c, x, **kw: S.cache_reserve(c, x, **kw), fork=lambda S, c, x, **kw: S.cache_fork(c, x, **kw),
+                    free=lambda S, c, x, **kw: S.cache_free(c, x, **kw), compact=lambda S, c, x, **kw: S.cache_compact(c, **kw))
+
+
+def own_arrays(S, lens):
+    """The arrays of a cache, to be held without a handle."""
+    cache, _, led = filled_cache(S, lens, 16, 2, 64, BF16, spare=40, max_pages=12)
+    return (cache.k, cache.v, cache.page_table, cache.seq_len, cache.ref_count), led
+
+
+@pytest.mark.parametrize("how", ["stream", "handle", "current"])
+@pytest.mark.parametrize("what", LEDGER_CALLS)
+def test_a_ledger_call_hands_out_memory_of_its_own_stream(S, monkeypatch, what, how):
+    """The workspace of a call on another stream is that stream's memory, so that one who lets go of the handle at once gets none of
+    it on the current one. Nothing is launched here: the calls are recorded."""
+    arrays, _ = own_arrays(S, [70, 0, 33, 0])
+    x = ints([0, 1, 0, 0] if what != "fork" else [-1, 0, -1, -1])
+    side = torch.cuda.Stream()
+    cache = S.PagedCache(*arrays)
+    n = S.stream_cache_workspace_bytes(cache.struct)
+    seen = []
+    with monkeypatch.context() as m:
+        m.setattr(S, "_lib", SimpleNamespace(**{f"stream_cache_{w}": lambda *a: seen.append(a) or 0 for w in LEDGER_CALLS}))
+        if how == "current":
+            with torch.cuda.stream(side):
+                LEDGER_CALLS[what](S, cache, x)
+        else:
+            LEDGER_CALLS[what](S, cache, x, stream=side if how == "stream" else side.cuda_stream)
+        del cache
+    (args,) = seen
+    at, size, stream = args[-3:]
+    assert size >= n and at % 256 == 0 and stream == side.cuda_stream
+    here = [torch.empty(m, dtype=torch.uint8, device="cuda") for m in (n, 512, 1024, 2048) for _ in range(8)]
+    assert all(y.data_ptr() + y.numel() <= at or at + size <= y.data_ptr() for y in here)
+
+
+@pytest.mark.parametrize("how", ["stream", "current", "graph"])
+@pytest.mark.parametrize("what", LEDGER_CALLS)
+def test_the_handle_is_let_go_before_its_call_has_run(S, what, how):
+    """The ledger's arrays held by the program, a handle made for one call only, and the current stream busy with memory of its own."""
+    lens = [70, 0, 33, 0, 90, 16]
+    x = dict(reserve=[20, 17, 0, 100, 3, 1], fork=[-1, 0, -1, 2, -1, -1], free=[1, 0, 0, 0, 1, 0], compact=None)[what]
+    dev = None if x is None else ints(x)
+    side = torch.cuda.Stream()
+    for waiting in (False, True):  # (the first time kernels are loaded, which waits for the GPU)
+        arrays, led = own_arrays(S, lens)
+        if what == "compact":
+            S.cache_free(S.PagedCache(*arrays), ints([0, 0, 1, 0, 0, 0])), led.free([0, 0, 1, 0, 0, 0])
+        torch.cuda.synchronize()
+        if how == "graph":
+            graph, cache = torch.cuda.CUDAGraph(), S.PagedCache(*arrays)
+            with torch.cuda.graph(graph):
+                got = LEDGER_CALLS[what](S, cache, dev)
+            del cache
+        with torch.cuda.stream(side):
+            if waiting:
+                torch.cuda._sleep(200_000_000)
+            if how == "graph":
+                graph.replay()
+            elif how == "current":
+                got = LEDGER_CALLS[what](S, S.PagedCache(*arrays), dev)
+        if how == "stream":
+            got = LEDGER_CALLS[what](S, S.PagedCache(*arrays), dev, stream=side)
+        here = [torch.full((m,), 0x77, dtype=torch.uint8, device="cuda") for m in (512, 1024, 2048) for _ in range(8)]
+        torch.cuda.current_stream().synchronize()
+        side.synchronize()
+        assert all((y == 0x77).all() for y in here)
+        if what in ("fork", "compact"):
+            pairs, want = led.fork(x) if what == "fork" else led.compact()
+            assert got.info.tolist() == want and got.pairs.tolist() == pairs
+        else:
+            assert got.tolist() == (led.reserve(x) if what == "reserve" else led.free(x))
+        assert led.same(SimpleNamespace(page_table=arrays[2], seq_len=arrays[3], ref_count=arrays[4], device=arrays[0].device))
