@@ -597,14 +597,19 @@ def _launch(device: torch.device, call, args, stream) -> None:
         _raise(status)
 
 
+def _checked_stream(stream, device: torch.device):
+    """A stream, or its handle, of whose device nothing is known."""
+    if isinstance(stream, torch.cuda.Stream) and stream.device != device:
+        raise ValueError("the stream must be one of the tensors' device")
+    return stream
+
+
 def _on_stream(stream, device: torch.device, call, *args, **kwargs):
     """``call`` with ``stream`` as the current one: what it allocates is then that stream's memory, which nobody on another
     one is given while the kernels have yet to run (a workspace is let go when the call returns)."""
-    if not isinstance(stream, torch.cuda.Stream):
+    if not isinstance(_checked_stream(stream, device), torch.cuda.Stream):
         handle = int(stream)
         stream = torch.cuda.ExternalStream(handle, device=device) if handle > 1 else torch.cuda.default_stream(device)  # (1: cudaStreamLegacy)
-    if stream.device != device:
-        raise ValueError("the stream must be one of the tensors' device")
     with torch.cuda.stream(stream):
         return call(*args, **kwargs)
 
@@ -783,7 +788,7 @@ def cache_copy_pages(cache: PagedCache, moves: CacheMoves, stream=None) -> None:
     _checked(pairs, torch.int32, (n, 2), "pairs", c.device)
     _checked(info, torch.int32, (4,), "info", c.device)
     _launch(c.device, (_lib or _load()).stream_cache_copy_pages,
-            (c._p, c.k.data_ptr(), c.v.data_ptr(), pairs.data_ptr(), info.data_ptr() + 4, n), stream)
+            (c._p, c.k.data_ptr(), c.v.data_ptr(), pairs.data_ptr(), info.data_ptr() + 4, n), _checked_stream(stream, c.device))
 
 
 def cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, cu_new: torch.Tensor, *, layer: int = 0,
@@ -806,7 +811,7 @@ def cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, cu_new: tor
         raise ValueError("no such layer")
     _launch(c.device, (_lib or _load()).stream_cache_write,
             (c._p, layer, k.data_ptr(), v.data_ptr(), shape[0], strides[0], strides[1], cu_new.data_ptr(), c.page_table.data_ptr(),
-             c.seq_len.data_ptr(), None if info is None else info.data_ptr(), c.k.data_ptr(), c.v.data_ptr()), stream)
+             c.seq_len.data_ptr(), None if info is None else info.data_ptr(), c.k.data_ptr(), c.v.data_ptr()), _checked_stream(stream, c.device))
 
 
 def decode_attention(q: torch.Tensor, cache: PagedCache, *, layer: int = 0, scale: float = 0.0, want_lse: bool = False,

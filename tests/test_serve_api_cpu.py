@@ -163,3 +163,29 @@ def test_output_in_the_place_of_q_waits_for_every_warps_copies(name, threads, ro
     behind = text[text.index("cp_async_wait<0>()"):]  # the first is behind the loop
     output = re.search(r"sm\.q \+", behind)
     assert "__syncthreads()" in behind[:output.start()]
+
+
+@pytest.mark.parametrize("what", ["prompt", "decode", "reserve", "fork", "free", "compact", "write", "copy"])
+def test_a_stream_of_another_device_is_refused(S, monkeypatch, what):
+    """By every call, before anything is launched or allocated. (Device cpu stands for the tensors' own.)"""
+    class Stream:
+        device, cuda_stream = torch.device("cuda", 1), 12345
+
+    class OnGpu(torch.Tensor):
+        is_cuda = True
+
+    monkeypatch.setattr(torch.cuda, "Stream", Stream)
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32)  # noqa: E731
+    k = torch.zeros(1, 4, 4, 2, 64)
+    q, one, cu = torch.zeros(2, 4, 64), ints(1, 0), ints(0, 1, 1)
+    c = object.__new__(S.PagedCache)
+    c.device, c.k, c.v, c.page_table, c.seq_len, c.ref_count = k.device, k, k, ints(-1, -1).view(2, 1), ints(0, 0), ints(0, 0, 0, 0)
+    c.n_layers, c.n_pages, c.page_size, c.n_kv_heads, c.d, c.n_slots, c.max_pages, c._p = 1, 4, 4, 2, 64, 2, 1, None
+    t = lambda x: x.as_subclass(OnGpu)  # noqa: E731
+    calls = dict(prompt=lambda st: S.prompt_attention(t(q), t(q), t(q), t(cu), stream=st), decode=lambda st: S.decode_attention(q, c, stream=st),
+                 reserve=lambda st: S.cache_reserve(c, one, stream=st), fork=lambda st: S.cache_fork(c, one, stream=st),
+                 free=lambda st: S.cache_free(c, one, stream=st), compact=lambda st: S.cache_compact(c, stream=st),
+                 write=lambda st: S.cache_write(c, q[:, :2], q[:, 2:], cu, stream=st),
+                 copy=lambda st: S.cache_copy_pages(c, S.CacheMoves(ints(-1, -1).view(1, 2), ints(1, 0, 0, 0)), stream=st))
+    with pytest.raises(ValueError, match="stream"):
+        calls[what](Stream())
