@@ -409,7 +409,7 @@ typedef struct {
  *   q, k, v     device, read only
  *   cu_q, cu_k  device int32 [n_seqs + 1], ascending; an entry outside 0 .. total_q (total_k) counts as the nearest
  *               inside, and a sequence whose end lies before its beginning is empty
- *   scale       logit scale; <= 0 selects 1/sqrt(d)
+ *   scale       logit scale, up to 2.3e38 (fp32 holds scale log2(e)); <= 0 selects 1/sqrt(d)
  *   out         device, dtype of the problem, contiguous [total_q, n_q_heads, d]; rows of no sequence stay as they are. Must
  *               not overlap an input
  *   lse_out     device float32 [n_q_heads, total_q] or NULL; likewise
@@ -519,7 +519,7 @@ stream_status stream_cache_write(const stream_cache *c, int32_t layer, const voi
  *
  *   n_q_heads   a multiple of n_kv_heads
  *   q           device [n_slots, n_q_heads, d] with the strides given (elements, innermost 1); read only
- *   scale       logit scale; <= 0 selects 1/sqrt(d)
+ *   scale       logit scale, up to 2.3e38 (fp32 holds scale log2(e)); <= 0 selects 1/sqrt(d)
  *   out         device, dtype of the cache, contiguous [n_slots, n_q_heads, d]; overwritten. Must not overlap an input
  *   lse_out     device float32 [n_slots, n_q_heads] or NULL
  *   workspace   device, 256-byte aligned, >= stream_decode_workspace_bytes(c, n_q_heads); overwritten, nothing is kept

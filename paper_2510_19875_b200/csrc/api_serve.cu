@@ -19,6 +19,13 @@ stream_status invalid(const char *text) {
 }
 bool natural(const void *p, int bytes) { return ((uintptr_t)p & (uintptr_t)(bytes - 1)) == 0; }
 
+// The scale in units of log2. A NaN selects no default, and a finite scale may pass fp32 here: both would make every output NaN.
+stream_status make_scale(float scale, int d, float *scale_log2) {
+    if (scale <= 0.f) scale = 1.0f / sqrtf((float)d);
+    *scale_log2 = scale * 1.4426950408889634f;
+    return std::isfinite(*scale_log2) ? STREAM_OK : invalid("scale must be finite, times log2(e) too");
+}
+
 // Strides of a [rows, heads, d] tensor: at least a head's row apart, where there is more than one.
 bool strides_ok(long long rows, long long s_t, int heads, long long s_h, int d) {
     return (rows <= 1 || s_t >= d) && (heads <= 1 || s_h >= d);
@@ -108,9 +115,9 @@ stream_status stream_prompt_attention(const stream_prompt *p, const void *q, con
     const int e = elem_bytes(p->dtype);
     if (!natural(q, e) || !natural(k, e) || !natural(v, e) || !natural(out, e) || !natural(lse_out, 4) || !natural(cu_q, 4) || !natural(cu_k, 4))
         return invalid("a pointer is not aligned to its elements");
-    if (!(scale > 0.f)) scale = 1.0f / sqrtf((float)g.d);
-    if (!std::isfinite(scale)) return invalid("scale must be finite");
-    g.cu_q = cu_q; g.cu_k = cu_k; g.scale_log2 = scale * 1.4426950408889634f; g.out = out; g.lse = lse_out;
+    rc = make_scale(scale, g.d, &g.scale_log2);
+    if (rc != STREAM_OK) return rc;
+    g.cu_q = cu_q; g.cu_k = cu_k; g.out = out; g.lse = lse_out;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (prompt_tc_supported(g, p->dtype, q, k, v)) return launch_prompt_tc(g, q, k, v, st);
     if (prompt_mma_supported(g, p->dtype, q, k, v)) return launch_prompt_mma(g, q, k, v, st);
@@ -220,8 +227,8 @@ stream_status stream_decode_attention(const stream_cache *c, int32_t layer, int3
     if (!natural(q, e) || !natural(k_pages, e) || !natural(v_pages, e) || !natural(out, e) || !natural(page_table, 4) || !natural(seq_len, 4) || !natural(lse_out, 4))
         return invalid("a pointer is not aligned to its elements");
     if ((long long)a.c.n_slots * n_q_heads > 0x7fffffffLL / 256) { set_error("too many slots and heads for 32-bit indexing"); return STREAM_ERR_UNSUPPORTED; }
-    if (!(scale > 0.f)) scale = 1.0f / sqrtf((float)a.c.d);
-    if (!std::isfinite(scale)) return invalid("scale must be finite");
+    rc = make_scale(scale, a.c.d, &a.scale_log2);
+    if (rc != STREAM_OK) return rc;
     const size_t need = decode_workspace_bytes(a.c);
     if (workspace == nullptr || workspace_bytes < need || ((uintptr_t)workspace & 255) != 0) {
         set_error("workspace must be a 256-byte aligned device buffer of at least %zu bytes", need);
@@ -234,7 +241,6 @@ stream_status stream_decode_attention(const stream_cache *c, int32_t layer, int3
     a.qs_h = n_q_heads > 1 ? q_stride_h : a.c.d;
     const long long at = (long long)layer * a.c.s_l * e;
     a.q = q; a.k = (const char *)k_pages + at; a.v = (const char *)v_pages + at;
-    a.scale_log2 = scale * 1.4426950408889634f;
     a.out = out; a.lse = lse_out;
     return launch_decode(a, c->dtype, workspace, (cudaStream_t)cuda_stream);
 }

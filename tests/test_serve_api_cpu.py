@@ -189,3 +189,9 @@ def test_a_stream_of_another_device_is_refused(S, monkeypatch, what):
                  copy=lambda st: S.cache_copy_pages(c, S.CacheMoves(ints(-1, -1).view(1, 2), ints(1, 0, 0, 0)), stream=st))
     with pytest.raises(ValueError, match="stream"):
         calls[what](Stream())
+
+
+@pytest.mark.parametrize("scale", [float("nan"), float("inf"), 3.4e38, 2.36e38])  # (the last, times log2(e), is 2^128 and a little)
+def test_scales_whose_logits_fp32_does_not_hold(S, scale):
+    refused(S, S.STREAM_ERR_INVALID_ARG, S.stream_prompt_attention, prompt(S), A, A, A, A, A, scale, A, None, 0)
+    refused(S, S.STREAM_ERR_INVALID_ARG, S.stream_decode_attention, cache(S), 0, 4, A, 256, 64, A, A, A, A, scale, A, None, A, 1 << 40, 0)
