@@ -819,7 +819,9 @@ def decode_attention(q: torch.Tensor, cache: PagedCache, *, layer: int = 0, scal
                      stream=None):
     """Attention of one new token of every slot, q ``[n_slots, H, d]``, over its cached tokens. Returns the output
     ``[n_slots, H, d]``, with ``want_lse`` (or ``lse_out``) also the logarithms of the softmax sums, float32
-    ``[n_slots, H]``. ``workspace``: uint8, at least :func:`stream_decode_workspace_bytes`, one per call that can overlap."""
+    ``[n_slots, H]``. ``workspace``: uint8, at least :func:`stream_decode_workspace_bytes`, one per call that can overlap.
+    Tokens whose page number is outside the cache are left out without an error here; the call's workspace has a record of them, which only
+    one who gave it can look at (:func:`stream_read_stats` of it then raises, status ``STREAM_ERR_DEVICE_CHECK``)."""
     c, shape, strides = cache, q.shape, q.stride()
     if len(shape) != 3 or shape[0] != c.n_slots or shape[2] != c.d or q.dtype is not c.k.dtype or q.device != c.device:
         raise ValueError("q must be [n_slots, H, d] with the cache's dtype and device")
