@@ -246,7 +246,7 @@ def _own(st, kind):
         return S.decode_attention(st["q"], cache, want_lse=True)
     if kind == "write":
         info = S.cache_reserve(cache, st["new"])
-        S.cache_write(cache, st["k_new"], st["v_new"], st["cu_new"])
+        S.cache_write(cache, st["k_new"], st["v_new"], st["cu_new"], info=info)
         return info, *st["ledger"], cache.k, cache.v
     forked = S.cache_fork(cache, st["parent"])
     S.cache_copy_pages(cache, forked)
