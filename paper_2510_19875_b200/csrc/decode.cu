@@ -317,7 +317,7 @@ template <class T, int D>
 cudaError_t launch_fma(const Args &A, int vec, cudaStream_t st) {
     const int smem = (int)sizeof(Smem<T, D>);
     static DeviceFlags done;
-    cudaError_t e = allow_smem(decode_kernel<T, D>, smem, done);
+    cudaError_t e = allow_smem_once(decode_kernel<T, D>, smem, done);
     if (e != cudaSuccess) return e;
     return launch_early(decode_kernel<T, D>, (unsigned)A.grid, kThreads, smem, st, A, vec);
 }

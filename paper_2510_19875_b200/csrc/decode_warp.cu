@@ -44,12 +44,6 @@ struct Smem {
     unsigned o_at[kThreads / 32];  // where in its ring a warp has left its O
 };
 
-__device__ __forceinline__ void ldmatrix4(unsigned addr, unsigned &a, unsigned &b, unsigned &c, unsigned &d) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(a), "=r"(b), "=r"(c), "=r"(d) : "r"(addr) : "memory");
-}
-__device__ __forceinline__ void ldmatrix4_t(unsigned addr, unsigned &a, unsigned &b, unsigned &c, unsigned &d) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(a), "=r"(b), "=r"(c), "=r"(d) : "r"(addr) : "memory");
-}
 // Byte of piece x (16 bytes) of row r in a tile: turned, so that eight rows' same piece touch every bank.
 template <class T, int D>
 __device__ __forceinline__ unsigned piece_at(int r, int x) {
@@ -69,7 +63,7 @@ struct Walk {
         q_addr = wp::smem_addr(sm.q);
         if constexpr (F::kQInRegs) {
 #pragma unroll
-            for (int x = 0; x < D / 16; ++x) ldmatrix4(q_addr + piece_at<T, D>(lane & 15, 2 * x + (lane >> 4)), qa[x][0], qa[x][1], qa[x][2], qa[x][3]);
+            for (int x = 0; x < D / 16; ++x) wp::ldmatrix4(q_addr + piece_at<T, D>(lane & 15, 2 * x + (lane >> 4)), qa[x]);
         }
 #pragma unroll
         for (int x = 0; x < D / 8; ++x)
@@ -92,12 +86,12 @@ struct Walk {
 #pragma unroll
         for (int x = 0; x < D / 16; ++x) {
             unsigned b[4], a[4];
-            ldmatrix4(kt + piece_at<T, D>(k_row, 2 * x + k_half), b[0], b[1], b[2], b[3]);
+            wp::ldmatrix4(kt + piece_at<T, D>(k_row, 2 * x + k_half), b);
             if constexpr (F::kQInRegs) {
 #pragma unroll
                 for (int y = 0; y < 4; ++y) a[y] = qa[x][y];
             } else {
-                ldmatrix4(q_addr + piece_at<T, D>(lane & 15, 2 * x + (lane >> 4)), a[0], a[1], a[2], a[3]);
+                wp::ldmatrix4(q_addr + piece_at<T, D>(lane & 15, 2 * x + (lane >> 4)), a);
             }
             wp::mma_bf16(sc[0], a[0], a[1], a[2], a[3], b[0], b[1]);
             wp::mma_bf16(sc[1], a[0], a[1], a[2], a[3], b[2], b[3]);
@@ -138,7 +132,7 @@ struct Walk {
 #pragma unroll
         for (int x = 0; x < D / 16; ++x) {
             unsigned b[4];
-            ldmatrix4_t(vt + piece_at<T, D>(v_row, 2 * x + v_half), b[0], b[1], b[2], b[3]);
+            wp::ldmatrix4_t(vt + piece_at<T, D>(v_row, 2 * x + v_half), b);
             wp::mma_bf16(o[2 * x], pa[0], pa[1], pa[2], pa[3], b[0], b[1]);
             wp::mma_bf16(o[2 * x + 1], pa[0], pa[1], pa[2], pa[3], b[2], b[3]);
         }
@@ -429,7 +423,7 @@ template <class T, int D>
 cudaError_t launch(Args &A, int n_sm, cudaStream_t st) {
     const int smem = (int)sizeof(Smem<T, D>);
     static DeviceFlags done;
-    cudaError_t e = allow_smem(decode_warp_kernel<T, D>, smem, done);
+    cudaError_t e = allow_smem_once(decode_warp_kernel<T, D>, smem, done);
     if (e != cudaSuccess) return e;
     const int most = Form<T, D>::kCtas * n_sm;
     if (A.grid > most) A.grid = most;

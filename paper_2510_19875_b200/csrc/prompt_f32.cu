@@ -45,11 +45,6 @@ __device__ __forceinline__ void split(float x, unsigned &hi, unsigned &lo) {
     asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(hi) : "f"(x));
     lo = __float_as_uint(x - __uint_as_float(hi));
 }
-__device__ __forceinline__ float4 load4_in_cluster(const float *own, unsigned cta) {
-    float4 x;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(wp::address_in_cluster(own, cta)) : "memory");
-    return x;
-}
 __device__ __forceinline__ void product(float (&c)[4], const unsigned (&ah)[4], const unsigned (&al)[4], unsigned bh0, unsigned bl0, unsigned bh1, unsigned bl1) {
     mma_tf32(c, al, bh0, bh1);  // (the small parts first)
     mma_tf32(c, ah, bl0, bl1);
@@ -260,7 +255,7 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_f32_kernel(const __grid_co
         for (int c = 0; c < 8; ++c)
             if (c < (int)ctas) {
                 const float f = fast_exp2(ms[c] - base);
-                const float4 y = load4_in_cluster(sm.q + r * F::kRow + x, (unsigned)c);
+                const float4 y = wp::load4_in_cluster(sm.q + r * F::kRow + x, (unsigned)c);
                 sum = fmaf(f, wp::load_in_cluster(&sm.l[r], (unsigned)c), sum);
                 w.x = fmaf(f, y.x, w.x); w.y = fmaf(f, y.y, w.y); w.z = fmaf(f, y.z, w.z); w.w = fmaf(f, y.w, w.w);
             }
@@ -278,7 +273,7 @@ template <int D>
 stream_status launch(const PromptGeom &g, const void *q, const void *k, const void *v, cudaStream_t st) {
     const int smem = (int)sizeof(Smem<D>);
     static DeviceFlags done;
-    cudaError_t e = allow_smem(prompt_f32_kernel<D>, smem, done);
+    cudaError_t e = allow_smem_once(prompt_f32_kernel<D>, smem, done);
     if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(prompt_f32)");
     const long long tiles = most_row_tiles(g, kRows);
     const int n_sm = current_sm_count();

@@ -1,4 +1,4 @@
-// Dense attention of packed prompts on fp32 FMA: fp32, and the bf16 shapes that the tensor-core kernels do not take.
+// Dense attention of packed prompts on fp32 FMA: fp32 with d = 256, and rows of either type that do not lie on 16 bytes.
 //
 // A CTA has 64 rows (token, query head) of one kv head, so that the query heads of a group share every key tile, and
 // walks the keys in tiles of 64 with the running maximum and sum of a softmax:
@@ -263,7 +263,7 @@ template <class T, int D>
 stream_status launch(const PromptGeom &g, const void *q, const void *k, const void *v, cudaStream_t st) {
     const int smem = (int)sizeof(Smem<D>);
     static DeviceFlags done;
-    cudaError_t e = allow_smem(prompt_kernel<T, D>, smem, done);
+    cudaError_t e = allow_smem_once(prompt_kernel<T, D>, smem, done);
     if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(prompt)");
     const long long tiles = most_row_tiles(g, kRows);
     const int n_sm = current_sm_count();

@@ -27,13 +27,6 @@ struct Smem {
     unsigned char k[2][kKeys * Form<D>::kRow], v[2][kKeys * Form<D>::kRow];
 };
 
-__device__ __forceinline__ void ldmatrix4(unsigned addr, unsigned (&r)[4]) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
-}
-__device__ __forceinline__ void ldmatrix4_t(unsigned addr, unsigned (&r)[4]) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
-}
-
 template <int D>
 __global__ void __launch_bounds__(kThreads, Form<D>::kCtas) prompt_mma_kernel(const __grid_constant__ PromptGeom g, const __nv_bfloat16 *q,
                                                                              const __nv_bfloat16 *k, const __nv_bfloat16 *v) {
@@ -97,7 +90,7 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas) prompt_mma_kernel(co
         __syncthreads();
         if (F::kQInRegs && j == 0) {
 #pragma unroll
-            for (int x = 0; x < D / 16; ++x) ldmatrix4(q_addr + x * 32, qa[F::kQInRegs ? x : 0]);
+            for (int x = 0; x < D / 16; ++x) wp::ldmatrix4(q_addr + x * 32, qa[F::kQInRegs ? x : 0]);
         }
         if (j < warp_most) {
             const unsigned kt = k_s + (unsigned)(buf * kKeys * F::kRow) + k_lane, vt = v_s + (unsigned)(buf * kKeys * F::kRow) + v_lane;
@@ -113,12 +106,12 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas) prompt_mma_kernel(co
 #pragma unroll
                     for (int y = 0; y < 4; ++y) a[y] = qa[x][y];
                 } else {
-                    ldmatrix4(q_addr + x * 32, a);
+                    wp::ldmatrix4(q_addr + x * 32, a);
                 }
 #pragma unroll
                 for (int n = 0; n < 4; ++n) {
                     unsigned b[4];
-                    ldmatrix4(kt + (unsigned)(n * 16 * F::kRow) + x * 32, b);
+                    wp::ldmatrix4(kt + (unsigned)(n * 16 * F::kRow) + x * 32, b);
                     wp::mma_bf16(sc[2 * n], a[0], a[1], a[2], a[3], b[0], b[1]);
                     wp::mma_bf16(sc[2 * n + 1], a[0], a[1], a[2], a[3], b[2], b[3]);
                 }
@@ -164,7 +157,7 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas) prompt_mma_kernel(co
 #pragma unroll
                 for (int x = 0; x < D / 16; ++x) {
                     unsigned b[4];
-                    ldmatrix4_t(vt + (unsigned)(n * 16 * F::kRow) + x * 32, b);
+                    wp::ldmatrix4_t(vt + (unsigned)(n * 16 * F::kRow) + x * 32, b);
                     wp::mma_bf16(o[2 * x], pa[0], pa[1], pa[2], pa[3], b[0], b[1]);
                     wp::mma_bf16(o[2 * x + 1], pa[0], pa[1], pa[2], pa[3], b[2], b[3]);
                 }
@@ -206,7 +199,7 @@ template <int D>
 stream_status launch(const PromptGeom &g, const void *q, const void *k, const void *v, cudaStream_t st) {
     const int smem = (int)sizeof(Smem<D>);
     static DeviceFlags done;
-    cudaError_t e = allow_smem(prompt_mma_kernel<D>, smem, done);
+    cudaError_t e = allow_smem_once(prompt_mma_kernel<D>, smem, done);
     if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(prompt_mma)");
     const long long tiles = most_row_tiles(g, kRows);
     if (tiles > 0x7fffffffLL) { set_error("too many rows for one launch"); return STREAM_ERR_UNSUPPORTED; }
@@ -217,7 +210,7 @@ stream_status launch(const PromptGeom &g, const void *q, const void *k, const vo
 }  // namespace
 
 bool prompt_mma_supported(const PromptGeom &g, int dtype, const void *q, const void *k, const void *v) {
-    if (dtype != STREAM_BF16 || g.total_k > 0x7fffff00) return false;  // (a tile's end is counted in 32 bits)
+    if (dtype != STREAM_BF16) return false;
     return (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)g.out) & 15) == 0 && ((g.qs_t | g.qs_h | g.ks_t | g.ks_h) & 7) == 0;
 }
 

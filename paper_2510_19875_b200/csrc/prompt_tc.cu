@@ -588,7 +588,7 @@ stream_status launch(const PromptGeom &g, const void *q, const void *k, const vo
     const int smem = (2 + F::kStages) * F::kTile + (int)sizeof(Tail<F>) + 1024;
     static_assert((2 + F::kStages) * F::kTile + (int)sizeof(Tail<F>) + 1024 <= 232448, "what a CTA may have");
     static DeviceFlags done;
-    cudaError_t e = allow_smem(prompt_tc_kernel<F>, smem, done);
+    cudaError_t e = allow_smem_once(prompt_tc_kernel<F>, smem, done);
     if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(prompt_tc)");
     const int n_sm = current_sm_count();
     if (n_sm <= 0) { set_error("cannot read the SM count of the current device"); return STREAM_ERR_CUDA; }
@@ -607,7 +607,6 @@ stream_status launch(const PromptGeom &g, const void *q, const void *k, const vo
 
 bool prompt_tc_supported(const PromptGeom &g, int dtype, const void *q, const void *k, const void *v) {
     if (dtype != STREAM_BF16 || (g.d != 64 && g.d != 128) || g.hpg > kRows || g.total_k < 1) return false;
-    if (g.total_q > 0x7fffff00 || g.total_k > 0x7fffff00) return false;  // (a tile's last row is a coordinate too)
     if ((((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)g.out) & 15) != 0 || ((g.qs_t | g.qs_h | g.ks_t | g.ks_h) & 7) != 0) return false;
     return ((long long)g.total_q / (2 * (kRows / g.hpg)) + g.n_seqs) * g.G <= kMaxItems;
 }

@@ -98,10 +98,10 @@ inline int current_sm_count() {
     if (dev < kMaxDevices) known[dev].store(n, std::memory_order_relaxed);
     return n;
 }
-// Dynamic shared memory of a kernel beyond 48 KB; `done`: of that kernel.
+// Dynamic shared memory of a kernel beyond 48 KB, asked for once a device; `done`: of that kernel.
 typedef std::atomic<unsigned long long> DeviceFlags;
 template <class... K>
-cudaError_t allow_smem(void (*kern)(K...), int bytes, DeviceFlags &done) {
+cudaError_t allow_smem_once(void (*kern)(K...), int bytes, DeviceFlags &done) {
     const int dev = current_device();
     const unsigned long long bit = dev >= 0 && dev < kMaxDevices ? 1ull << dev : 0ull;
     if ((done.load(std::memory_order_relaxed) & bit) != 0) return cudaSuccess;
