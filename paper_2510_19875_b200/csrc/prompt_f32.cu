@@ -22,8 +22,9 @@ constexpr float kOutgrown = 30.f;  // log2
 
 template <int D>
 struct Form {
-    // Of a tile: half the code of 64 (the first pass through it, from cold instruction caches, takes 5 us), and no spills: us, one head of 2048
-    // tokens, d = 64, 28.4 -> 26.8; 25 prompts of up to 45, 16 heads, 18.6 -> 15.8. Two CTAs an SM.
+    // Of a tile: half the code of 64 (the first pass through it, from cold instruction caches, takes 5 us). us with 64 and with 32, d = 64: one head of
+    // 2048 tokens 27.0, 26.6; 25 prompts of up to 45, 16 heads, 20.0, 16.4; eight heads of 8192 1314, 1350. d = 128: eight heads of 4096 1062, 744 (with 64 the
+    // registers do not do; with 32 eight bytes are spilled). Two CTAs an SM.
     static constexpr int kKeys = D >= 64 ? 32 : 64;
     static constexpr int kRow = D + 16;               // floats of a row of Q and K: eight lanes, two rows of four pieces, touch every bank
     static constexpr int kVRow = D + 4;               // of V: four pairs of rows, two pieces

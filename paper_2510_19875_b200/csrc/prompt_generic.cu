@@ -5,7 +5,8 @@
 //     m' = max(m, max_j s_j),   l' = l 2^(m - m') + sum_j 2^(s_j - m'),   O' = O 2^(m - m') + sum_j 2^(s_j - m') v_j,
 // logits in units of log2. A thread holds 4 x 4 logits and 4 rows x d / 16 channels of O. Where the row tiles are fewer than
 // the SMs, a cluster of up to eight CTAs has the tile: each walks every n-th key tile, and their m, l and O meet
-// through shared memory, in a fixed order, every CTA joining its share of the rows.
+// through shared memory, in a fixed order, every CTA joining its share of the rows. 2048 tokens: fp32, 8 heads, d = 256 498 us (34.5 TFLOP/s); off 16 bytes, 8 heads of fp32,
+// d = 64, 253 us (17.0), 32 / 8 heads of bf16, d = 128, 1298 us (26.5).
 #include "serve_common.cuh"
 #include "warp_common.cuh"
 

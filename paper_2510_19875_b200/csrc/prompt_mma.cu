@@ -5,7 +5,8 @@
 // sequence's last key. A warp's logits stay in registers, turn into bf16 weights 2^(scale (s - ref)) there and are the A operand
 // of the product with V as they lie. `ref` is a row's maximum at its first tile, moved (O and the sum with it) only when a logit has
 // outgrown it by 2^30; the sum is that of the unrounded weights. Late tokens, with the most keys, come first. Bound by the
-// latency of dependent steps at eight to sixteen warps an SM.
+// latency of dependent steps at eight to sixteen warps an SM: 32 / 8 heads, 4096 tokens, d = 256 920 us (299 TFLOP/s), d = 32 175 us (196); 597 tokens, d = 256, 46.5 us
+// (126: 152 CTAs for 148 SMs).
 #include "serve_common.cuh"
 #include "warp_common.cuh"
 

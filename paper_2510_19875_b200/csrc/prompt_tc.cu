@@ -38,7 +38,7 @@ constexpr int kMaxSeqs = 256;            // of a launch
 constexpr int kMaxLevels = 2048;         // items of a kv head that are put in order
 constexpr long long kMaxItems = 0x7fffffffll - (1 << 20);
 constexpr float kOutgrown = 30.f;        // log2
-// K and V bytes of the kv heads whose items are walked together, of the 126 MB of L2 (32 / 8 heads, TFLOP/s: 131072 tokens, all heads
+// K and V bytes of the kv heads whose items are walked together, of the 126 MB of L2; of this kernel, which reads every key tile (the sparse passes have kL2KvBytes) (32 / 8 heads, TFLOP/s: 131072 tokens, all heads
 // 1094 to 1117, one at a time 1202 to 1217; 65536, all 1196 to 1219, two 1193 to 1207, three 1250 to 1268; 16384 in halves 1285 for 1372).
 constexpr long long kKvInL2 = 110ll << 20;
 
@@ -520,8 +520,9 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
     const unsigned tmem = tl->tmem_base;
     // Items in the order of their key tiles, over all sequences (in the sequences' order the last CTA was 9 % behind the mean: 12 prompts of up to 4500
     // tokens; in this one 2 %). An item's place is how many stand in front of it, which each sequence says in closed form. Not where every
-    // item has a CTA of its own, nor where there is too much to count (16 terms a thread take 2 us): the items are many and
-    // small against a CTA's sum then.
+    // item has a CTA of its own, nor where there is too much to count (16 terms a thread take 2 us): the items are many and small against
+    // a CTA's sum then, and counting costs more than order gives (us as the sequences lie, and put in order all the same, 28 / 4 heads: 64 prompts of 500 tokens
+    // 222, 273; of 100 to 900 311, 351; of 50 to 2000 337, 361; 32 / 8 heads 234, 259; 304, 315; 361, 363).
     const int n_levels = tl->n_levels;
     const bool sorted = g.n_seqs > 1 && tl->n_items > (int)gridDim.x && n_levels <= kMaxLevels && n_levels * g.n_seqs <= 16 * kThreads;
     if (tid == 0) tl->sorted = sorted ? 1 : 0;
