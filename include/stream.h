@@ -531,6 +531,81 @@ stream_status stream_decode_attention(const stream_cache *c, int32_t layer, int3
                                       const int32_t *seq_len, float scale, void *out, float *lse_out, void *workspace,
                                       size_t workspace_bytes, void *cuda_stream);
 
+/*
+ * The keys and values of slots read back as packed rows: what stream_prompt_attention needs of a prompt that comes in pieces. The rows cu[s] ..
+ * cu[s+1] - 1 of k_out and v_out become the last tokens of slot s, up to seq_len[s] - 1 (all of them where there are as many
+ * rows as tokens). Rows of no slot stay as they are; tokens whose position or page cannot be are zeros.
+ *   cu              device int32 [n_slots + 1], ascending, clamped like cu_q
+ *   k_out, v_out    device, dtype of the cache, contiguous [total, n_kv_heads, d]
+ */
+stream_status stream_cache_read(const stream_cache *c, int32_t layer, const void *k_pages, const void *v_pages, const int32_t *cu,
+                                int64_t total, const int32_t *page_table, const int32_t *seq_len, void *k_out, void *v_out, void *cuda_stream);
+
+/*
+ * Attention with a sliding window and sinks: a query at position p of its sequence sees the keys j <= p with j > p - window or j < sinks, that
+ * is the last `window` keys, its own among them, and the first `sinks` ones. (The fixed pattern that a searched mask is set against, and
+ * what models do whose layers look back only so far.) window >= 1, sinks >= 0, and both may be larger than any sequence.
+ *
+ * stream_prompt_window_attention: as stream_prompt_attention with causal = 1 (else INVALID_ARG); query i of a sequence with n queries and m keys
+ * is at position i + m - n. Keys that no query of a sequence sees are not read, but for those that share a tile with others.
+ *
+ * stream_decode_window_attention: as stream_decode_attention; a slot's query is at position seq_len[s] - 1. Pages all of whose tokens lie
+ * between the sinks and the window are not read, and their entries of the table may be anything.
+ */
+stream_status stream_prompt_window_attention(const stream_prompt *p, int32_t window, int32_t sinks, const void *q, const void *k,
+                                             const void *v, const int32_t *cu_q, const int32_t *cu_k, float scale, void *out,
+                                             float *lse_out, void *cuda_stream);
+stream_status stream_decode_window_attention(const stream_cache *c, int32_t layer, int32_t n_q_heads, int32_t window, int32_t sinks,
+                                             const void *q, int64_t q_stride_s, int64_t q_stride_h, const void *k_pages,
+                                             const void *v_pages, const int32_t *page_table, const int32_t *seq_len, float scale,
+                                             void *out, float *lse_out, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * A paged cache in 8 bits: K and V are e4m3 (sign, four bits of exponent, three of mantissa; up to 448), and the tokens of a block, in one kv
+ * head, share a scale: a key is its e4m3 numbers times its block's scale. The scales of K and V are each float32 [n_layers, n_pages,
+ * page_size / block, n_kv_heads] with the strides below. The ledger is that of any cache: its calls take &c->cache.
+ *
+ * A block's scale is the smallest power of two 2^e, -90 <= e <= 120, of which no element is more than 448 times: e4m3's relative precision, 2^-4 at most, does
+ * not depend on a scale, powers of two make the division exact, and what is rounded again when a block's scale grows stays
+ * what it was, but for elements below 2^-6 of the new scale. */
+typedef struct {
+    stream_cache cache;     /* dtype: of queries, outputs and new keys and values; strides: of the e4m3 arrays, in elements (bytes) */
+    int32_t block;          /* tokens that share a scale; divides page_size */
+    int32_t reserved;       /* 0 */
+    int64_t scale_stride_l, scale_stride_p, scale_stride_b, scale_stride_h; /* layer, page, block, head; elements; one whose extent is 1 does not matter */
+} stream_cache8;
+
+/*
+ * stream_cache_write for a cache in 8 bits. A block whose first token is among the new ones gets a scale for its new tokens. One that
+ * has tokens in front of them keeps its scale or takes the one that the new tokens ask for, whichever is larger; where it grows, those
+ * tokens are rounded again: rn(x old / new). The sum of a block's roundings is so at most a step of its last scale. Infinities become +-448
+ * scales, with e = 120; NaN stays NaN and asks for no scale. Everything else as stream_cache_write.
+ *   k_scale, v_scale  the scales' first elements (layer 0); written: layer `layer`
+ */
+stream_status stream_cache8_write(const stream_cache8 *c, int32_t layer, const void *k, const void *v, int64_t total, int64_t stride_t,
+                                  int64_t stride_h, const int32_t *cu_new, const int32_t *page_table, const int32_t *seq_len,
+                                  const int32_t *done, void *k_pages, void *v_pages, float *k_scale, float *v_scale, void *cuda_stream);
+
+/* stream_cache_read for a cache in 8 bits: the rows of k_out and v_out, of dtype c->cache.dtype, are e4m3 numbers times their scales. */
+stream_status stream_cache8_read(const stream_cache8 *c, int32_t layer, const void *k_pages, const void *v_pages, const float *k_scale,
+                                 const float *v_scale, const int32_t *cu, int64_t total, const int32_t *page_table, const int32_t *seq_len,
+                                 void *k_out, void *v_out, void *cuda_stream);
+
+/* stream_cache_copy_pages for a cache in 8 bits: pages and their scales. */
+stream_status stream_cache8_copy_pages(const stream_cache8 *c, void *k_pages, void *v_pages, float *k_scale, float *v_scale,
+                                       const int32_t *pairs, const int32_t *count, int32_t n_pairs, void *cuda_stream);
+
+/*
+ * stream_decode_attention over a cache in 8 bits, with a window and sinks where window > 0 (stream_decode_window_attention; 0: every key is
+ * seen, whatever sinks says). Any scales of 2^-100 to 2^100 will do, powers of two or not; a token whose key scale is 0 counts as not there. Products are those of
+ * e4m3 numbers, which fp16 holds, with queries and weights in fp16 (bf16 caches: 2^-11 of a weight; fp32 ones: two fp16 numbers each, 2^-22). Everything
+ * else, the workspace too (stream_decode_workspace_bytes of &c->cache), as stream_decode_attention.
+ */
+stream_status stream_decode_attention8(const stream_cache8 *c, int32_t layer, int32_t n_q_heads, int32_t window, int32_t sinks,
+                                       const void *q, int64_t q_stride_s, int64_t q_stride_h, const void *k_pages, const void *v_pages,
+                                       const float *k_scale, const float *v_scale, const int32_t *page_table, const int32_t *seq_len,
+                                       float scale, void *out, float *lse_out, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,275 @@
+// A paged cache in 8 bits: new tokens rounded into their pages, and tokens read back.
+//
+// A block's scale is the smallest power of two 2^e with amax <= 448 2^e, which the exponent and the fraction of amax say, so that x 2^-e is exact and
+// one rounding, to e4m3, is all there is. A group of threads has a block of one kv head's keys or values: their largest
+// element, the block's scale, the numbers. Which blocks have new tokens nobody has to count: n tokens touch n / block + 2 blocks at most, so that
+// slot s has the places cu[s] / block + 2 s and those behind it, up to the next slot's, and some of them stay empty. Both kernels move every
+// byte once (a new token's twice where a block is more than the group's registers hold) and are bound by HBM or, for few tokens, by the chain of
+// loads: offsets, lengths, page, tokens.
+#include <cuda_fp8.h>
+
+#include "serve_common.cuh"
+#include "warp_common.cuh"
+
+namespace stream {
+namespace {
+
+constexpr int kThreads = 128;
+constexpr int kCtas = 64;   // an SM of a grid, at most
+constexpr int kHold = 8;    // pieces that a thread holds
+constexpr int kMinExp = -90, kMaxExp = 120;
+
+// The exponent e of the scale for elements up to amax.
+__device__ __forceinline__ int scale_exp(float amax) {
+    const unsigned b = __float_as_uint(amax);
+    const int e = (int)(b >> 23) - 127 - 8 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0);  // 448 = 1.75 2^8
+    return min(max(e, kMinExp), kMaxExp);
+}
+__device__ __forceinline__ float two_to(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }
+
+// Eight elements.
+template <class T>
+__device__ __forceinline__ void load_piece(const T *p, bool vec, float (&x)[8]) {
+    if (!vec) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = to_float(p[i]);
+    } else if constexpr (sizeof(T) == 4) {
+        const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
+        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+    } else {
+        const uint4 a = *reinterpret_cast<const uint4 *>(p);
+        const unsigned w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+    }
+}
+__device__ __forceinline__ uint2 round8(const float (&x)[8], float f) {
+    unsigned w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __nv_cvt_float2_to_fp8x2(make_float2(x[2 * i] * f, x[2 * i + 1] * f), __NV_SATFINITE, __NV_E4M3);
+    return make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
+}
+__device__ __forceinline__ float2 widen8(unsigned two) {
+    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3);
+    return __half22float2(*reinterpret_cast<const __half2 *>(&h));
+}
+__device__ __forceinline__ void store8(unsigned char *p, uint2 w, bool vec) {
+    if (vec) {
+        *reinterpret_cast<uint2 *>(p) = w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = (unsigned char)((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
+    }
+}
+__device__ __forceinline__ uint2 load8(const unsigned char *p, bool vec) {
+    if (vec) return *reinterpret_cast<const uint2 *>(p);
+    uint2 w = make_uint2(0, 0);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) (i < 4 ? w.x : w.y) |= (unsigned)p[i] << (8 * (i & 3));
+    return w;
+}
+
+struct WriteArgs {
+    CacheGeom c;             // strides: elements of the pages, which are bytes
+    Scales sc;
+    const void *x[2];        // K, V
+    unsigned char *pages[2];
+    const int32_t *cu, *done;
+    int total;
+    long long s_t, s_h;      // elements, of x
+    int vec_in, vec_out;
+    long long places;        // of blocks
+};
+
+// Place of the first block of slot s.
+__device__ __forceinline__ long long place_of(const WriteArgs &a, int s) { return min(max(a.cu[s], 0), a.total) / a.sc.block + 2ll * s; }
+
+// kGroup threads a block: 32, or all of the CTA's.
+template <class T, int kGroup>
+__global__ void __launch_bounds__(kThreads) write8_kernel(const __grid_constant__ WriteArgs a) {
+    __shared__ float tops[kThreads / 32];
+    after_previous_kernel();
+    const CacheGeom &c = a.c;
+    if (a.done != nullptr && *a.done == 0) return;
+    constexpr int kGroups = kThreads / kGroup;
+    const int lane = threadIdx.x & 31, me = threadIdx.x % kGroup, row_pieces = c.d / 8, block = a.sc.block;
+    const long long items = a.places * c.G * 2;
+    for (long long it = (long long)blockIdx.x * kGroups + threadIdx.x / kGroup; it < items; it += (long long)gridDim.x * kGroups) {
+        const int kv = (int)(it & 1), h = (int)((it >> 1) % c.G);
+        const long long place = (it >> 1) / c.G;
+        int s = 0;
+        for (int hi = c.n_slots; hi - s > 1;) {  // the last slot that begins at or before the place (32 candidates a step)
+            const int step = (hi - s + 31) / 32;
+            const long long at = s + (long long)lane * step;
+            const unsigned below = __ballot_sync(0xffffffffu, at < hi && place_of(a, (int)min(at, (long long)c.n_slots - 1)) <= place);
+            s += (below != 0 ? 31 - __clz(below) : 0) * step;
+            hi = min(hi, s + step);
+        }
+        const Span sp = span_of(a.cu, s, a.total);
+        const int len = tokens_of(c, s), start = max(len - sp.n, 0);  // the first new token (rows in front of the slot's first token are passed over)
+        const long long nth = place - place_of(a, s), lo64 = (start / block + nth) * block;
+        if (nth < 0 || lo64 >= len || sp.n == 0) continue;  // (the whole group)
+        const int lo = (int)lo64, hi = min(len, lo + block), first = max(lo, start);
+        const int page = c.table[(long long)s * c.max_pages + lo / c.page];
+        if ((unsigned)page >= (unsigned)c.n_pages) continue;
+        float *const scale_at = const_cast<float *>(kv ? a.sc.v : a.sc.k) + page * a.sc.s_p + (lo % c.page / block) * a.sc.s_b + h * a.sc.s_h;
+        unsigned char *const to = a.pages[kv] + page * c.s_p + (long long)(lo % c.page) * c.s_t + h * c.s_h;
+        const T *const from = (const T *)a.x[kv] + (long long)(sp.first + sp.n - (len - first)) * a.s_t + h * a.s_h;
+        const int n = (hi - first) * row_pieces;
+        const bool held = n <= kGroup * kHold;
+        const float had = first > lo ? *scale_at : 0.f;
+        float x[kHold][8], top = 0.f;
+        for (int p0 = 0; p0 < n; p0 += kGroup * kHold) {
+#pragma unroll
+            for (int i = 0; i < kHold; ++i) {
+                const int p = p0 + i * kGroup + me;
+                if (p < n) {
+                    load_piece(from + (long long)(p / row_pieces) * a.s_t + (p % row_pieces) * 8, a.vec_in != 0, x[i]);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[i][e]));
+                }
+            }
+        }
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+        if constexpr (kGroup > 32) {
+            __syncthreads();  // (the block before has been read)
+            if (lane == 0) tops[threadIdx.x >> 5] = top;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < kThreads / 32; ++w) top = fmaxf(top, tops[w]);
+        }
+        __syncwarp();  // (every lane has read the scale)
+        const float asked = two_to(scale_exp(top)), scale = had > asked && had < CUDART_INF_F ? had : asked, inv = 1.f / scale;
+        if (me == 0 && scale != had) *scale_at = scale;
+        if (first > lo && had != scale) {  // what the block has, rounded again
+            const float f = had / scale;
+            for (int p = me; p < (first - lo) * row_pieces; p += kGroup) {
+                unsigned char *const at = to + (long long)(p / row_pieces) * c.s_t + (p % row_pieces) * 8;
+                const uint2 w = load8(at, a.vec_out != 0);
+                float y[8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 z = widen8((i < 2 ? w.x : w.y) >> (16 * (i & 1)) & 0xffffu);
+                    y[2 * i] = z.x;
+                    y[2 * i + 1] = z.y;
+                }
+                store8(at, round8(y, f), a.vec_out != 0);
+            }
+        }
+        unsigned char *const dst = to + (long long)(first - lo) * c.s_t;
+        for (int p0 = 0; p0 < n; p0 += kGroup * kHold) {
+#pragma unroll
+            for (int i = 0; i < kHold; ++i) {
+                const int p = p0 + i * kGroup + me;
+                if (p < n) {
+                    if (!held) load_piece(from + (long long)(p / row_pieces) * a.s_t + (p % row_pieces) * 8, a.vec_in != 0, x[i]);
+                    store8(dst + (long long)(p / row_pieces) * c.s_t + (p % row_pieces) * 8, round8(x[i], inv), a.vec_out != 0);
+                }
+            }
+        }
+    }
+}
+
+struct ReadArgs {
+    CacheGeom c;
+    Scales sc;
+    const unsigned char *pages[2];
+    void *x[2];
+    const int32_t *cu;
+    int total;
+};
+
+// A warp a token; kPiece elements at a time: 16, or one where a row or an output is off 16 bytes.
+template <class T, int kPiece>
+__global__ void __launch_bounds__(kThreads) read8_kernel(const __grid_constant__ ReadArgs a) {
+    after_previous_kernel();
+    const CacheGeom &c = a.c;
+    const int lane = threadIdx.x & 31, row_pieces = c.d / kPiece;
+    for (long long t = (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); t < a.total; t += (long long)gridDim.x * (kThreads / 32)) {
+        const int s = slot_of_row(a.cu, c.n_slots, t, lane);
+        const Span sp = span_of(a.cu, s, a.total);
+        if (t < sp.first || t >= (long long)sp.first + sp.n) continue;
+        const long long pos = (long long)tokens_of(c, s) - sp.n + (t - sp.first);
+        const int page = pos >= 0 ? c.table[(long long)s * c.max_pages + (int)pos / c.page] : -1;
+        const bool there = (unsigned)page < (unsigned)c.n_pages;
+        const int in_page = there ? (int)pos % c.page : 0;
+        const long long from = there ? page * c.s_p + in_page * c.s_t : 0, z = there ? page * a.sc.s_p + in_page / a.sc.block * a.sc.s_b : 0;
+        for (int u = lane; u < c.G * row_pieces; u += 32) {
+            const int h = u / row_pieces, x = (u - h * row_pieces) * kPiece;
+            uint4 w[2] = {};
+            float scale[2] = {0.f, 0.f};
+            if (there) {
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv) {
+                    const unsigned char *const at = a.pages[kv] + from + h * c.s_h + x;
+                    if constexpr (kPiece == 16) w[kv] = *reinterpret_cast<const uint4 *>(at);
+                    else w[kv].x = *at;
+                    scale[kv] = (kv ? a.sc.v : a.sc.k)[z + h * a.sc.s_h];
+                }
+            }
+#pragma unroll
+            for (int kv = 0; kv < 2; ++kv) {
+                T *const to = (T *)a.x[kv] + (t * c.G + h) * c.d + x;
+                const unsigned v[4] = {w[kv].x, w[kv].y, w[kv].z, w[kv].w};
+                if constexpr (kPiece == 1) {
+                    to[0] = (T)(widen8(v[0]).x * scale[kv]);
+                } else {
+                    __align__(16) T y[16];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float2 f = widen8(v[i >> 1] >> (16 * (i & 1)) & 0xffffu);
+                        y[2 * i] = (T)(f.x * scale[kv]);
+                        y[2 * i + 1] = (T)(f.y * scale[kv]);
+                    }
+#pragma unroll
+                    for (int i = 0; i < (int)sizeof(T); ++i) reinterpret_cast<uint4 *>(to)[i] = reinterpret_cast<const uint4 *>(y)[i];
+                }
+            }
+        }
+    }
+}
+
+bool on(long long bytes, const void *p, const void *q) { return (((uintptr_t)p | (uintptr_t)q) & (uintptr_t)(bytes - 1)) == 0; }
+
+}  // namespace
+
+stream_status launch_write8(const CacheGeom &c, const Scales &sc, int dtype, const void *k, const void *v, int total, long long s_t, long long s_h,
+                            const int32_t *cu_new, const int32_t *done, void *k_pages, void *v_pages, cudaStream_t st) {
+    const int e = dtype == STREAM_F32 ? 4 : 2;
+    WriteArgs a = {};
+    a.c = c; a.sc = sc; a.x[0] = k; a.x[1] = v; a.pages[0] = (unsigned char *)k_pages; a.pages[1] = (unsigned char *)v_pages;
+    a.cu = cu_new; a.done = done; a.total = total; a.s_t = s_t; a.s_h = s_h;
+    a.vec_in = on(16, k, v) && ((s_t | s_h) * e & 15) == 0;
+    a.vec_out = on(8, k_pages, v_pages) && ((c.s_p | c.s_t | c.s_h) & 7) == 0;
+    a.places = total / sc.block + 2ll * c.n_slots;
+    const int n_sm = current_sm_count();
+    if (n_sm <= 0) { set_error("cannot read the SM count of the current device"); return STREAM_ERR_CUDA; }
+    // a warp a block where a block's new tokens fit its registers (few tokens a slot, or small blocks), else a CTA
+    const long long per_slot = ((long long)total + c.n_slots - 1) / c.n_slots, rows = per_slot < sc.block ? per_slot : sc.block;
+    const bool warp = rows * (c.d / 8) <= 32 * kHold;
+    const long long items = a.places * c.G * 2, ctas = warp ? (items + 3) / 4 : items, most = (long long)n_sm * kCtas;
+    const unsigned grid = (unsigned)(ctas < most ? ctas : most);
+    cudaError_t rc;
+    if (dtype == STREAM_F32) rc = warp ? launch_early(write8_kernel<float, 32>, grid, kThreads, 0, st, a) : launch_early(write8_kernel<float, kThreads>, grid, kThreads, 0, st, a);
+    else rc = warp ? launch_early(write8_kernel<__nv_bfloat16, 32>, grid, kThreads, 0, st, a) : launch_early(write8_kernel<__nv_bfloat16, kThreads>, grid, kThreads, 0, st, a);
+    return rc == cudaSuccess ? STREAM_OK : cuda_fail(rc, "8-bit cache write launch");
+}
+
+stream_status launch_read8(const CacheGeom &c, const Scales &sc, int dtype, const void *k_pages, const void *v_pages, const int32_t *cu, int total,
+                           void *k_out, void *v_out, cudaStream_t st) {
+    ReadArgs a = {};
+    a.c = c; a.sc = sc; a.pages[0] = (const unsigned char *)k_pages; a.pages[1] = (const unsigned char *)v_pages; a.x[0] = k_out; a.x[1] = v_out;
+    a.cu = cu; a.total = total;
+    const bool vec = on(16, k_pages, v_pages) && on(16, k_out, v_out) && ((c.s_p | c.s_t | c.s_h) & 15) == 0;
+    const int n_sm = current_sm_count();
+    if (n_sm <= 0) { set_error("cannot read the SM count of the current device"); return STREAM_ERR_CUDA; }
+    const long long ctas = ((long long)total + kThreads / 32 - 1) / (kThreads / 32), most = (long long)n_sm * kCtas;
+    const unsigned grid = (unsigned)(ctas < most ? ctas : most);
+    cudaError_t rc;
+    if (dtype == STREAM_F32) rc = vec ? launch_early(read8_kernel<float, 16>, grid, kThreads, 0, st, a) : launch_early(read8_kernel<float, 1>, grid, kThreads, 0, st, a);
+    else rc = vec ? launch_early(read8_kernel<__nv_bfloat16, 16>, grid, kThreads, 0, st, a) : launch_early(read8_kernel<__nv_bfloat16, 1>, grid, kThreads, 0, st, a);
+    return rc == cudaSuccess ? STREAM_OK : cuda_fail(rc, "8-bit cache read launch");
+}
+
+}  // namespace stream

@@ -79,16 +79,7 @@ __global__ void __launch_bounds__(kThreads) write_kernel(const __grid_constant__
     if (a.done != nullptr && *a.done == 0) return;
     const int lane = threadIdx.x & 31;
     for (long long t = (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); t < a.total; t += (long long)gridDim.x * (kThreads / 32)) {
-        // the slot whose rows hold t: the last one that begins at or before it (32 candidates a step)
-        int lo = 0, hi = c.n_slots;
-        while (hi - lo > 1) {
-            const int step = (hi - lo + 31) / 32;
-            const long long at = lo + (long long)lane * step;
-            const unsigned below = __ballot_sync(0xffffffffu, at < hi && a.cu[at] <= t);
-            const int last = below != 0 ? 31 - __clz(below) : 0;
-            lo += last * step;
-            hi = min(hi, lo + step);
-        }
+        const int lo = slot_of_row(a.cu, c.n_slots, t, lane);
         const Span sp = span_of(a.cu, lo, a.total);
         const int len = tokens_of(c, lo);
         const long long pos = (long long)len - sp.n + (t - sp.first);
@@ -106,7 +97,44 @@ __global__ void __launch_bounds__(kThreads) write_kernel(const __grid_constant__
     }
 }
 
-// The widest unit that all of these are multiples of: 16, 8, 4 or 2 bytes.
+// The way back: packed rows out of the pages, zeros where there is no page.
+struct ReadArgs {
+    CacheGeom c;
+    const char *k_pages, *v_pages;
+    char *k, *v;
+    const int32_t *cu;
+    int total, elem;
+    int run, per_token;          // as in WriteArgs
+};
+
+template <class Unit>
+__global__ void __launch_bounds__(kThreads) read_kernel(const __grid_constant__ ReadArgs a) {
+    after_previous_kernel();
+    const CacheGeom &c = a.c;
+    const int lane = threadIdx.x & 31;
+    for (long long t = (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); t < a.total; t += (long long)gridDim.x * (kThreads / 32)) {
+        const int s = slot_of_row(a.cu, c.n_slots, t, lane);
+        const Span sp = span_of(a.cu, s, a.total);
+        if (t < sp.first || t >= (long long)sp.first + sp.n) continue;
+        const long long pos = (long long)tokens_of(c, s) - sp.n + (t - sp.first);
+        const int page = pos >= 0 ? c.table[(long long)s * c.max_pages + (int)pos / c.page] : -1;
+        const bool there = (unsigned)page < (unsigned)c.n_pages;
+        const long long from = there ? (page * c.s_p + ((int)pos % c.page) * c.s_t) * a.elem : 0, to = t * a.per_token * (long long)sizeof(Unit);
+        for (int u = lane; u < a.per_token; u += 32) {
+            const int h = u / a.run;
+            const long long x = h * c.s_h * a.elem + (long long)(u - h * a.run) * (int)sizeof(Unit);
+            Unit k = {}, v = {};
+            if (there) {
+                k = *reinterpret_cast<const Unit *>(a.k_pages + from + x);
+                v = *reinterpret_cast<const Unit *>(a.v_pages + from + x);
+            }
+            *reinterpret_cast<Unit *>(a.k + to + u * (long long)sizeof(Unit)) = k;
+            *reinterpret_cast<Unit *>(a.v + to + u * (long long)sizeof(Unit)) = v;
+        }
+    }
+}
+
+// The widest unit that all of these are multiples of: 16, 8, 4, 2 bytes or one.
 int unit_of(std::initializer_list<long long> bytes) {
     unsigned long long any = 16;
     for (long long b : bytes) any |= (unsigned long long)b;
@@ -114,8 +142,8 @@ int unit_of(std::initializer_list<long long> bytes) {
 }
 
 template <class A>
-cudaError_t launch_unit(int unit, void (*k16)(A), void (*k8)(A), void (*k4)(A), void (*k2)(A), unsigned grid, cudaStream_t st, const A &a) {
-    return launch_early(unit == 16 ? k16 : unit == 8 ? k8 : unit == 4 ? k4 : k2, grid, kThreads, 0, st, a);
+cudaError_t launch_unit(int unit, void (*k16)(A), void (*k8)(A), void (*k4)(A), void (*k2)(A), unsigned grid, cudaStream_t st, const A &a, void (*k1)(A) = nullptr) {
+    return launch_early(unit == 16 ? k16 : unit == 8 ? k8 : unit == 4 ? k4 : unit == 2 ? k2 : k1, grid, kThreads, 0, st, a);
 }
 
 }  // namespace
@@ -141,8 +169,8 @@ stream_status launch_copy_pages(const CacheGeom &c, int elem, void *k, void *v, 
     const long long items = (long long)n_pairs * c.n_layers * 2 * a.pieces, most = (long long)n_sm * kCtas;
     const unsigned grid = (unsigned)(items < most ? items : most);
     const cudaError_t e = n_in == 1 && n_out == 1
-        ? launch_unit<CopyArgs>(unit, copy_pages_kernel<uint4, true>, copy_pages_kernel<uint2, true>, copy_pages_kernel<unsigned, true>, copy_pages_kernel<unsigned short, true>, grid, st, a)
-        : launch_unit<CopyArgs>(unit, copy_pages_kernel<uint4, false>, copy_pages_kernel<uint2, false>, copy_pages_kernel<unsigned, false>, copy_pages_kernel<unsigned short, false>, grid, st, a);
+        ? launch_unit<CopyArgs>(unit, copy_pages_kernel<uint4, true>, copy_pages_kernel<uint2, true>, copy_pages_kernel<unsigned, true>, copy_pages_kernel<unsigned short, true>, grid, st, a, copy_pages_kernel<unsigned char, true>)
+        : launch_unit<CopyArgs>(unit, copy_pages_kernel<uint4, false>, copy_pages_kernel<uint2, false>, copy_pages_kernel<unsigned, false>, copy_pages_kernel<unsigned short, false>, grid, st, a, copy_pages_kernel<unsigned char, false>);
     return e == cudaSuccess ? STREAM_OK : cuda_fail(e, "cache copy launch");
 }
 
@@ -163,6 +191,23 @@ stream_status launch_write(const CacheGeom &c, int elem, const void *k, const vo
     const cudaError_t e = launch_unit<WriteArgs>(unit, write_kernel<uint4>, write_kernel<uint2>, write_kernel<unsigned>, write_kernel<unsigned short>,
                                                  (unsigned)(blocks < most ? blocks : most), st, a);
     return e == cudaSuccess ? STREAM_OK : cuda_fail(e, "cache write launch");
+}
+
+stream_status launch_read(const CacheGeom &c, int elem, const void *k_pages, const void *v_pages, const int32_t *cu, int total, void *k_out, void *v_out, cudaStream_t st) {
+    ReadArgs a = {};
+    a.c = c; a.k_pages = (const char *)k_pages; a.v_pages = (const char *)v_pages; a.k = (char *)k_out; a.v = (char *)v_out;
+    a.cu = cu; a.total = total; a.elem = elem;
+    const long long row = (long long)c.d * elem, all = row * c.G;
+    const int unit = unit_of({(long long)(uintptr_t)k_pages, (long long)(uintptr_t)v_pages, (long long)(uintptr_t)k_out, (long long)(uintptr_t)v_out,
+                              c.s_p * elem, c.s_t * elem, c.s_h * elem, row});
+    a.per_token = (int)(all / unit);
+    a.run = c.G == 1 || c.s_h == c.d ? a.per_token : (int)(row / unit);
+    const int n_sm = current_sm_count();
+    if (n_sm <= 0) { set_error("cannot read the SM count of the current device"); return STREAM_ERR_CUDA; }
+    const long long blocks = ((long long)total + kThreads / 32 - 1) / (kThreads / 32), most = (long long)n_sm * kCtas;
+    const cudaError_t e = launch_unit<ReadArgs>(unit, read_kernel<uint4>, read_kernel<uint2>, read_kernel<unsigned>, read_kernel<unsigned short>,
+                                                (unsigned)(blocks < most ? blocks : most), st, a);
+    return e == cudaSuccess ? STREAM_OK : cuda_fail(e, "cache read launch");
 }
 
 }  // namespace stream

@@ -46,7 +46,7 @@ __device__ __forceinline__ float4 read4(const unsigned char *p) {
     }
 }
 
-template <class T, int D>
+template <class T, int D, bool W>
 __global__ void __launch_bounds__(kThreads) decode_kernel(Args A, int vec) {
     using F = Form<T, D>;
     extern __shared__ __align__(16) unsigned char smem_raw[];
@@ -56,18 +56,19 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(Args A, int vec) {
     after_previous_kernel();
     T *const out = (T *)A.a.out;
     write_empty_slots<T>(A);
-    const Share mine = share_of(A, all_places(A, lane), (int)blockIdx.x);
+    const Share mine = share_of(A, all_places<W>(A, lane), (int)blockIdx.x);
     unsigned bad = 0;
     Place pl = {0, 0, 0};
     int n_parts = 0;
     Left left = {};
-    for (Segment sg = open_segment(A, mine.first, mine.end, lane, pl); sg.next >= 0; sg = open_segment(A, sg.next, mine.end, lane, pl)) {
+    for (Segment sg = open_segment<W>(A, mine.first, mine.end, lane, pl); sg.next >= 0; sg = open_segment<W>(A, sg.next, mine.end, lane, pl)) {
         const int s = sg.slot, nh = sg.heads, h0 = sg.h0, key0 = sg.key0, key_end = sg.key_end;
         const int n_tiles = (key_end - key0 + F::kKeys - 1) / F::kKeys;
         const int32_t *const row = c.table + (long long)s * c.max_pages;
+        const Seen seen = seen_of<W>(A.a, s);
         auto page_of = [&](int tile) -> int {  // of this thread's key
-            const int key = key0 + tile * F::kKeys + tid;
-            if (key >= key_end) return -1;
+            const int walked = key0 + tile * F::kKeys + tid, key = W ? seen.key(walked) : walked;
+            if (walked >= key_end || (W && !seen.sees(key))) return -1;
             const int page = row[key / c.page];
             if ((unsigned)page < (unsigned)c.n_pages) return page;
             bad = (unsigned)s + 1u;
@@ -78,7 +79,7 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(Args A, int vec) {
             const int *const pages = sm.page[tile % 3];
             for (int i = tid; i < F::kKeys * kPieces; i += kThreads) {
                 const int r = i / kPieces, x = i % kPieces, page = pages[r];
-                const long long e = (long long)max(page, 0) * c.s_p + (long long)((key0 + tile * F::kKeys + r) % c.page) * c.s_t + (long long)sg.kvh * c.s_h + x * (16 / (int)sizeof(T));
+                const long long e = (long long)max(page, 0) * c.s_p + (long long)((W ? seen.key(key0 + tile * F::kKeys + r) : key0 + tile * F::kKeys + r) % c.page) * c.s_t + (long long)sg.kvh * c.s_h + x * (16 / (int)sizeof(T));
                 const T *const ks = (const T *)A.a.k + e, *const vs = (const T *)A.a.v + e;
                 unsigned char *const kd = sm.k[buf] + r * F::kRow + x * 16, *const vd = sm.v[buf] + r * F::kRow + x * 16;
                 if (vec) {
@@ -314,28 +315,62 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     if (A.a.lse != nullptr && tid == 0) A.a.lse[to] = l > 0.f ? (m + log2f(l)) * kLn2 : -CUDART_INF_F;
 }
 
-template <class T, int D>
+template <class T, int D, bool W>
 cudaError_t launch_fma(const Args &A, int vec, cudaStream_t st) {
     const int smem = (int)sizeof(Smem<T, D>);
     static DeviceFlags done;
-    cudaError_t e = allow_smem_once(decode_kernel<T, D>, smem, done);
+    cudaError_t e = allow_smem_once(decode_kernel<T, D, W>, smem, done);
     if (e != cudaSuccess) return e;
-    return launch_early(decode_kernel<T, D>, (unsigned)A.grid, kThreads, smem, st, A, vec);
+    return launch_early(decode_kernel<T, D, W>, (unsigned)A.grid, kThreads, smem, st, A, vec);
 }
-template <class T>
+template <class T, bool W>
 cudaError_t launch_fma_d(const Args &A, int vec, cudaStream_t st) {
     switch (A.a.c.d) {
-        case 16: return launch_fma<T, 16>(A, vec, st);
-        case 32: return launch_fma<T, 32>(A, vec, st);
-        case 64: return launch_fma<T, 64>(A, vec, st);
-        case 128: return launch_fma<T, 128>(A, vec, st);
-        default: return launch_fma<T, 256>(A, vec, st);
+        case 16: return launch_fma<T, 16, W>(A, vec, st);
+        case 32: return launch_fma<T, 32, W>(A, vec, st);
+        case 64: return launch_fma<T, 64, W>(A, vec, st);
+        case 128: return launch_fma<T, 128, W>(A, vec, st);
+        default: return launch_fma<T, 256, W>(A, vec, st);
     }
+}
+template <bool W>
+cudaError_t launch_keys(Args &A, int dtype, int n_sm, cudaStream_t st) {
+    const int e = dtype == STREAM_F32 ? 4 : 2;
+    const DecodeCall &a = A.a;
+    const long long any = (long long)(uintptr_t)a.k | (long long)(uintptr_t)a.v | a.c.s_p * e | a.c.s_t * e | a.c.s_h * e;
+    const int vec = any % 16 == 0 ? 1 : 0;
+    if (warp_supported(a, dtype)) return launch_warp(A, dtype, n_sm, st);
+    return dtype == STREAM_F32 ? launch_fma_d<float, W>(A, vec, st) : launch_fma_d<__nv_bfloat16, W>(A, vec, st);
 }
 
 constexpr size_t kLeftBytes = (kMaxGrid * sizeof(Left) + 255) & ~(size_t)255;
 
 }  // namespace
+
+namespace decode {
+
+Args args_of(const DecodeCall &a, void *workspace, int n_sm) {
+    Args A;
+    A.a = a;
+    A.chunks = (a.hpg + kMaxHeads - 1) / kMaxHeads;
+    A.per_slot = a.c.G * A.chunks;
+    A.header = (WorkspaceHeader *)workspace;
+    A.left = (Left *)((char *)workspace + sizeof(WorkspaceHeader));
+    A.parts = (float *)((char *)A.left + kLeftBytes);
+    long long keys = (long long)a.c.max_pages * a.c.page;  // of a slot, at most
+    if (a.window > 0) keys = std::min(keys, ((long long)a.window + kUnit - 1) + ((long long)a.sinks + kUnit - 1));
+    const long long most = (long long)a.c.n_slots * A.per_slot * ((keys + kUnit - 1) / kUnit + kOpen);
+    const int want = 2 * n_sm < kMaxGrid ? 2 * n_sm : kMaxGrid;
+    A.grid = (int)(most < want ? most : want);
+    return A;
+}
+
+cudaError_t launch_joins(const Args &A, int dtype, cudaStream_t st) {
+    const dim3 joins(A.grid + 1, A.a.hpg < kMaxHeads ? A.a.hpg : kMaxHeads);
+    return dtype == STREAM_F32 ? launch_early(join_kernel<float>, joins, kJoinThreads, 0, st, A) : launch_early(join_kernel<__nv_bfloat16>, joins, kJoinThreads, 0, st, A);
+}
+
+}  // namespace decode
 
 size_t decode_workspace_bytes(const CacheGeom &c) {
     return sizeof(WorkspaceHeader) + kLeftBytes + (size_t)kMaxGrid * 2 * kMaxHeads * (c.d + 2) * sizeof(float);
@@ -344,25 +379,10 @@ size_t decode_workspace_bytes(const CacheGeom &c) {
 stream_status launch_decode(const DecodeCall &a, int dtype, void *workspace, cudaStream_t st) {
     const int n_sm = current_sm_count();
     if (n_sm <= 0) { set_error("cannot read the SM count of the current device"); return STREAM_ERR_CUDA; }
-    const int e = dtype == STREAM_F32 ? 4 : 2;
-    Args A;
-    A.a = a;
-    A.chunks = (a.hpg + kMaxHeads - 1) / kMaxHeads;
-    A.per_slot = a.c.G * A.chunks;
-    A.header = (WorkspaceHeader *)workspace;
-    A.left = (Left *)((char *)workspace + sizeof(WorkspaceHeader));
-    A.parts = (float *)((char *)A.left + kLeftBytes);
-    const long long most = (long long)a.c.n_slots * A.per_slot * (((long long)a.c.max_pages * a.c.page + kUnit - 1) / kUnit + kOpen);
-    const int want = 2 * n_sm < kMaxGrid ? 2 * n_sm : kMaxGrid;
-    A.grid = (int)(most < want ? most : want);
-    const long long any = (long long)(uintptr_t)a.k | (long long)(uintptr_t)a.v | a.c.s_p * e | a.c.s_t * e | a.c.s_h * e;
-    const int vec = any % 16 == 0 ? 1 : 0;
-    cudaError_t rc = warp_supported(a, dtype) ? launch_warp(A, dtype, n_sm, st)
-                     : dtype == STREAM_F32   ? launch_fma_d<float>(A, vec, st)
-                                             : launch_fma_d<__nv_bfloat16>(A, vec, st);
+    Args A = args_of(a, workspace, n_sm);
+    cudaError_t rc = a.window > 0 ? launch_keys<true>(A, dtype, n_sm, st) : launch_keys<false>(A, dtype, n_sm, st);
     if (rc != cudaSuccess) return cuda_fail(rc, "decode attention launch");
-    const dim3 joins(A.grid + 1, a.hpg < kMaxHeads ? a.hpg : kMaxHeads);
-    rc = dtype == STREAM_F32 ? launch_early(join_kernel<float>, joins, kJoinThreads, 0, st, A) : launch_early(join_kernel<__nv_bfloat16>, joins, kJoinThreads, 0, st, A);
+    rc = launch_joins(A, dtype, st);
     return rc == cudaSuccess ? STREAM_OK : cuda_fail(rc, "decode join launch");
 }
 

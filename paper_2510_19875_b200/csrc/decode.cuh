@@ -32,6 +32,10 @@ struct Args {
     int q_vec;                   // (decode_warp.cu) q is read in pieces of 16 bytes
 };
 
+// The arguments that follow from the call, and the grid at most; the joins' launch.
+Args args_of(const DecodeCall &a, void *workspace, int n_sm);
+cudaError_t launch_joins(const Args &A, int dtype, cudaStream_t st);
+
 // Rows of 16-byte pieces, up to 512 bytes. May lower A.grid.
 bool warp_supported(const DecodeCall &a, int dtype);
 cudaError_t launch_warp(Args &A, int dtype, int n_sm, cudaStream_t st);
@@ -42,26 +46,46 @@ cudaError_t launch_warp(Args &A, int dtype, int n_sm, cudaStream_t st);
 // 8192 tokens 54.2, 46.4, 45.8, 47.3; the four 96.3, 88.5, 88.5, 88.6; nine of up to 5003, fp32, 21.0, 20.0, 20.0, 19.8; slots of some tokens 7 to 10 with any.
 constexpr int kOpen = 2;
 
+// Which keys of a slot are walked where there is a window (W): the units of the sinks, then, behind a gap, those from the window's first key on. A
+// segment counts its keys without the gap; units are whole on both sides of it, so that a tile's keys lie as they do without.
+struct Seen {
+    int n;          // keys that are walked
+    int sink_keys;  // of them in front of the gap
+    int gap;        // keys
+    int sinks, low; // seen are keys < sinks and keys >= low
+    __device__ __forceinline__ int key(int walked) const { return walked < sink_keys ? walked : walked + gap; }
+    __device__ __forceinline__ bool sees(int key) const { return key < sinks || key >= low; }
+};
+template <bool W>
+__device__ __forceinline__ Seen seen_of(const DecodeCall &a, int s) {
+    const int n = tokens_of(a.c, s);
+    if constexpr (!W) return {n, n, 0, n, 0};
+    const int low = max(0, n - a.window), sink = (min(a.sinks, n) + kUnit - 1) / kUnit, gap = max(0, low / kUnit - sink) * kUnit;
+    return {n - gap, sink * kUnit, gap, a.sinks, low};
+}
+
 // Sums over the slots, by whole warps (the same in every lane).
-__device__ __forceinline__ int units_of(const CacheGeom &c, int s) { return s < c.n_slots ? (tokens_of(c, s) + kUnit - 1) / kUnit : 0; }
-__device__ __forceinline__ int places_of(const CacheGeom &c, int s) {
-    const int u = units_of(c, s);
+template <bool W>
+__device__ __forceinline__ int places_of(const DecodeCall &a, int s) {
+    const int u = s < a.c.n_slots ? (seen_of<W>(a, s).n + kUnit - 1) / kUnit : 0;
     return u > 0 ? u + kOpen : 0;
 }
+template <bool W>
 __device__ __forceinline__ long long all_places(const Args &A, int lane) {
     long long sum = 0;
-    for (int s = lane; s < A.a.c.n_slots; s += 32) sum += places_of(A.a.c, s);
+    for (int s = lane; s < A.a.c.n_slots; s += 32) sum += places_of<W>(A.a, s);
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
     return sum * A.per_slot;
 }
 // Whose a place is: the slot, where that slot's places begin, how many it has for one owner. `from`: one at or before it.
 struct Place { int slot, n; long long first; };
+template <bool W>
 __device__ __forceinline__ Place place_of(const Args &A, long long at, int lane, Place from) {
     const CacheGeom &c = A.a.c;
     long long sum = from.first;
     for (int s0 = from.slot; s0 < c.n_slots; s0 += 32) {
-        const int n = places_of(c, s0 + lane);
+        const int n = places_of<W>(A.a, s0 + lane);
         long long incl = n;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -91,9 +115,10 @@ struct Segment {
     long long next;      // the place behind it
     long long owner_end; // the place behind all of its owner's
     int slot, kvh, h0, heads;
-    int key0, key_end;   // keys of the slot (none where key0 = key_end)
+    int key0, key_end;   // keys of the slot (none where key0 = key_end), as Seen counts them
     bool whole;          // all of them
 };
+template <bool W>
 __device__ __forceinline__ Segment segment_of(const Args &A, const Place &pl, long long at, long long end) {
     Segment sg;
     const int owner = (int)((at - pl.first) / pl.n), chunk = owner % A.chunks;
@@ -106,16 +131,17 @@ __device__ __forceinline__ Segment segment_of(const Args &A, const Place &pl, lo
     sg.heads = min(kMaxHeads, A.a.hpg - chunk * kMaxHeads);
     const int unit0 = (int)max(at - first - kOpen, 0ll), unit1 = (int)max(sg.next - first - kOpen, 0ll);
     sg.key0 = unit0 * kUnit;
-    sg.key_end = (int)min((long long)tokens_of(A.a.c, pl.slot), (long long)unit1 * kUnit);
+    sg.key_end = (int)min((long long)seen_of<W>(A.a, pl.slot).n, (long long)unit1 * kUnit);
     if (unit0 == unit1) sg.key_end = sg.key0;
     sg.whole = unit0 == 0 && unit1 == pl.n - kOpen;
     return sg;
 }
 // The first segment with keys at or behind place `at` of a share that ends at `end`; pl: a place at or before it. next = -1: none.
+template <bool W>
 __device__ __forceinline__ Segment open_segment(const Args &A, long long at, long long end, int lane, Place &pl) {
     while (at < end) {
-        pl = place_of(A, at, lane, pl);
-        const Segment sg = segment_of(A, pl, at, end);
+        pl = place_of<W>(A, at, lane, pl);
+        const Segment sg = segment_of<W>(A, pl, at, end);
         if (sg.key_end > sg.key0) return sg;
         at = sg.next;
     }

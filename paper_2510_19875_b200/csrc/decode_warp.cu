@@ -254,7 +254,7 @@ struct Walk<float, D> {
     }
 };
 
-template <class T, int D>
+template <class T, int D, bool W>
 __global__ void __launch_bounds__(kThreads, Form<T, D>::kCtas) decode_warp_kernel(const __grid_constant__ Args A) {
     using F = Form<T, D>;
     extern __shared__ __align__(128) unsigned char smem_raw[];
@@ -264,7 +264,7 @@ __global__ void __launch_bounds__(kThreads, Form<T, D>::kCtas) decode_warp_kerne
     after_previous_kernel();
     T *const out = (T *)A.a.out;
     write_empty_slots<T>(A);
-    const Share mine = share_of(A, all_places(A, lane), (int)blockIdx.x);
+    const Share mine = share_of(A, all_places<W>(A, lane), (int)blockIdx.x);
     unsigned char *const ring_ptr = sm.ring[warp];
     const unsigned ring = wp::smem_addr(ring_ptr), q_smem = wp::smem_addr(sm.q);
     const bool one_page = c.page % kStep == 0;  // a tile's keys lie side by side
@@ -278,21 +278,22 @@ __global__ void __launch_bounds__(kThreads, Form<T, D>::kCtas) decode_warp_kerne
     unsigned at = 0;
     unsigned long long keys_there = 0;  // 16 flags a place of the ring
     int page = -1;                      // lane i < 16: the page of key i of the next step to be fetched, -1: none
+    Seen seen = {};
     auto page_of = [&](int n) -> int {
-        const int key = key_w + 4 * n * kStep + lane;
-        if (n >= n_steps || lane >= kStep || key >= key_end) return -1;
+        const int walked = key_w + 4 * n * kStep + lane, key = W ? seen.key(walked) : walked;
+        if (n >= n_steps || lane >= kStep || walked >= key_end) return -1;
         const int x = table[key / c.page];
         if ((unsigned)x < (unsigned)c.n_pages) return x;
-        bad = (unsigned)slot + 1u;
+        if (!W || seen.sees(key)) bad = (unsigned)slot + 1u;
         return -1;
     };
     auto fetch = [&](int n) {  // step n, and the pages of the one after it are looked up
         const int own_page = page;
         page = page_of(n + 1);
         if (n < n_steps) {
-            const unsigned place = (at + (unsigned)n) % F::kStages, there = __ballot_sync(0xffffffffu, own_page >= 0);
+            const int walked = key_w + 4 * n * kStep + lane, key = W ? seen.key(walked) : walked;
+            const unsigned place = (at + (unsigned)n) % F::kStages, there = __ballot_sync(0xffffffffu, own_page >= 0 && (!W || seen.sees(key)));
             keys_there = (keys_there & ~(0xffffull << (16 * place))) | (unsigned long long)there << (16 * place);
-            const int key = key_w + 4 * n * kStep + lane;
             const long long own = own_page >= 0 ? (long long)own_page * c.s_p + (long long)(key % c.page) * c.s_t : 0;
             const unsigned dst = ring + place * 2 * F::kTile;
             const long long base = __shfl_sync(0xffffffffu, own, 0) + row_l * c.s_t;
@@ -316,6 +317,7 @@ __global__ void __launch_bounds__(kThreads, Form<T, D>::kCtas) decode_warp_kerne
     auto open = [&](const Segment &sg) {
         at += (unsigned)n_steps;
         slot = sg.slot;
+        if constexpr (W) seen = seen_of<W>(A.a, slot);
         table = c.table + (long long)slot * c.max_pages;
         ks = (const T *)A.a.k + (long long)sg.kvh * c.s_h;
         vs = (const T *)A.a.v + (long long)sg.kvh * c.s_h;
@@ -350,7 +352,7 @@ __global__ void __launch_bounds__(kThreads, Form<T, D>::kCtas) decode_warp_kerne
     Place pl = {0, 0, 0};
     int n_parts = 0;
     Left left = {};
-    Segment sg = open_segment(A, mine.first, mine.end, lane, pl);
+    Segment sg = open_segment<W>(A, mine.first, mine.end, lane, pl);
     if (sg.next >= 0) open(sg);
     while (sg.next >= 0) {
         const int s = sg.slot;
@@ -371,7 +373,7 @@ __global__ void __launch_bounds__(kThreads, Form<T, D>::kCtas) decode_warp_kerne
             walk.step(sm, warp, kt, ring_ptr + place * 2 * F::kTile, keys, sg.heads, A.a.scale_log2, lane);
             __syncwarp();  // (the tile is read before its place is filled again)
         }
-        const Segment next = open_segment(A, sg.next, mine.end, lane, pl);
+        const Segment next = open_segment<W>(A, sg.next, mine.end, lane, pl);
         if (next.next >= 0) {
             open(next);
         } else {
@@ -420,15 +422,19 @@ __global__ void __launch_bounds__(kThreads, Form<T, D>::kCtas) decode_warp_kerne
     leave_to_joins(A, left, bad);
 }
 
-template <class T, int D>
-cudaError_t launch(Args &A, int n_sm, cudaStream_t st) {
+template <class T, int D, bool W>
+cudaError_t launch_form(Args &A, int n_sm, cudaStream_t st) {
     const int smem = (int)sizeof(Smem<T, D>);
     static DeviceFlags done;
-    cudaError_t e = allow_smem_once(decode_warp_kernel<T, D>, smem, done);
+    cudaError_t e = allow_smem_once(decode_warp_kernel<T, D, W>, smem, done);
     if (e != cudaSuccess) return e;
     const int most = Form<T, D>::kCtas * n_sm;
     if (A.grid > most) A.grid = most;
-    return launch_early(decode_warp_kernel<T, D>, (unsigned)A.grid, kThreads, smem, st, A);
+    return launch_early(decode_warp_kernel<T, D, W>, (unsigned)A.grid, kThreads, smem, st, A);
+}
+template <class T, int D>
+cudaError_t launch(Args &A, int n_sm, cudaStream_t st) {
+    return A.a.window > 0 ? launch_form<T, D, true>(A, n_sm, st) : launch_form<T, D, false>(A, n_sm, st);
 }
 
 }  // namespace

@@ -43,7 +43,7 @@ __device__ __forceinline__ float4 load4(const T *p, bool vec) {
     }
 }
 
-template <class T, int D>
+template <class T, int D, bool W>
 __global__ void __launch_bounds__(kThreads) prompt_kernel(PromptGeom g, const T *q, const T *k, const T *v, int vec) {
     extern __shared__ __align__(16) unsigned char smem_raw[];
     Smem<D> &sm = *reinterpret_cast<Smem<D> *>(smem_raw);
@@ -68,6 +68,10 @@ __global__ void __launch_bounds__(kThreads) prompt_kernel(PromptGeom g, const T 
         return min(sk.n, max(0, tok + shift + 1));
     };
     const int most = keys_of(n_rows - 1);
+    Walked wk = {};
+    if constexpr (W) wk = walked_keys<kKeys>(g, (int)(row_base / g.hpg) + shift, sk.n);
+    const int walked = most - wk.gap;  // keys without the gap
+    auto key_of = [&](long long j) -> long long { return W && j >= wk.sink_keys ? j + wk.gap : j; };  // of a tile's first
     const T *const qs = q + (long long)sq.first * g.qs_t + (long long)kvh * g.hpg * g.qs_h;
     const T *const ks = k + (long long)sk.first * g.ks_t + (long long)kvh * g.ks_h;
     const T *const vs = v + (long long)sk.first * g.ks_t + (long long)kvh * g.ks_h;
@@ -81,9 +85,10 @@ __global__ void __launch_bounds__(kThreads) prompt_kernel(PromptGeom g, const T 
         *reinterpret_cast<float4 *>(&sm.q[r * kPad + c]) = make_float4(x.x * g.scale_log2, x.y * g.scale_log2, x.z * g.scale_log2, x.w * g.scale_log2);
     }
     float m[4], l[4], o[4][kParts * kCols];
-    int see[4];
+    int see[4], low[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
+        low[i] = W ? window_begin(g, (int)((row_base + min(ty * 4 + i, n_rows - 1)) / g.hpg) + shift) : 0;
         m[i] = -CUDART_INF_F;
         l[i] = 0.f;
         see[i] = keys_of(ty * 4 + i);
@@ -93,10 +98,11 @@ __global__ void __launch_bounds__(kThreads) prompt_kernel(PromptGeom g, const T 
     constexpr int kBufs = Smem<D>::kBufs;
     const long long step = (long long)ctas * kKeys;
     auto fetch = [&](long long j0, int buf) {
-        if (j0 < most) {
+        if (j0 < walked) {
+            const long long j = key_of(j0);
             for (int i = tid; i < kKeys * (D / 4); i += kThreads) {
                 const int r = i / (D / 4), c = (i % (D / 4)) * 4;
-                const long long key = j0 + r;
+                const long long key = j + r;
                 const bool there = key < sk.n;
                 const T *const kp = ks + (there ? key * g.ks_t : 0) + c, *const vp = vs + (there ? key * g.ks_t : 0) + c;
                 float *const kd = &sm.k[buf][r * kPad + c], *const vd = &sm.v[buf][r * D + c];
@@ -114,7 +120,7 @@ __global__ void __launch_bounds__(kThreads) prompt_kernel(PromptGeom g, const T 
     const long long j_first = (long long)rank * kKeys;
     if (kBufs == 2) fetch(j_first, 0);
     int buf = 0;
-    for (long long j0 = j_first; j0 < most; j0 += step, buf ^= kBufs - 1) {
+    for (long long j0 = j_first; j0 < walked; j0 += step, buf ^= kBufs - 1) {
         if (kBufs == 2) {
             fetch(j0 + step, buf ^ 1);
             wp::cp_async_wait<1>();
@@ -124,6 +130,7 @@ __global__ void __launch_bounds__(kThreads) prompt_kernel(PromptGeom g, const T 
             wp::cp_async_wait<0>();
         }
         __syncthreads();
+        const long long ja = key_of(j0);
         float s[4][4];  // rows ty * 4 + i, keys tx + 16 * j
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -146,7 +153,7 @@ __global__ void __launch_bounds__(kThreads) prompt_kernel(PromptGeom g, const T 
             float mx = -CUDART_INF_F;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                if (j0 + tx + 16 * j >= see[i]) s[i][j] = -CUDART_INF_F;
+                if (ja + tx + 16 * j >= see[i] || (W && ja + tx + 16 * j < low[i] && ja + tx + 16 * j >= g.sinks)) s[i][j] = -CUDART_INF_F;
                 mx = fmaxf(mx, s[i][j]);
             }
 #pragma unroll
@@ -260,11 +267,11 @@ __global__ void __launch_bounds__(kThreads) prompt_kernel(PromptGeom g, const T 
     }
 }
 
-template <class T, int D>
+template <class T, int D, bool W>
 stream_status launch(const PromptGeom &g, const void *q, const void *k, const void *v, cudaStream_t st) {
     const int smem = (int)sizeof(Smem<D>);
     static DeviceFlags done;
-    cudaError_t e = allow_smem_once(prompt_kernel<T, D>, smem, done);
+    cudaError_t e = allow_smem_once(prompt_kernel<T, D, W>, smem, done);
     if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(prompt)");
     const long long tiles = most_row_tiles(g, kRows);
     const int n_sm = current_sm_count();
@@ -276,26 +283,27 @@ stream_status launch(const PromptGeom &g, const void *q, const void *k, const vo
     const long long any = (long long)(uintptr_t)q | (long long)(uintptr_t)k | (long long)(uintptr_t)v;
     const long long strides = g.qs_t | g.qs_h | g.ks_t | g.ks_h;
     const int vec = any % (4 * (int)sizeof(T)) == 0 && strides % 4 == 0 ? 1 : 0;
-    if (cluster == 1) e = launch_early(prompt_kernel<T, D>, (unsigned)tiles, kThreads, smem, st, g, (const T *)q, (const T *)k, (const T *)v, vec);
-    else e = launch_clusters(prompt_kernel<T, D>, (unsigned)tiles * cluster, kThreads, smem, st, cluster, g, (const T *)q, (const T *)k, (const T *)v, vec);
+    if (cluster == 1) e = launch_early(prompt_kernel<T, D, W>, (unsigned)tiles, kThreads, smem, st, g, (const T *)q, (const T *)k, (const T *)v, vec);
+    else e = launch_clusters(prompt_kernel<T, D, W>, (unsigned)tiles * cluster, kThreads, smem, st, cluster, g, (const T *)q, (const T *)k, (const T *)v, vec);
     return e == cudaSuccess ? STREAM_OK : cuda_fail(e, "prompt attention launch");
 }
 
-template <class T>
+template <class T, bool W>
 stream_status launch_d(const PromptGeom &g, const void *q, const void *k, const void *v, cudaStream_t st) {
     switch (g.d) {
-        case 16: return launch<T, 16>(g, q, k, v, st);
-        case 32: return launch<T, 32>(g, q, k, v, st);
-        case 64: return launch<T, 64>(g, q, k, v, st);
-        case 128: return launch<T, 128>(g, q, k, v, st);
-        default: return launch<T, 256>(g, q, k, v, st);
+        case 16: return launch<T, 16, W>(g, q, k, v, st);
+        case 32: return launch<T, 32, W>(g, q, k, v, st);
+        case 64: return launch<T, 64, W>(g, q, k, v, st);
+        case 128: return launch<T, 128, W>(g, q, k, v, st);
+        default: return launch<T, 256, W>(g, q, k, v, st);
     }
 }
 
 }  // namespace
 
 stream_status launch_prompt_generic(const PromptGeom &g, int dtype, const void *q, const void *k, const void *v, cudaStream_t st) {
-    return dtype == STREAM_F32 ? launch_d<float>(g, q, k, v, st) : launch_d<__nv_bfloat16>(g, q, k, v, st);
+    if (g.window > 0) return dtype == STREAM_F32 ? launch_d<float, true>(g, q, k, v, st) : launch_d<__nv_bfloat16, true>(g, q, k, v, st);
+    return dtype == STREAM_F32 ? launch_d<float, false>(g, q, k, v, st) : launch_d<__nv_bfloat16, false>(g, q, k, v, st);
 }
 
 }  // namespace stream

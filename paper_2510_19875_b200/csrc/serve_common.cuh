@@ -18,7 +18,19 @@ struct PromptGeom {
     float scale_log2;  // logit scale times log2(e)
     void *out;
     float *lse;
+    int window, sinks; // window > 0: a query at position p sees the keys j <= p with j > p - window or j < sinks
 };
+
+// What a tile of rows walks of the keys where there is a window, in tiles of kKeys: those of the sinks, and behind a gap all from the first key that
+// the first row's window has. (Positions below 0 see nothing.)
+struct Walked { int sink_keys, gap; };  // keys in front of the gap, keys of the gap: multiples of kKeys
+template <int kKeys>
+__device__ __forceinline__ Walked walked_keys(const PromptGeom &g, int first_pos, int n_keys) {
+    const int low = max(0, max(first_pos, 0) - g.window + 1) / kKeys, sink = (min(g.sinks, n_keys) + kKeys - 1) / kKeys;
+    return {sink * kKeys, max(0, low - sink) * kKeys};
+}
+// The first key of a position's window.
+__device__ __forceinline__ int window_begin(const PromptGeom &g, int pos) { return max(0, max(pos, 0) - g.window + 1); }
 
 // A paged cache and the ledger.
 struct CacheGeom {
@@ -34,6 +46,19 @@ struct Span { int first, n; };
 __device__ __forceinline__ Span span_of(const int32_t *cu, int s, int total) {
     const int a = min(max(cu[s], 0), total), b = min(max(cu[s + 1], a), total);
     return {a, b - a};
+}
+// The slot whose packed rows hold row t, if any does: the last one that begins at or before it (32 candidates a step). By a whole warp.
+__device__ __forceinline__ int slot_of_row(const int32_t *cu, int n_slots, long long t, int lane) {
+    int lo = 0, hi = n_slots;
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 31) / 32;
+        const long long at = lo + (long long)lane * step;
+        const unsigned below = __ballot_sync(0xffffffffu, at < hi && cu[at] <= t);
+        const int last = below != 0 ? 31 - __clz(below) : 0;
+        lo += last * step;
+        hi = min(hi, lo + step);
+    }
+    return lo;
 }
 // Tokens of a slot.
 __device__ __forceinline__ int tokens_of(const CacheGeom &c, int s) { return min(max(c.len[s], 0), c.max_pages * c.page); }
@@ -126,9 +151,17 @@ struct DecodeCall {
     float scale_log2;
     void *out;
     float *lse;
+    int window, sinks;     // as in PromptGeom
+};
+// The scales of a cache in 8 bits: of the layer.
+struct Scales {
+    const float *k, *v;
+    long long s_p, s_b, s_h;  // page, block, head
+    int block;                // tokens
 };
 size_t decode_workspace_bytes(const CacheGeom &c);
 stream_status launch_decode(const DecodeCall &a, int dtype, void *workspace, cudaStream_t st);
+stream_status launch_decode8(const DecodeCall &a, const Scales &sc, int dtype, void *workspace, cudaStream_t st);
 
 size_t ledger_workspace_bytes(const CacheGeom &c);
 stream_status launch_reserve(const CacheGeom &c, const int32_t *n_new, int32_t *info, void *ws, cudaStream_t st);
@@ -138,5 +171,10 @@ stream_status launch_compact(const CacheGeom &c, int32_t *pairs, int32_t *info, 
 stream_status launch_copy_pages(const CacheGeom &c, int elem, void *k, void *v, const int32_t *pairs, const int32_t *count, int n_pairs, cudaStream_t st);
 stream_status launch_write(const CacheGeom &c, int elem, const void *k, const void *v, int total, long long s_t, long long s_h,
                            const int32_t *cu_new, const int32_t *done, void *k_pages, void *v_pages, cudaStream_t st);
+stream_status launch_read(const CacheGeom &c, int elem, const void *k_pages, const void *v_pages, const int32_t *cu, int total, void *k_out, void *v_out, cudaStream_t st);
+stream_status launch_write8(const CacheGeom &c, const Scales &sc, int dtype, const void *k, const void *v, int total, long long s_t, long long s_h,
+                            const int32_t *cu_new, const int32_t *done, void *k_pages, void *v_pages, cudaStream_t st);
+stream_status launch_read8(const CacheGeom &c, const Scales &sc, int dtype, const void *k_pages, const void *v_pages, const int32_t *cu, int total,
+                           void *k_out, void *v_out, cudaStream_t st);
 
 }  // namespace stream

@@ -8,7 +8,7 @@ streams only.
 
 Masks and the sparse attention on them: ``build_mask`` ... ``mask_difference``. Dense attention and the
 key-value cache of chains that are being generated: ``prompt_attention``, ``decode_attention``,
-``PagedCache`` and the ``cache_*`` functions.
+``PagedCache``, ``PagedCache8`` (8 bits an element) and the ``cache_*`` functions.
 """
 from __future__ import annotations
 
@@ -61,6 +61,13 @@ class StreamCache(ctypes.Structure):
     _fields_ = [("n_slots", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32),
                 ("n_kv_heads", ctypes.c_int32), ("d", ctypes.c_int32), ("n_layers", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("stride_l", ctypes.c_int64), ("stride_p", ctypes.c_int64), ("stride_t", ctypes.c_int64), ("stride_h", ctypes.c_int64)]
+
+
+class StreamCache8(ctypes.Structure):
+    """``stream_cache8`` of stream.h."""
+
+    _fields_ = [("cache", StreamCache), ("block", ctypes.c_int32), ("reserved", ctypes.c_int32), ("scale_stride_l", ctypes.c_int64),
+                ("scale_stride_p", ctypes.c_int64), ("scale_stride_b", ctypes.c_int64), ("scale_stride_h", ctypes.c_int64)]
 
 
 class StreamStats(ctypes.Structure):
@@ -165,6 +172,21 @@ def _load():
     lib.stream_decode_workspace_bytes.argtypes = [PC, i32]
     lib.stream_decode_attention.restype = ctypes.c_int
     lib.stream_decode_attention.argtypes = [PC, i32, i32, vp, i64, i64, vp, vp, vp, vp, ctypes.c_float, vp, vp, vp, sz, vp]
+    P8 = ctypes.POINTER(StreamCache8)
+    lib.stream_cache_read.restype = ctypes.c_int
+    lib.stream_cache_read.argtypes = [PC, i32, vp, vp, vp, i64, vp, vp, vp, vp, vp]
+    lib.stream_prompt_window_attention.restype = ctypes.c_int
+    lib.stream_prompt_window_attention.argtypes = [vp, i32, i32, vp, vp, vp, vp, vp, ctypes.c_float, vp, vp, vp]
+    lib.stream_decode_window_attention.restype = ctypes.c_int
+    lib.stream_decode_window_attention.argtypes = [PC, i32, i32, i32, i32, vp, i64, i64, vp, vp, vp, vp, ctypes.c_float, vp, vp, vp, sz, vp]
+    lib.stream_cache8_write.restype = ctypes.c_int
+    lib.stream_cache8_write.argtypes = [P8, i32, vp, vp, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.stream_cache8_read.restype = ctypes.c_int
+    lib.stream_cache8_read.argtypes = [P8, i32, vp, vp, vp, vp, vp, i64, vp, vp, vp, vp, vp]
+    lib.stream_cache8_copy_pages.restype = ctypes.c_int
+    lib.stream_cache8_copy_pages.argtypes = [P8, vp, vp, vp, vp, vp, vp, i32, vp]
+    lib.stream_decode_attention8.restype = ctypes.c_int
+    lib.stream_decode_attention8.argtypes = [P8, i32, i32, i32, i32, vp, i64, i64, vp, vp, vp, vp, vp, vp, ctypes.c_float, vp, vp, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -368,6 +390,49 @@ def stream_decode_attention(c: StreamCache, layer: int, n_q_heads: int, q, q_str
     _raise(_load().stream_decode_attention(ctypes.byref(c), int(layer), int(n_q_heads), _addr(q), int(q_stride_s), int(q_stride_h),
                                            _addr(k_pages), _addr(v_pages), _addr(page_table), _addr(seq_len), float(scale),
                                            _addr(out), _addr(lse_out), _addr(workspace), workspace_bytes, _stream_handle(stream)))
+
+
+def stream_cache_read(c: StreamCache, layer: int, k_pages, v_pages, cu, total: int, page_table, seq_len, k_out, v_out, stream=None) -> None:
+    _raise(_load().stream_cache_read(ctypes.byref(c), layer, _addr(k_pages), _addr(v_pages), _addr(cu), total, _addr(page_table), _addr(seq_len),
+                                     _addr(k_out), _addr(v_out), _stream_handle(stream)))
+
+
+def stream_prompt_window_attention(p: StreamPrompt, window: int, sinks: int, q, k, v, cu_q, cu_k, scale: float, out, lse_out, stream=None) -> None:
+    _raise(_load().stream_prompt_window_attention(ctypes.byref(p), window, sinks, _addr(q), _addr(k), _addr(v), _addr(cu_q), _addr(cu_k), scale,
+                                                  _addr(out), _addr(lse_out), _stream_handle(stream)))
+
+
+def stream_decode_window_attention(c: StreamCache, layer: int, n_q_heads: int, window: int, sinks: int, q, q_stride_s: int, q_stride_h: int, k_pages,
+                                   v_pages, page_table, seq_len, scale: float, out, lse_out, workspace, workspace_bytes: int, stream=None) -> None:
+    _raise(_load().stream_decode_window_attention(ctypes.byref(c), layer, n_q_heads, window, sinks, _addr(q), q_stride_s, q_stride_h, _addr(k_pages),
+                                                  _addr(v_pages), _addr(page_table), _addr(seq_len), scale, _addr(out), _addr(lse_out),
+                                                  _addr(workspace), workspace_bytes, _stream_handle(stream)))
+
+
+def stream_cache8_write(c: StreamCache8, layer: int, k, v, total: int, stride_t: int, stride_h: int, cu_new, page_table, seq_len, done, k_pages,
+                        v_pages, k_scale, v_scale, stream=None) -> None:
+    _raise(_load().stream_cache8_write(ctypes.byref(c), layer, _addr(k), _addr(v), total, stride_t, stride_h, _addr(cu_new), _addr(page_table),
+                                       _addr(seq_len), _addr(done), _addr(k_pages), _addr(v_pages), _addr(k_scale), _addr(v_scale),
+                                       _stream_handle(stream)))
+
+
+def stream_cache8_read(c: StreamCache8, layer: int, k_pages, v_pages, k_scale, v_scale, cu, total: int, page_table, seq_len, k_out, v_out,
+                       stream=None) -> None:
+    _raise(_load().stream_cache8_read(ctypes.byref(c), layer, _addr(k_pages), _addr(v_pages), _addr(k_scale), _addr(v_scale), _addr(cu), total,
+                                      _addr(page_table), _addr(seq_len), _addr(k_out), _addr(v_out), _stream_handle(stream)))
+
+
+def stream_cache8_copy_pages(c: StreamCache8, k_pages, v_pages, k_scale, v_scale, pairs, count, n_pairs: int, stream=None) -> None:
+    _raise(_load().stream_cache8_copy_pages(ctypes.byref(c), _addr(k_pages), _addr(v_pages), _addr(k_scale), _addr(v_scale), _addr(pairs), _addr(count),
+                                            n_pairs, _stream_handle(stream)))
+
+
+def stream_decode_attention8(c: StreamCache8, layer: int, n_q_heads: int, window: int, sinks: int, q, q_stride_s: int, q_stride_h: int, k_pages,
+                             v_pages, k_scale, v_scale, page_table, seq_len, scale: float, out, lse_out, workspace, workspace_bytes: int,
+                             stream=None) -> None:
+    _raise(_load().stream_decode_attention8(ctypes.byref(c), layer, n_q_heads, window, sinks, _addr(q), q_stride_s, q_stride_h, _addr(k_pages),
+                                            _addr(v_pages), _addr(k_scale), _addr(v_scale), _addr(page_table), _addr(seq_len), scale, _addr(out),
+                                            _addr(lse_out), _addr(workspace), workspace_bytes, _stream_handle(stream)))
 
 
 # ----------------------------------------------------------------------------------------------
@@ -618,12 +683,22 @@ _PROMPT = struct.Struct("@iiiiqqiiqqqq")  # StreamPrompt's fields
 assert _PROMPT.size == ctypes.sizeof(StreamPrompt)
 
 
+def _window(window: int, sinks: int) -> tuple[int, int]:
+    """As the library takes them: larger than any sequence is as large as any."""
+    if window < 0 or sinks < 0:
+        raise ValueError("window and sinks must not be negative")
+    if sinks and not window:
+        raise ValueError("sinks are what is seen beside a window")
+    return min(window, 0x7fffffff), min(sinks, 0x7fffffff)
+
+
 def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor, cu_k: torch.Tensor | None = None, *,
-                     causal: bool = True, scale: float = 0.0, want_lse: bool = False, out: torch.Tensor | None = None,
-                     lse_out: torch.Tensor | None = None, stream=None):
+                     causal: bool = True, scale: float = 0.0, window: int = 0, sinks: int = 0, want_lse: bool = False,
+                     out: torch.Tensor | None = None, lse_out: torch.Tensor | None = None, stream=None):
     """Dense attention of packed prompts: q ``[total_q, H, d]``, k and v ``[total_k, G, d]``, ``cu_q`` and ``cu_k``
     int32 CUDA tensors ``[n_seqs + 1]`` with the sequences' first rows (``cu_k``: default ``cu_q``). Under a causal
-    mask a sequence's last query sees all its keys. Returns the output ``[total_q, H, d]``, with ``want_lse`` (or
+    mask a sequence's last query sees all its keys; with a ``window`` (0: none) a query sees the last ``window`` of those keys, its own among
+    them, and the first ``sinks``. Returns the output ``[total_q, H, d]``, with ``want_lse`` (or
     ``lse_out``) also the logarithms of the softmax sums, float32 ``[H, total_q]``. Rows of no sequence are left as they are. ``stream``, here and
     below: the call runs and allocates as under ``torch.cuda.stream(stream)``."""
     if not (q.is_cuda and k.is_cuda and v.is_cuda and cu_q.is_cuda):
@@ -648,7 +723,12 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: to
     elif cu_k is not cu_q:
         _checked(cu_k, torch.int32, n, "cu_k", device)
     if stream is not None:
-        return _on_stream(stream, device, prompt_attention, q, k, v, cu_q, cu_k, causal=causal, scale=scale, want_lse=want_lse, out=out, lse_out=lse_out)
+        return _on_stream(stream, device, prompt_attention, q, k, v, cu_q, cu_k, causal=causal, scale=scale, window=window, sinks=sinks,
+                          want_lse=want_lse, out=out, lse_out=lse_out)
+    if window or sinks:
+        window, sinks = _window(window, sinks)
+        if not causal:
+            raise ValueError("a window looks back: causal must be true")
     total, H, d = qs
     fields = (n[0] - 1, H, ks[1], d, total, ks[0], int(causal), _DTYPES[dtype], q_strides[0], q_strides[1], k_strides[0], k_strides[1])
     try:
@@ -663,9 +743,12 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: to
         _checked(lse_out, torch.float32, (H, total), "lse_out", device)
     elif want_lse:
         lse_out = torch.empty_strided((H, total), (total, 1), dtype=torch.float32, device=device)
-    _launch(device, (_lib or _load()).stream_prompt_attention,
-            (p, q.data_ptr(), k.data_ptr(), v.data_ptr(), cu_q.data_ptr(), cu_k.data_ptr(), scale, out.data_ptr(),
-             None if lse_out is None else lse_out.data_ptr()), None)
+    args = (q.data_ptr(), k.data_ptr(), v.data_ptr(), cu_q.data_ptr(), cu_k.data_ptr(), scale, out.data_ptr(),
+            None if lse_out is None else lse_out.data_ptr())
+    if window:
+        _launch(device, (_lib or _load()).stream_prompt_window_attention, (p, window, sinks, *args), None)
+    else:
+        _launch(device, (_lib or _load()).stream_prompt_attention, (p, *args), None)
     return out if lse_out is None else (out, lse_out)
 
 
@@ -692,6 +775,9 @@ class PagedCache:
             raise ValueError("k and v must be [n_layers, n_pages, page_size, n_kv_heads, d], alike in strides, dtype and device")
         if k.dtype not in _DTYPES:
             raise ValueError("k and v must be float32 or bfloat16")
+        self._keep(k, v, page_table, seq_len, ref_count, k.dtype)
+
+    def _keep(self, k, v, page_table, seq_len, ref_count, dtype) -> None:
         if k.stride(4) != 1:
             raise ValueError("innermost stride must be 1")
         if page_table.dim() != 2:
@@ -704,13 +790,21 @@ class PagedCache:
         self.seq_len = _checked(seq_len, torch.int32, (self.n_slots,), "seq_len", self.device)
         self.ref_count = _checked(ref_count, torch.int32, (self.n_pages,), "ref_count", self.device)
         self.struct = StreamCache(self.n_slots, self.n_pages, self.page_size, self.max_pages, self.n_kv_heads, self.d, self.n_layers,
-                                  _DTYPES[k.dtype], *k.stride()[:4])
+                                  _DTYPES[dtype], *k.stride()[:4])
         n = stream_cache_workspace_bytes(self.struct)
         if n == 0:
             raise StreamError(STREAM_ERR_INVALID_ARG, stream_last_error())
         self._ledger_bytes = n
         self._p = ctypes.byref(self.struct)
         self._decode_bytes = {}  # workspace of decode_attention by query heads
+
+    @property
+    def dtype(self) -> torch.dtype:
+        """Of queries, outputs and new keys and values."""
+        return self.k.dtype
+
+    def _pages(self):
+        return self.k.data_ptr(), self.v.data_ptr()
 
     def _ledger(self):
         return self.page_table.data_ptr(), self.seq_len.data_ptr(), self.ref_count.data_ptr()
@@ -724,12 +818,59 @@ class PagedCache:
         return torch.empty_strided((self._ledger_bytes,), (1,), dtype=torch.uint8, device=self.device)
 
 
+class PagedCache8(PagedCache):
+    """A paged key-value cache in 8 bits; see ``stream_cache8`` in stream.h.
+
+    ``k`` and ``v`` are float8_e4m3fn, ``k_scale`` and ``v_scale`` float32 ``[n_layers, n_pages, page_size / block, n_kv_heads]`` (any strides,
+    both alike): a key is its e4m3 numbers times its block's scale. ``dtype``: that of queries, outputs and new keys and values.
+    The rest, and the ``cache_*`` functions and :func:`decode_attention`, as for :class:`PagedCache`; :func:`new_cache8` makes an empty one."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, page_table: torch.Tensor, seq_len: torch.Tensor,
+                 ref_count: torch.Tensor, *, dtype: torch.dtype = torch.bfloat16):
+        if not k.is_cuda or not v.is_cuda:
+            raise ValueError("k and v must be CUDA tensors (there is no CPU path)")
+        if k.dim() != 5 or v.shape != k.shape or v.stride() != k.stride() or v.device != k.device:
+            raise ValueError("k and v must be [n_layers, n_pages, page_size, n_kv_heads, d], alike in strides and device")
+        if k.dtype is not torch.float8_e4m3fn or v.dtype is not torch.float8_e4m3fn:
+            raise ValueError("k and v must be float8_e4m3fn")
+        if dtype not in _DTYPES:
+            raise ValueError("dtype must be float32 or bfloat16")
+        n, z = k.shape, k_scale.shape
+        if len(z) != 4 or z[:2] != n[:2] or z[2] < 1 or n[2] % z[2] != 0 or z[3] != n[3]:
+            raise ValueError("k_scale must be [n_layers, n_pages, page_size / block, n_kv_heads]")
+        for x in (k_scale, v_scale):
+            if x.dtype is not torch.float32 or x.device != k.device or x.shape != z or x.stride() != k_scale.stride():
+                raise ValueError("k_scale and v_scale must be float32, alike, and on the device of k and v")
+        self._keep(k, v, page_table, seq_len, ref_count, dtype)
+        self.k_scale, self.v_scale, self.block = k_scale, v_scale, n[2] // z[2]
+        self.struct8 = StreamCache8(self.struct, self.block, 0, *k_scale.stride())
+        self._p8, self._dtype = ctypes.byref(self.struct8), dtype
+
+    @property
+    def dtype(self) -> torch.dtype:
+        return self._dtype
+
+    def _pages(self):
+        return self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr()
+
+
 def new_cache(n_slots: int, n_pages: int, page_size: int, max_pages: int, n_kv_heads: int, d: int, *, n_layers: int = 1,
               dtype: torch.dtype = torch.bfloat16, device="cuda") -> PagedCache:
     """An empty cache: all slots empty, all pages free (what the pages hold is not set)."""
     k, v = (torch.empty(n_layers, n_pages, page_size, n_kv_heads, d, dtype=dtype, device=device) for _ in range(2))
     return PagedCache(k, v, torch.full((n_slots, max_pages), -1, dtype=torch.int32, device=k.device),
                       torch.zeros(n_slots, dtype=torch.int32, device=k.device), torch.zeros(n_pages, dtype=torch.int32, device=k.device))
+
+
+def new_cache8(n_slots: int, n_pages: int, page_size: int, max_pages: int, n_kv_heads: int, d: int, *, block: int, n_layers: int = 1,
+               dtype: torch.dtype = torch.bfloat16, device="cuda") -> PagedCache8:
+    """An empty cache in 8 bits whose tokens share a scale in blocks of ``block``, which divides ``page_size``."""
+    if block < 1 or page_size % block != 0:
+        raise ValueError("block must be positive and divide page_size")
+    k, v = (torch.empty(n_layers, n_pages, page_size, n_kv_heads, d, dtype=torch.float8_e4m3fn, device=device) for _ in range(2))
+    k_scale, v_scale = (torch.zeros(n_layers, n_pages, page_size // block, n_kv_heads, device=device) for _ in range(2))
+    return PagedCache8(k, v, k_scale, v_scale, torch.full((n_slots, max_pages), -1, dtype=torch.int32, device=k.device),
+                       torch.zeros(n_slots, dtype=torch.int32, device=k.device), torch.zeros(n_pages, dtype=torch.int32, device=k.device), dtype=dtype)
 
 
 def cache_reserve(cache: PagedCache, n_new: torch.Tensor, stream=None) -> torch.Tensor:
@@ -787,8 +928,11 @@ def cache_copy_pages(cache: PagedCache, moves: CacheMoves, stream=None) -> None:
     n = pairs.shape[0]
     _checked(pairs, torch.int32, (n, 2), "pairs", c.device)
     _checked(info, torch.int32, (4,), "info", c.device)
-    _launch(c.device, (_lib or _load()).stream_cache_copy_pages,
-            (c._p, c.k.data_ptr(), c.v.data_ptr(), pairs.data_ptr(), info.data_ptr() + 4, n), _checked_stream(stream, c.device))
+    args = *c._pages(), pairs.data_ptr(), info.data_ptr() + 4, n
+    if isinstance(c, PagedCache8):
+        _launch(c.device, (_lib or _load()).stream_cache8_copy_pages, (c._p8, *args), _checked_stream(stream, c.device))
+    else:
+        _launch(c.device, (_lib or _load()).stream_cache_copy_pages, (c._p, *args), _checked_stream(stream, c.device))
 
 
 def cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, cu_new: torch.Tensor, *, layer: int = 0,
@@ -796,11 +940,11 @@ def cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, cu_new: tor
     """Writes new tokens' keys and values (``[total, n_kv_heads, d]``, rows ``cu_new[s] .. cu_new[s + 1]`` being slot s's
     last tokens) to the pages of one layer, after :func:`cache_reserve`. With its ``info`` nothing is written if it was
     refused; a caller that has not looked at the info passes it on (the lengths are then as they were, and the last
-    tokens there would be overwritten)."""
+    tokens there would be overwritten). A cache in 8 bits takes them rounded, and their blocks' scales."""
     c, shape, strides = cache, k.shape, k.stride()
     if len(shape) != 3 or shape[1] != c.n_kv_heads or shape[2] != c.d or v.shape != shape or v.stride() != strides:
         raise ValueError("k and v must be [total, n_kv_heads, d], alike in strides")
-    if k.dtype is not c.k.dtype or v.dtype is not c.k.dtype or k.device != c.device or v.device != c.device:
+    if k.dtype is not c.dtype or v.dtype is not c.dtype or k.device != c.device or v.device != c.device:
         raise ValueError("k and v must have the cache's dtype and device")
     if strides[2] != 1:
         raise ValueError("innermost stride must be 1")
@@ -809,28 +953,60 @@ def cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, cu_new: tor
         _checked(info, torch.int32, (4,), "info", c.device)
     if not 0 <= layer < c.n_layers:  # (beyond 32 bits too, of which the call would see the lower ones)
         raise ValueError("no such layer")
-    _launch(c.device, (_lib or _load()).stream_cache_write,
-            (c._p, layer, k.data_ptr(), v.data_ptr(), shape[0], strides[0], strides[1], cu_new.data_ptr(), c.page_table.data_ptr(),
-             c.seq_len.data_ptr(), None if info is None else info.data_ptr(), c.k.data_ptr(), c.v.data_ptr()), _checked_stream(stream, c.device))
+    args = (layer, k.data_ptr(), v.data_ptr(), shape[0], strides[0], strides[1], cu_new.data_ptr(), c.page_table.data_ptr(),
+            c.seq_len.data_ptr(), None if info is None else info.data_ptr(), *c._pages())
+    if isinstance(c, PagedCache8):
+        _launch(c.device, (_lib or _load()).stream_cache8_write, (c._p8, *args), _checked_stream(stream, c.device))
+    else:
+        _launch(c.device, (_lib or _load()).stream_cache_write, (c._p, *args), _checked_stream(stream, c.device))
 
 
-def decode_attention(q: torch.Tensor, cache: PagedCache, *, layer: int = 0, scale: float = 0.0, want_lse: bool = False,
+def cache_read(cache: PagedCache, cu: torch.Tensor, total: int, *, layer: int = 0, out: tuple[torch.Tensor, torch.Tensor] | None = None, stream=None):
+    """Keys and values of a layer out of the pages, packed: rows ``cu[s] .. cu[s + 1]`` (int32 ``[n_slots + 1]``) are slot s's last tokens, as many
+    of them. Returns k and v, ``[total, n_kv_heads, d]``, what :func:`prompt_attention` takes for prompts that come in pieces (or fills
+    ``out``, a pair of them). Rows of no slot are left as they are, tokens without a page are zeros."""
+    c = cache
+    _checked(cu, torch.int32, (c.n_slots + 1,), "cu", c.device)
+    if not 0 <= layer < c.n_layers:
+        raise ValueError("no such layer")
+    if not 0 <= total <= 0x7fffffff:
+        raise ValueError("total must be 0 .. 2^31 - 1")
+    if stream is not None:
+        return _on_stream(stream, c.device, cache_read, c, cu, total, layer=layer, out=out)
+    G, d = c.n_kv_heads, c.d
+    if out is None:
+        k, v = (torch.empty_strided((total, G, d), (G * d, d, 1), dtype=c.dtype, device=c.device) for _ in range(2))
+    else:
+        k, v = (_checked(x, c.dtype, (total, G, d), "out", c.device) for x in out)
+    args = *c._pages(), cu.data_ptr(), total, c.page_table.data_ptr(), c.seq_len.data_ptr(), k.data_ptr(), v.data_ptr()
+    if isinstance(c, PagedCache8):
+        _launch(c.device, (_lib or _load()).stream_cache8_read, (c._p8, layer, *args), None)
+    else:
+        _launch(c.device, (_lib or _load()).stream_cache_read, (c._p, layer, *args), None)
+    return k, v
+
+
+def decode_attention(q: torch.Tensor, cache: PagedCache, *, layer: int = 0, scale: float = 0.0, window: int = 0, sinks: int = 0, want_lse: bool = False,
                      out: torch.Tensor | None = None, lse_out: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
                      stream=None):
-    """Attention of one new token of every slot, q ``[n_slots, H, d]``, over its cached tokens. Returns the output
+    """Attention of one new token of every slot, q ``[n_slots, H, d]``, over its cached tokens (with a ``window``, 0: none, over the last ``window``
+    of them, its own among them, and the first ``sinks``). Returns the output
     ``[n_slots, H, d]``, with ``want_lse`` (or ``lse_out``) also the logarithms of the softmax sums, float32
     ``[n_slots, H]``. ``workspace``: uint8, at least :func:`stream_decode_workspace_bytes`, one per call that can overlap.
     Tokens whose page number is outside the cache are left out without an error here; the call's workspace has a record of them, which only
     one who gave it can look at (:func:`stream_read_stats` of it then raises, status ``STREAM_ERR_DEVICE_CHECK``)."""
     c, shape, strides = cache, q.shape, q.stride()
-    if len(shape) != 3 or shape[0] != c.n_slots or shape[2] != c.d or q.dtype is not c.k.dtype or q.device != c.device:
+    if len(shape) != 3 or shape[0] != c.n_slots or shape[2] != c.d or q.dtype is not c.dtype or q.device != c.device:
         raise ValueError("q must be [n_slots, H, d] with the cache's dtype and device")
     if strides[2] != 1:
         raise ValueError("innermost stride must be 1")
     if not 0 <= layer < c.n_layers:
         raise ValueError("no such layer")
     if stream is not None:
-        return _on_stream(stream, c.device, decode_attention, q, c, layer=layer, scale=scale, want_lse=want_lse, out=out, lse_out=lse_out, workspace=workspace)
+        return _on_stream(stream, c.device, decode_attention, q, c, layer=layer, scale=scale, window=window, sinks=sinks, want_lse=want_lse, out=out,
+                          lse_out=lse_out, workspace=workspace)
+    if window or sinks:
+        window, sinks = _window(window, sinks)
     n, H, d = shape
     if out is None:
         out = torch.empty_strided(shape, (H * d, d, 1), dtype=q.dtype, device=c.device)
@@ -850,7 +1026,12 @@ def decode_attention(q: torch.Tensor, cache: PagedCache, *, layer: int = 0, scal
         need = workspace.numel()
         if workspace.dtype is not torch.uint8 or not workspace.is_contiguous() or workspace.device != c.device:
             raise ValueError("workspace must be a contiguous uint8 tensor on the cache's device")
-    _launch(c.device, (_lib or _load()).stream_decode_attention,
-            (c._p, layer, H, q.data_ptr(), strides[0], strides[1], c.k.data_ptr(), c.v.data_ptr(), c.page_table.data_ptr(),
-             c.seq_len.data_ptr(), scale, out.data_ptr(), None if lse_out is None else lse_out.data_ptr(), workspace.data_ptr(), need), None)
+    tail = (*c._pages(), c.page_table.data_ptr(), c.seq_len.data_ptr(), scale, out.data_ptr(), None if lse_out is None else lse_out.data_ptr(),
+            workspace.data_ptr(), need)
+    if isinstance(c, PagedCache8):
+        _launch(c.device, (_lib or _load()).stream_decode_attention8, (c._p8, layer, H, window, sinks, q.data_ptr(), strides[0], strides[1], *tail), None)
+    elif window:
+        _launch(c.device, (_lib or _load()).stream_decode_window_attention, (c._p, layer, H, window, sinks, q.data_ptr(), strides[0], strides[1], *tail), None)
+    else:
+        _launch(c.device, (_lib or _load()).stream_decode_attention, (c._p, layer, H, q.data_ptr(), strides[0], strides[1], *tail), None)
     return out if lse_out is None else (out, lse_out)
