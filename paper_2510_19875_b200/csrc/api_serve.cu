@@ -114,7 +114,6 @@ stream_status prompt_attention(const stream_prompt *p, int window, int sinks, co
     rc = make_scale(scale, g.d, &g.scale_log2);
     if (rc != STREAM_OK) return rc;
     g.cu_q = cu_q; g.cu_k = cu_k; g.out = out; g.lse = lse_out; g.window = window; g.sinks = sinks;
-    if (window > 0) return launch_prompt_generic(g, p->dtype, q, k, v, st);
     if (prompt_tc_supported(g, p->dtype, q, k, v)) return launch_prompt_tc(g, q, k, v, st);
     if (prompt_mma_supported(g, p->dtype, q, k, v)) return launch_prompt_mma(g, q, k, v, st);
     if (prompt_f32_supported(g, p->dtype, q, k, v)) return launch_prompt_f32(g, q, k, v, st);

@@ -52,7 +52,7 @@ __device__ __forceinline__ void product(float (&c)[4], const unsigned (&ah)[4], 
     mma_tf32(c, ah, bh0, bh1);
 }
 
-template <int D>
+template <int D, bool W>
 __global__ void __launch_bounds__(kThreads, 2) prompt_f32_kernel(const __grid_constant__ PromptGeom g, const float *q, const float *k, const float *v) {
     using F = Form<D>;
     constexpr int kKeys = F::kKeys, kTiles = kKeys / 8, kPieces = D / 4;
@@ -74,15 +74,18 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_f32_kernel(const __grid_co
     auto keys_of = [&](int r) -> int {  // keys that row r of the tile sees (rows behind the last see what it does)
         return g.causal ? min(sk.n, max(0, token_of(min(r, n_rows - 1)) + sk.n - sq.n + 1)) : sk.n;
     };
-    const int most = keys_of(n_rows - 1), warp_most = keys_of(warp * 16 + 15), warp_least = keys_of(warp * 16);
+    Walked wk = {};
+    if constexpr (W) wk = walked_keys<kKeys>(g, tok_base + sk.n - sq.n, sk.n);
+    const int most = keys_of(n_rows - 1), walked = most - wk.gap, warp_most = keys_of(warp * 16 + 15), warp_least = keys_of(warp * 16);
     const int see[2] = {keys_of(warp * 16 + quad), keys_of(warp * 16 + quad + 8)};
     const float *const ks = k + (long long)sk.first * g.ks_t + (long long)kvh * g.ks_h;
     const float *const vs = v + (long long)sk.first * g.ks_t + (long long)kvh * g.ks_h;
     const unsigned q_s = wp::smem_addr(sm.q), k_s = wp::smem_addr(sm.k[0]), v_s = wp::smem_addr(sm.v[0]);
     auto fetch = [&](int j, int buf) {
-        if (j < most) {
+        if (j < walked) {
+            const int j0 = W ? wk.key(j) : j;
             for (int i = tid; i < kKeys * kPieces; i += kThreads) {
-                const int r = i / kPieces, x = i % kPieces, key = j + r;
+                const int r = i / kPieces, x = i % kPieces, key = j0 + r;
                 const bool there = key < sk.n;
                 const long long e = (there ? key * g.ks_t : 0) + x * 4;
                 wp::cp_async16(k_s + (unsigned)((buf * kKeys + r) * F::kRow + x * 4) * 4u, ks + e, there ? 16 : 0);
@@ -105,8 +108,14 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_f32_kernel(const __grid_co
 #pragma unroll
         for (int y = 0; y < 4; ++y) o[x][y] = 0.f;
     float ref[2] = {-CUDART_INF_F, -CUDART_INF_F}, l[2] = {0.f, 0.f};  // of rows quad and quad + 8, in units of log2
-    for (int j = first, buf = 0; j < most; j += stride, buf ^= 1) {
-        fetch(j + stride, buf ^ 1);
+    int low[2] = {0, 0};  // the first keys of their windows
+    if constexpr (W) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r) low[r] = window_begin(g, token_of(min(warp * 16 + quad + 8 * r, n_rows - 1)) + sk.n - sq.n);
+    }
+    for (int jw = first, buf = 0; jw < walked; jw += stride, buf ^= 1) {
+        const int j = W ? wk.key(jw) : jw;
+        fetch(jw + stride, buf ^ 1);
         wp::cp_async_wait<1>();
         __syncthreads();
         if (j < warp_most) {
@@ -142,7 +151,9 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_f32_kernel(const __grid_co
 #pragma unroll
                 for (int y = 0; y < 4; ++y) {
                     sc[n][y] *= g.scale_log2;
-                    if (hidden && j + n * 8 + t * 2 + (y & 1) >= see[y >> 1]) sc[n][y] = -CUDART_INF_F;
+                    const int key = j + n * 8 + t * 2 + (y & 1);
+                    if (hidden && key >= see[y >> 1]) sc[n][y] = -CUDART_INF_F;
+                    if (W && key < low[y >> 1] && key >= g.sinks) sc[n][y] = -CUDART_INF_F;
                     outgrown = outgrown || sc[n][y] - ref[y >> 1] > kOutgrown;  // (the first: infinity)
                 }
             if (__any_sync(0xffffffffu, outgrown)) {
@@ -270,11 +281,11 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_f32_kernel(const __grid_co
     wp::cluster_wait();  // (nobody leaves while its shared memory is read)
 }
 
-template <int D>
-stream_status launch(const PromptGeom &g, const void *q, const void *k, const void *v, cudaStream_t st) {
+template <int D, bool W>
+stream_status launch_form(const PromptGeom &g, const void *q, const void *k, const void *v, cudaStream_t st) {
     const int smem = (int)sizeof(Smem<D>);
     static DeviceFlags done;
-    cudaError_t e = allow_smem_once(prompt_f32_kernel<D>, smem, done);
+    cudaError_t e = allow_smem_once(prompt_f32_kernel<D, W>, smem, done);
     if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(prompt_f32)");
     const long long tiles = most_row_tiles(g, kRows);
     const int n_sm = current_sm_count();
@@ -283,9 +294,14 @@ stream_status launch(const PromptGeom &g, const void *q, const void *k, const vo
     unsigned cluster = 1;
     while (cluster < 8 && tiles * cluster <= n_sm && (long long)g.total_k > (long long)cluster * Form<D>::kKeys) cluster *= 2;
     if (tiles * cluster > 0x7fffffffLL) { set_error("too many rows for one launch"); return STREAM_ERR_UNSUPPORTED; }
-    if (cluster == 1) e = launch_early(prompt_f32_kernel<D>, (unsigned)tiles, kThreads, smem, st, g, (const float *)q, (const float *)k, (const float *)v);
-    else e = launch_clusters(prompt_f32_kernel<D>, (unsigned)tiles * cluster, kThreads, smem, st, cluster, g, (const float *)q, (const float *)k, (const float *)v);
+    if (cluster == 1) e = launch_early(prompt_f32_kernel<D, W>, (unsigned)tiles, kThreads, smem, st, g, (const float *)q, (const float *)k, (const float *)v);
+    else e = launch_clusters(prompt_f32_kernel<D, W>, (unsigned)tiles * cluster, kThreads, smem, st, cluster, g, (const float *)q, (const float *)k, (const float *)v);
     return e == cudaSuccess ? STREAM_OK : cuda_fail(e, "prompt_f32 launch");
+}
+
+template <int D>
+stream_status launch(const PromptGeom &g, const void *q, const void *k, const void *v, cudaStream_t st) {
+    return g.window > 0 ? launch_form<D, true>(g, q, k, v, st) : launch_form<D, false>(g, q, k, v, st);
 }
 
 }  // namespace

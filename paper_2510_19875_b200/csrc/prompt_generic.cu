@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(kThreads) prompt_kernel(PromptGeom g, const T 
     Walked wk = {};
     if constexpr (W) wk = walked_keys<kKeys>(g, (int)(row_base / g.hpg) + shift, sk.n);
     const int walked = most - wk.gap;  // keys without the gap
-    auto key_of = [&](long long j) -> long long { return W && j >= wk.sink_keys ? j + wk.gap : j; };  // of a tile's first
+    auto key_of = [&](long long j) -> long long { return W && j >= wk.sink_keys ? j + wk.gap : j; };
     const T *const qs = q + (long long)sq.first * g.qs_t + (long long)kvh * g.hpg * g.qs_h;
     const T *const ks = k + (long long)sk.first * g.ks_t + (long long)kvh * g.ks_h;
     const T *const vs = v + (long long)sk.first * g.ks_t + (long long)kvh * g.ks_h;

@@ -28,7 +28,7 @@ struct Smem {
     unsigned char k[2][kKeys * Form<D>::kRow], v[2][kKeys * Form<D>::kRow];
 };
 
-template <int D>
+template <int D, bool W>
 __global__ void __launch_bounds__(kThreads, Form<D>::kCtas) prompt_mma_kernel(const __grid_constant__ PromptGeom g, const __nv_bfloat16 *q,
                                                                              const __nv_bfloat16 *k, const __nv_bfloat16 *v) {
     using F = Form<D>;
@@ -48,15 +48,18 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas) prompt_mma_kernel(co
         const int tok = (int)((row_base + min(r, n_rows - 1)) / g.hpg);
         return min(sk.n, max(0, tok + sk.n - sq.n + 1));
     };
-    const int most = keys_of(n_rows - 1), warp_most = keys_of(warp * 16 + 15);
+    Walked wk = {};
+    if constexpr (W) wk = walked_keys<kKeys>(g, (int)(row_base / g.hpg) + sk.n - sq.n, sk.n);
+    const int most = keys_of(n_rows - 1), walked = most - wk.gap, warp_most = keys_of(warp * 16 + 15);
     const __nv_bfloat16 *const qs = q + (long long)sq.first * g.qs_t + (long long)kvh * g.hpg * g.qs_h;
     const __nv_bfloat16 *const ks = k + (long long)sk.first * g.ks_t + (long long)kvh * g.ks_h;
     const __nv_bfloat16 *const vs = v + (long long)sk.first * g.ks_t + (long long)kvh * g.ks_h;
     const unsigned q_s = wp::smem_addr(sm.q), k_s = wp::smem_addr(sm.k[0]), v_s = wp::smem_addr(sm.v[0]);
     auto fetch = [&](int j, int buf) {
-        if (j < most) {
+        if (j < walked) {
+            const int j0 = W ? wk.key(j) : j;
             for (int i = tid; i < kKeys * kPieces; i += kThreads) {
-                const int r = i / kPieces, x = i % kPieces, key = j + r;
+                const int r = i / kPieces, x = i % kPieces, key = j0 + r;
                 const bool there = key < sk.n;
                 const long long e = (there ? key * g.ks_t : 0) + x * 8;
                 const unsigned to = (unsigned)(buf * kKeys * F::kRow + r * F::kRow + x * 16);
@@ -85,11 +88,17 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas) prompt_mma_kernel(co
     float ref[2] = {-CUDART_INF_F, -CUDART_INF_F}, l[2] = {0.f, 0.f};  // of rows quad and quad + 8, in units of log2
     const int see[2] = {keys_of(warp * 16 + quad), keys_of(warp * 16 + quad + 8)};
     const int warp_least = keys_of(warp * 16);
-    for (int j = 0, buf = 0; j < most; j += kKeys, buf ^= 1) {
-        fetch(j + kKeys, buf ^ 1);
+    int low[2] = {0, 0};  // the first keys of their windows
+    if constexpr (W) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r) low[r] = window_begin(g, (int)((row_base + min(warp * 16 + quad + 8 * r, n_rows - 1)) / g.hpg) + sk.n - sq.n);
+    }
+    for (int jw = 0, buf = 0; jw < walked; jw += kKeys, buf ^= 1) {
+        const int j = W ? wk.key(jw) : jw;
+        fetch(jw + kKeys, buf ^ 1);
         wp::cp_async_wait<1>();
         __syncthreads();
-        if (F::kQInRegs && j == 0) {
+        if (F::kQInRegs && jw == 0) {
 #pragma unroll
             for (int x = 0; x < D / 16; ++x) wp::ldmatrix4(q_addr + x * 32, qa[F::kQInRegs ? x : 0]);
         }
@@ -124,7 +133,9 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas) prompt_mma_kernel(co
 #pragma unroll
                 for (int y = 0; y < 4; ++y) {
                     sc[n][y] *= g.scale_log2;
-                    if (hidden && j + n * 8 + (lane & 3) * 2 + (y & 1) >= see[y >> 1]) sc[n][y] = -CUDART_INF_F;
+                    const int key = j + n * 8 + (lane & 3) * 2 + (y & 1);
+                    if (hidden && key >= see[y >> 1]) sc[n][y] = -CUDART_INF_F;
+                    if (W && key < low[y >> 1] && key >= g.sinks) sc[n][y] = -CUDART_INF_F;
                     outgrown = outgrown || sc[n][y] - ref[y >> 1] > kOutgrown;  // (the first: infinity)
                 }
             if (__any_sync(0xffffffffu, outgrown)) {
@@ -196,16 +207,21 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas) prompt_mma_kernel(co
     }
 }
 
-template <int D>
-stream_status launch(const PromptGeom &g, const void *q, const void *k, const void *v, cudaStream_t st) {
+template <int D, bool W>
+stream_status launch_form(const PromptGeom &g, const void *q, const void *k, const void *v, cudaStream_t st) {
     const int smem = (int)sizeof(Smem<D>);
     static DeviceFlags done;
-    cudaError_t e = allow_smem_once(prompt_mma_kernel<D>, smem, done);
+    cudaError_t e = allow_smem_once(prompt_mma_kernel<D, W>, smem, done);
     if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(prompt_mma)");
     const long long tiles = most_row_tiles(g, kRows);
     if (tiles > 0x7fffffffLL) { set_error("too many rows for one launch"); return STREAM_ERR_UNSUPPORTED; }
-    e = launch_early(prompt_mma_kernel<D>, (unsigned)tiles, kThreads, smem, st, g, (const __nv_bfloat16 *)q, (const __nv_bfloat16 *)k, (const __nv_bfloat16 *)v);
+    e = launch_early(prompt_mma_kernel<D, W>, (unsigned)tiles, kThreads, smem, st, g, (const __nv_bfloat16 *)q, (const __nv_bfloat16 *)k, (const __nv_bfloat16 *)v);
     return e == cudaSuccess ? STREAM_OK : cuda_fail(e, "prompt_mma launch");
+}
+
+template <int D>
+stream_status launch(const PromptGeom &g, const void *q, const void *k, const void *v, cudaStream_t st) {
+    return g.window > 0 ? launch_form<D, true>(g, q, k, v, st) : launch_form<D, false>(g, q, k, v, st);
 }
 
 }  // namespace

@@ -84,7 +84,10 @@ struct Item {
     int kvh, tok0;        // the first tile's first token; the second one's is per_tile later
     int n[2];             // key tiles of each; -1: there is no such tile
     int most;             // of both
+    Walked wk;            // (where there is a window)
 };
+template <bool W>
+__device__ __forceinline__ int first_key(const Item &it, int j) { return W ? it.wk.key(j * kKeys) : j * kKeys; }  // of key tile j
 
 // The first sequence whose levels end behind the nth.
 template <class F>
@@ -98,7 +101,7 @@ __device__ __forceinline__ int sequence_of(const Tail<F> *tl, int n_seqs, int nt
     return lo;
 }
 
-template <class F>
+template <bool W, class F>
 __device__ __forceinline__ Item item_at(const Params &P, const Tail<F> *tl, int id) {
     const PromptGeom &g = P.g;
     Item it;
@@ -118,12 +121,13 @@ __device__ __forceinline__ Item item_at(const Params &P, const Tail<F> *tl, int 
     const int pairs = ceil_div(it.s.q_n, 2 * P.per_tile);
     it.tok0 = (pairs - 1 - level) * 2 * P.per_tile;  // late tokens, with the most keys, first
     it.most = 0;
+    it.wk = W ? walked_keys<kKeys>(g, it.tok0 + it.s.k_n - it.s.q_n, it.s.k_n) : Walked{0, 0};
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
         const int t0 = it.tok0 + x * P.per_tile;
         const int last = min(t0 + P.per_tile, it.s.q_n) - 1;
         const int keys = g.causal ? min(it.s.k_n, max(0, last + 1 + it.s.k_n - it.s.q_n)) : it.s.k_n;
-        it.n[x] = t0 < it.s.q_n ? (int)(((long long)keys + kKeys - 1) / kKeys) : -1;
+        it.n[x] = t0 < it.s.q_n ? (int)(((long long)max(0, keys - it.wk.gap) + kKeys - 1) / kKeys) : -1;
         it.most = max(it.most, it.n[x]);
     }
     return it;
@@ -145,7 +149,7 @@ struct Use {
     __device__ __forceinline__ unsigned phase() const { return (u / F::kStages) & 1u; }
 };
 
-template <class F>
+template <bool W, class F>
 __device__ void load_role(const Params &P, const CUtensorMap *tq, const CUtensorMap *tk, const CUtensorMap *tv, Tail<F> *tl,
                           unsigned q_smem, unsigned ring) {
     Use<F> use;
@@ -156,14 +160,14 @@ __device__ void load_role(const Params &P, const CUtensorMap *tq, const CUtensor
             const unsigned bar = smem_u32(raw ? &tl->v_raw[use.stage()] : &tl->full[use.stage()]), dst = ring + use.stage() * F::kTile;
             mbar_arrive_expect_tx(bar, F::kTile);
 #pragma unroll
-            for (int c = 0; c < F::kHalves; ++c) tma_load_4d(dst + c * F::kHalf, map, bar, c * 64, it.s.k_first + j * kKeys, it.kvh, 0);
+            for (int c = 0; c < F::kHalves; ++c) tma_load_4d(dst + c * F::kHalf, map, bar, c * 64, it.s.k_first + first_key<W>(it, j), it.kvh, 0);
         }
         __syncwarp();
         ++use.u;
         return true;
     };
     for (int round = 0, id; (id = nth_item(round)) < tl->n_items; ++round) {
-        const Item it = item_at(P, tl, id);
+        const Item it = item_at<W>(P, tl, id);
         if (it.most == 0) continue;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
@@ -181,27 +185,28 @@ __device__ void load_role(const Params &P, const CUtensorMap *tq, const CUtensor
         }
         if (it.n[0] <= 0 && !kv(it, tk, 0, false)) return;
         for (int j = 0; j < it.most; ++j) {
-            if (!kv(it, tv, j, (long long)(j + 1) * kKeys > it.s.k_n)) return;
+            if (!kv(it, tv, j, (long long)first_key<W>(it, j) + kKeys > it.s.k_n)) return;
             if (j + 1 < it.most && !kv(it, tk, j + 1, false)) return;
         }
     }
 }
 
 // Zeros over the rows of a V tile behind the last key.
-template <class F>
+template <bool W, class F>
 __device__ void zero_role(const Params &P, Tail<F> *tl, unsigned char *ring, int lane) {
     Use<F> use;
     unsigned parity = 0;  // of each stage's barrier
     for (int round = 0, id; (id = nth_item(round)) < tl->n_items; ++round) {
-        const Item it = item_at(P, tl, id);
+        const Item it = item_at<W>(P, tl, id);
         if (it.most == 0) continue;
         use.u += 2 * (unsigned)it.most;
-        if ((long long)it.most * kKeys <= it.s.k_n) continue;
+        const int last_key = first_key<W>(it, it.most - 1);  // (of the tiles the last alone can reach beyond the last key)
+        if ((long long)last_key + kKeys <= it.s.k_n) continue;
         Use<F> last;
         last.u = use.u - 1;
         if (!wait_w(&tl->v_raw[last.stage()], (parity >> last.stage()) & 1u, tl, 1003, kWhileOthersWork)) return;
         parity ^= 1u << last.stage();
-        const int there = it.s.k_n - (it.most - 1) * kKeys;
+        const int there = it.s.k_n - last_key;
         unsigned char *const tile = ring + last.stage() * F::kTile;
 #pragma unroll
         for (int c = 0; c < F::kHalves; ++c)
@@ -213,7 +218,7 @@ __device__ void zero_role(const Params &P, Tail<F> *tl, unsigned char *ring, int
     }
 }
 
-template <class F>
+template <bool W, class F>
 __device__ void mma_role(const Params &P, Tail<F> *tl, unsigned q_smem, unsigned ring, unsigned tmem) {
     Use<F> use;
     unsigned n_q[2] = {0, 0}, n_p[2] = {0, 0};
@@ -245,7 +250,7 @@ __device__ void mma_role(const Params &P, Tail<F> *tl, unsigned q_smem, unsigned
         __syncwarp();
     };
     for (int round = 0, id; (id = nth_item(round)) < tl->n_items; ++round) {
-        const Item it = item_at(P, tl, id);
+        const Item it = item_at<W>(P, tl, id);
         if (it.most == 0) continue;
         if (!wait_w(&tl->full[use.stage()], use.phase(), tl, 1011)) return;
 #pragma unroll
@@ -319,7 +324,7 @@ __device__ __forceinline__ void rescale(unsigned taddr, float f) {
     tmem_st_wait();
 }
 
-template <class F>
+template <bool W, class F>
 __device__ void softmax_role(const Params &P, Tail<F> *tl, unsigned tmem, int t) {
     const PromptGeom &g = P.g;
     const int x = t >> 7, row = t & 127, lane = t & 31, wq = row >> 5;
@@ -338,13 +343,14 @@ __device__ void softmax_role(const Params &P, Tail<F> *tl, unsigned tmem, int t)
     unsigned n_s = 0, n_o = 0;
     __nv_bfloat16 *const out = (__nv_bfloat16 *)g.out;
     for (int round = 0, id; (id = nth_item(round)) < tl->n_items; ++round) {
-        const Item it = item_at(P, tl, id);
+        const Item it = item_at<W>(P, tl, id);
         const int n_tiles = it.n[x];
         if (n_tiles < 0) continue;
         const int tok0 = it.tok0 + x * P.per_tile, tok = tok0 + tok_r;
         // rows that are none see what the last one does, so that they cost nothing
         const int last = min(tok, min(tok0 + P.per_tile, it.s.q_n) - 1);
         const int keys = g.causal ? min(it.s.k_n, max(0, last + 1 + it.s.k_n - it.s.q_n)) : it.s.k_n;
+        const int low = W ? window_begin(g, last + it.s.k_n - it.s.q_n) : 0;
         const bool mine = tok_r < P.per_tile && tok < it.s.q_n;
         float ref = -CUDART_INF_F, l = 0.f;
         for (int j = 0; j < n_tiles; ++j) {
@@ -354,7 +360,17 @@ __device__ void softmax_role(const Params &P, Tail<F> *tl, unsigned tmem, int t)
 #pragma unroll
             for (int c = 0; c < 4; ++c) tmem_ld_32x32_issue(s_addr + c * 32, sr[c >> 1] + (c & 1) * 32);
             tmem_ld_wait();
-            const int n_hi = min(keys - j * kKeys, kKeys);
+            const int base = first_key<W>(it, j), n_hi = min(keys - base, kKeys);
+            if constexpr (W) {  // keys between the sinks and the window
+                const int from = max(g.sinks - base, 0), to = min(low - base, kKeys);
+                if (__any_sync(0xffffffffu, from < to)) {
+#pragma unroll
+                    for (int i = 0; i < 64; ++i) {
+                        sr[0][i] = i >= from && i < to ? 0xff800000u : sr[0][i];
+                        sr[1][i] = i + 64 >= from && i + 64 < to ? 0xff800000u : sr[1][i];
+                    }
+                }
+            }
             if (__any_sync(0xffffffffu, n_hi < kKeys)) {
 #pragma unroll
                 for (int i = 0; i < 64; ++i) {
@@ -449,7 +465,7 @@ __device__ void softmax_role(const Params &P, Tail<F> *tl, unsigned tmem, int t)
     }
 }
 
-template <class F>
+template <class F, bool W>
 __global__ void __launch_bounds__(kThreads, 1)
 prompt_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
                  const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ Params P) {
@@ -524,7 +540,7 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
     // a CTA's sum then, and counting costs more than order gives (us as the sequences lie, and put in order all the same, 28 / 4 heads: 64 prompts of 500 tokens
     // 222, 273; of 100 to 900 311, 351; of 50 to 2000 337, 361; 32 / 8 heads 234, 259; 304, 315; 361, 363).
     const int n_levels = tl->n_levels;
-    const bool sorted = g.n_seqs > 1 && tl->n_items > (int)gridDim.x && n_levels <= kMaxLevels && n_levels * g.n_seqs <= 16 * kThreads;
+    const bool sorted = !W && g.n_seqs > 1 && tl->n_items > (int)gridDim.x && n_levels <= kMaxLevels && n_levels * g.n_seqs <= 16 * kThreads;
     if (tid == 0) tl->sorted = sorted ? 1 : 0;
     for (int i = tid; sorted && i < n_levels; i += kThreads) {
         const int own = sequence_of(tl, g.n_seqs, i), level = i - (own > 0 ? tl->level_end[own - 1] : 0), span2 = 2 * P.per_tile;
@@ -549,11 +565,11 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
     }
     __syncthreads();
     if (warp < 4) {
-        if (warp == 0) load_role<F>(P, &tmap_q, &tmap_k, &tmap_v, tl, smem_u32(smem), smem_u32(ring));
-        else if (warp == 1) mma_role<F>(P, tl, smem_u32(smem), smem_u32(ring), tmem);
-        else if (warp == 2) zero_role<F>(P, tl, ring, lane);
+        if (warp == 0) load_role<W>(P, &tmap_q, &tmap_k, &tmap_v, tl, smem_u32(smem), smem_u32(ring));
+        else if (warp == 1) mma_role<W>(P, tl, smem_u32(smem), smem_u32(ring), tmem);
+        else if (warp == 2) zero_role<W>(P, tl, ring, lane);
     } else {
-        softmax_role<F>(P, tl, tmem, tid - 128);
+        softmax_role<W>(P, tl, tmem, tid - 128);
     }
     __syncwarp();
     leave(&tl->abort_flag, tmem, warp == 1);
@@ -572,13 +588,13 @@ stream_status make_map_q(CUtensorMap *map, const PromptGeom &g, const void *q, i
     return STREAM_OK;
 }
 
-template <class F>
+template <class F, bool W>
 stream_status launch(const PromptGeom &g, const void *q, const void *k, const void *v, cudaStream_t st) {
     Params P;
     P.g = g;
     P.per_tile = kRows / g.hpg;
     const long long fit = kKvInL2 / ((long long)g.total_k * F::D * 4);
-    P.heads = (int)(fit < 1 ? 1 : fit > g.G ? g.G : fit);
+    P.heads = W || fit > g.G ? g.G : (int)(fit < 1 ? 1 : fit);
     CUtensorMap tq, tk, tv;
     stream_status rc = make_map_q(&tq, g, q, P.per_tile);
     if (rc != STREAM_OK) return rc;
@@ -589,7 +605,7 @@ stream_status launch(const PromptGeom &g, const void *q, const void *k, const vo
     const int smem = (2 + F::kStages) * F::kTile + (int)sizeof(Tail<F>) + 1024;
     static_assert((2 + F::kStages) * F::kTile + (int)sizeof(Tail<F>) + 1024 <= 232448, "what a CTA may have");
     static DeviceFlags done;
-    cudaError_t e = allow_smem_once(prompt_tc_kernel<F>, smem, done);
+    cudaError_t e = allow_smem_once(prompt_tc_kernel<F, W>, smem, done);
     if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(prompt_tc)");
     const int n_sm = current_sm_count();
     if (n_sm <= 0) { set_error("cannot read the SM count of the current device"); return STREAM_ERR_CUDA; }
@@ -598,7 +614,7 @@ stream_status launch(const PromptGeom &g, const void *q, const void *k, const vo
         P.g.cu_q = g.cu_q + s0;
         P.g.cu_k = g.cu_k + s0;
         const long long items = ((long long)g.total_q / (2 * P.per_tile) + P.g.n_seqs) * g.G;  // at most
-        e = launch_early(prompt_tc_kernel<F>, (unsigned)(items < n_sm ? items : n_sm), kThreads, smem, st, tq, tk, tv, P);
+        e = launch_early(prompt_tc_kernel<F, W>, (unsigned)(items < n_sm ? items : n_sm), kThreads, smem, st, tq, tk, tv, P);
         if (e != cudaSuccess) return cuda_fail(e, "prompt_tc launch");
     }
     return STREAM_OK;
@@ -613,7 +629,8 @@ bool prompt_tc_supported(const PromptGeom &g, int dtype, const void *q, const vo
 }
 
 stream_status launch_prompt_tc(const PromptGeom &g, const void *q, const void *k, const void *v, cudaStream_t st) {
-    return g.d == 128 ? launch<Form<128>>(g, q, k, v, st) : launch<Form<64>>(g, q, k, v, st);
+    if (g.window > 0) return g.d == 128 ? launch<Form<128>, true>(g, q, k, v, st) : launch<Form<64>, true>(g, q, k, v, st);
+    return g.d == 128 ? launch<Form<128>, false>(g, q, k, v, st) : launch<Form<64>, false>(g, q, k, v, st);
 }
 
 stream_status read_prompt_status(unsigned int out[2], cudaStream_t st) {

@@ -22,12 +22,15 @@ struct PromptGeom {
 };
 
 // What a tile of rows walks of the keys where there is a window, in tiles of kKeys: those of the sinks, and behind a gap all from the first key that
-// the first row's window has. (Positions below 0 see nothing.)
-struct Walked { int sink_keys, gap; };  // keys in front of the gap, keys of the gap: multiples of kKeys
+// the first row's window has. (Positions below 0 see nothing. Counted without the gap, a tile's first key is a multiple of kKeys.)
+struct Walked {
+    int sink_keys, gap;  // keys in front of the gap, a multiple of kKeys; keys of the gap
+    __device__ __forceinline__ int key(int walked) const { return walked < sink_keys ? walked : walked + gap; }
+};
 template <int kKeys>
 __device__ __forceinline__ Walked walked_keys(const PromptGeom &g, int first_pos, int n_keys) {
-    const int low = max(0, max(first_pos, 0) - g.window + 1) / kKeys, sink = (min(g.sinks, n_keys) + kKeys - 1) / kKeys;
-    return {sink * kKeys, max(0, low - sink) * kKeys};
+    const int low = max(0, max(first_pos, 0) - g.window + 1), sinks = (min(g.sinks, n_keys) + kKeys - 1) / kKeys * kKeys;
+    return {sinks, max(0, low - sinks)};
 }
 // The first key of a position's window.
 __device__ __forceinline__ int window_begin(const PromptGeom &g, int pos) { return max(0, max(pos, 0) - g.window + 1); }

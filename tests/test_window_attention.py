@@ -60,6 +60,15 @@ def test_more_items_than_ctas(S, H, G, d, lens):
     run(S, q, k, v, cu_q, cu_k, 200, 3)
 
 
+@pytest.mark.parametrize("d,dtype", [(128, BF16), (64, BF16), (256, BF16), (64, F32), (256, F32)])
+def test_a_window_as_long_as_the_sequences_is_the_dense_call(S, d, dtype):
+    q, k, v, cu_q, cu_k = inputs(4, 2, d, [300, 40], [300, 70], dtype)
+    dense = S.prompt_attention(q, k, v, ints(cu_q), ints(cu_k), want_lse=True)
+    for window, sinks in ((300, 0), (1, 300), (2 ** 31 - 1, 0)):
+        out, lse = S.prompt_attention(q, k, v, ints(cu_q), ints(cu_k), window=window, sinks=sinks, want_lse=True)
+        assert torch.equal(out, dense[0]) and torch.equal(lse, dense[1])
+
+
 @pytest.mark.parametrize("d,dtype", [(128, BF16), (64, BF16), (32, BF16), (64, F32), (256, F32)])
 def test_logits_that_outgrow_their_reference_and_late_first_keys(S, d, dtype):
     q, k, v, cu_q, cu_k = inputs(4, 2, d, [700], [700], dtype, sink=False)
