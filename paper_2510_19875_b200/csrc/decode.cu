@@ -65,7 +65,7 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(Args A, int vec) {
         const int s = sg.slot, nh = sg.heads, h0 = sg.h0, key0 = sg.key0, key_end = sg.key_end;
         const int n_tiles = (key_end - key0 + F::kKeys - 1) / F::kKeys;
         const int32_t *const row = c.table + (long long)s * c.max_pages;
-        const Seen seen = seen_of<W>(A.a, s);
+        const Seen seen = seen_of<W, kUnit64>(A.a, s);
         auto page_of = [&](int tile) -> int {  // of this thread's key
             const int walked = key0 + tile * F::kKeys + tid, key = W ? seen.key(walked) : walked;
             if (walked >= key_end || (W && !seen.sees(key))) return -1;
@@ -203,7 +203,7 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(Args A, int vec) {
         }
         float *const part = part_of(A, (int)blockIdx.x, n_parts);
         if (!sg.whole) {
-            if (sg.key0 == 0) left = {pieces_of(sg, mine), n_parts, sg.heads, 0u, (long long)sg.slot * A.a.H + sg.h0, 0ll};
+            if (sg.key0 == 0) left = {pieces_of(sg.owner_end, mine), n_parts, sg.heads, 0u, (long long)sg.slot * A.a.H + sg.h0, 0ll};
             ++n_parts;
         }
 #pragma unroll
@@ -349,7 +349,7 @@ constexpr size_t kLeftBytes = (kMaxGrid * sizeof(Left) + 255) & ~(size_t)255;
 
 namespace decode {
 
-Args args_of(const DecodeCall &a, void *workspace, int n_sm) {
+Args args_of(const DecodeCall &a, void *workspace, int n_sm, int unit, int open) {
     Args A;
     A.a = a;
     A.chunks = (a.hpg + kMaxHeads - 1) / kMaxHeads;
@@ -357,9 +357,10 @@ Args args_of(const DecodeCall &a, void *workspace, int n_sm) {
     A.header = (WorkspaceHeader *)workspace;
     A.left = (Left *)((char *)workspace + sizeof(WorkspaceHeader));
     A.parts = (float *)((char *)A.left + kLeftBytes);
+    A.warp_parts = A.parts + (size_t)kMaxGrid * 2 * kMaxHeads * (a.c.d + 2);
     long long keys = (long long)a.c.max_pages * a.c.page;  // of a slot, at most
-    if (a.window > 0) keys = std::min(keys, ((long long)a.window + kUnit - 1) + ((long long)a.sinks + kUnit - 1));
-    const long long most = (long long)a.c.n_slots * A.per_slot * ((keys + kUnit - 1) / kUnit + kOpen);
+    if (a.window > 0) keys = std::min(keys, (long long)a.window + a.sinks + 2 * (unit - 1));
+    const long long most = (long long)a.c.n_slots * A.per_slot * ((keys + unit - 1) / unit + open);
     const int want = 2 * n_sm < kMaxGrid ? 2 * n_sm : kMaxGrid;
     A.grid = (int)(most < want ? most : want);
     return A;
@@ -373,7 +374,7 @@ cudaError_t launch_joins(const Args &A, int dtype, cudaStream_t st) {
 }  // namespace decode
 
 size_t decode_workspace_bytes(const CacheGeom &c) {
-    return sizeof(WorkspaceHeader) + kLeftBytes + (size_t)kMaxGrid * 2 * kMaxHeads * (c.d + 2) * sizeof(float);
+    return sizeof(WorkspaceHeader) + kLeftBytes + (size_t)kMaxGrid * (2 + kThreads / 32) * kMaxHeads * (c.d + 2) * sizeof(float);
 }
 
 stream_status launch_decode(const DecodeCall &a, int dtype, void *workspace, cudaStream_t st) {

@@ -7,7 +7,14 @@ namespace stream {
 namespace decode {
 
 constexpr int kThreads = 128;
-constexpr int kUnit = 64;        // keys
+// The kernels that have the cache's own numbers deal units of 64 keys.
+constexpr int kUnit64 = 64;
+
+// A segment costs a CTA kOpen64 units beside its own: the way from one owner's last key to the next one's first, the warps' meeting and
+// the output. So an owner takes up as many places more in the row that is dealt out, in front of its units. (Without them a CTA with
+// many short slots was the last by far: four slots of up to 131072 tokens, 32 / 8 heads: 80 us most CTAs, 126 the last.) With 1, 2, 3, 4, us: 64 slots of up to
+// 8192 tokens 54.2, 46.4, 45.8, 47.3; the four 96.3, 88.5, 88.5, 88.6; nine of up to 5003, fp32, 21.0, 20.0, 20.0, 19.8; slots of some tokens 7 to 10 with any.
+constexpr int kOpen64 = 2;
 constexpr int kMaxHeads = 16;    // query heads of a segment (a larger group is walked in several segments)
 constexpr int kMaxGrid = 320;
 
@@ -27,24 +34,19 @@ struct Args {
     int per_slot;                // owners of a slot's units: (kv head, up to 16 of its query heads)
     int chunks;                  // owners of a kv head
     float *parts;                // [grid][2][kMaxHeads * (d + 2)]: m, l, O
+    float *warp_parts;           // (decode8.cu) [grid][warps][kMaxHeads * (d + 2)]
     struct Left *left;           // [grid]
     WorkspaceHeader *header;
-    int q_vec;                   // (decode_warp.cu) q is read in pieces of 16 bytes
+    int q_vec;                   // q is read in pieces (decode_warp.cu: of 16 bytes; decode8.cu: of four elements)
 };
 
 // The arguments that follow from the call, and the grid at most; the joins' launch.
-Args args_of(const DecodeCall &a, void *workspace, int n_sm);
+Args args_of(const DecodeCall &a, void *workspace, int n_sm, int unit = kUnit64, int open = kOpen64);
 cudaError_t launch_joins(const Args &A, int dtype, cudaStream_t st);
 
 // Rows of 16-byte pieces, up to 512 bytes. May lower A.grid.
 bool warp_supported(const DecodeCall &a, int dtype);
 cudaError_t launch_warp(Args &A, int dtype, int n_sm, cudaStream_t st);
-
-// A segment costs a CTA kOpen units beside its own: the way from one owner's last key to the next one's first, the warps' meeting and
-// the output. So an owner takes up as many places more in the row that is dealt out, in front of its units. (Without them a CTA with
-// many short slots was the last by far: four slots of up to 131072 tokens, 32 / 8 heads: 80 us most CTAs, 126 the last.) With 1, 2, 3, 4, us: 64 slots of up to
-// 8192 tokens 54.2, 46.4, 45.8, 47.3; the four 96.3, 88.5, 88.5, 88.6; nine of up to 5003, fp32, 21.0, 20.0, 20.0, 19.8; slots of some tokens 7 to 10 with any.
-constexpr int kOpen = 2;
 
 // Which keys of a slot are walked where there is a window (W): the units of the sinks, then, behind a gap, those from the window's first key on. A
 // segment counts its keys without the gap; units are whole on both sides of it, so that a tile's keys lie as they do without.
@@ -56,7 +58,7 @@ struct Seen {
     __device__ __forceinline__ int key(int walked) const { return walked < sink_keys ? walked : walked + gap; }
     __device__ __forceinline__ bool sees(int key) const { return key < sinks || key >= low; }
 };
-template <bool W>
+template <bool W, int kUnit>
 __device__ __forceinline__ Seen seen_of(const DecodeCall &a, int s) {
     const int n = tokens_of(a.c, s);
     if constexpr (!W) return {n, n, 0, n, 0};
@@ -65,27 +67,27 @@ __device__ __forceinline__ Seen seen_of(const DecodeCall &a, int s) {
 }
 
 // Sums over the slots, by whole warps (the same in every lane).
-template <bool W>
+template <bool W, int kUnit, int kOpen>
 __device__ __forceinline__ int places_of(const DecodeCall &a, int s) {
-    const int u = s < a.c.n_slots ? (seen_of<W>(a, s).n + kUnit - 1) / kUnit : 0;
+    const int u = s < a.c.n_slots ? (seen_of<W, kUnit>(a, s).n + kUnit - 1) / kUnit : 0;
     return u > 0 ? u + kOpen : 0;
 }
-template <bool W>
+template <bool W, int kUnit = kUnit64, int kOpen = kOpen64>
 __device__ __forceinline__ long long all_places(const Args &A, int lane) {
     long long sum = 0;
-    for (int s = lane; s < A.a.c.n_slots; s += 32) sum += places_of<W>(A.a, s);
+    for (int s = lane; s < A.a.c.n_slots; s += 32) sum += places_of<W, kUnit, kOpen>(A.a, s);
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
     return sum * A.per_slot;
 }
 // Whose a place is: the slot, where that slot's places begin, how many it has for one owner. `from`: one at or before it.
 struct Place { int slot, n; long long first; };
-template <bool W>
+template <bool W, int kUnit, int kOpen>
 __device__ __forceinline__ Place place_of(const Args &A, long long at, int lane, Place from) {
     const CacheGeom &c = A.a.c;
     long long sum = from.first;
     for (int s0 = from.slot; s0 < c.n_slots; s0 += 32) {
-        const int n = places_of<W>(A.a, s0 + lane);
+        const int n = places_of<W, kUnit, kOpen>(A.a, s0 + lane);
         long long incl = n;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -118,30 +120,32 @@ struct Segment {
     int key0, key_end;   // keys of the slot (none where key0 = key_end), as Seen counts them
     bool whole;          // all of them
 };
-template <bool W>
+template <bool W, int kUnit, int kOpen>
 __device__ __forceinline__ Segment segment_of(const Args &A, const Place &pl, long long at, long long end) {
     Segment sg;
-    const int owner = (int)((at - pl.first) / pl.n), chunk = owner % A.chunks;
+    const long long ahead = at - pl.first;  // (a division of 64 bits is hundreds of cycles)
+    const int owner = ahead >> 32 == 0 ? (int)((unsigned)ahead / (unsigned)pl.n) : (int)(ahead / pl.n);
+    const int chunk = A.chunks == 1 ? 0 : owner % A.chunks;
+    sg.kvh = A.chunks == 1 ? owner : owner / A.chunks;
     const long long first = pl.first + (long long)owner * pl.n;
     sg.owner_end = first + pl.n;
     sg.next = min(sg.owner_end, end);
     sg.slot = pl.slot;
-    sg.kvh = owner / A.chunks;
     sg.h0 = sg.kvh * A.a.hpg + chunk * kMaxHeads;
     sg.heads = min(kMaxHeads, A.a.hpg - chunk * kMaxHeads);
     const int unit0 = (int)max(at - first - kOpen, 0ll), unit1 = (int)max(sg.next - first - kOpen, 0ll);
     sg.key0 = unit0 * kUnit;
-    sg.key_end = (int)min((long long)seen_of<W>(A.a, pl.slot).n, (long long)unit1 * kUnit);
+    sg.key_end = (int)min((long long)seen_of<W, kUnit>(A.a, pl.slot).n, (long long)unit1 * kUnit);
     if (unit0 == unit1) sg.key_end = sg.key0;
     sg.whole = unit0 == 0 && unit1 == pl.n - kOpen;
     return sg;
 }
 // The first segment with keys at or behind place `at` of a share that ends at `end`; pl: a place at or before it. next = -1: none.
-template <bool W>
+template <bool W, int kUnit = kUnit64, int kOpen = kOpen64>
 __device__ __forceinline__ Segment open_segment(const Args &A, long long at, long long end, int lane, Place &pl) {
     while (at < end) {
-        pl = place_of<W>(A, at, lane, pl);
-        const Segment sg = segment_of<W>(A, pl, at, end);
+        if (pl.n == 0 || at >= pl.first + (long long)pl.n * A.per_slot) pl = place_of<W, kUnit, kOpen>(A, at, lane, pl);
+        const Segment sg = segment_of<W, kUnit, kOpen>(A, pl, at, end);
         if (sg.key_end > sg.key0) return sg;
         at = sg.next;
     }
@@ -165,9 +169,7 @@ __device__ __forceinline__ void write_empty_slots(const Args &A) {
 }
 
 // The n of Left for a segment that begins with its owner's first key and is not all of it.
-__device__ __forceinline__ int pieces_of(const Segment &sg, const Share &mine) {
-    return (int)((sg.owner_end - 1) / mine.per) - (int)blockIdx.x + 1;
-}
+__device__ __forceinline__ int pieces_of(long long owner_end, const Share &mine) { return (int)((owner_end - 1) / mine.per) - (int)blockIdx.x + 1; }
 // `bad`: of every thread. The other fields are thread 0's.
 __device__ __forceinline__ void leave_to_joins(const Args &A, Left left, unsigned bad) {
     __shared__ unsigned any;

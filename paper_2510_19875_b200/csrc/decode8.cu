@@ -2,7 +2,7 @@
 //
 //     x_t = scale log2(e) sk_t (q . k8_t),     out = sum_t 2^(x_t - m) sv_t v8_t / sum_t 2^(x_t - m)
 //
-// The keys of all slots and heads are dealt to the CTAs as in decode.cu, and a warp walks its tiles of 16 keys alone, as in decode_warp.cu. Half the bytes
+// The keys of all slots and heads are dealt to the CTAs as in decode.cu, and a warp walks its tiles of 32 keys alone, as in decode_warp.cu. Half the bytes
 // a key leave half the time for it, so that the products turn: the keys are the rows of S^T = K Q^T and V's channels those of O^T = V^T P^T, the
 // query heads, of which a kv head has mostly eight or fewer, the eight columns (16 heads: two products from the same K and V). e4m3
 // is exact in fp16. A lane's four bytes of K are four channels side by side of one key: Q's channels are taken in that order. Two rows of V
@@ -21,30 +21,43 @@ namespace {
 
 using namespace decode;
 
-constexpr int kStep = 16;            // keys of a warp's tile
+constexpr int kWarps = kThreads / 32;
+constexpr int kStep = 32;            // keys of a warp's tile: one a lane where pages are looked up. And the keys of a unit
+// What a segment costs a warp beside its keys, in units.
+#ifndef OPEN8
+#define OPEN8 2
+#endif
+constexpr int kOpen = OPEN8;
 constexpr float kOutgrown = 30.f;    // log2: of the sum's reference
 constexpr float kTop = 14.f;         // log2: a weight for the product at its reference
 
 template <class T, int D, int N>
 struct Form {
     static constexpr bool kPair = sizeof(T) == 4;               // two fp16 numbers an operand
+    static constexpr int kParts = kPair ? 2 : 1;
     static constexpr int kPieces = D / 16;                      // of 16 bytes of a row, and steps of K Q^T
     static constexpr int kTile = kStep * D;                     // bytes
     static constexpr int kPlace = 2 * kTile + 2 * kStep * 4;    // K, V, the keys' scales
-    static constexpr int kStages = D == 128 ? (N == 1 ? 5 : 4) : D == 256 ? 4 : 8;
-    static constexpr int kCtas = D == 256 ? 1 : 2;              // of an SM
     static constexpr int kHeads = 8 * N;
-    static constexpr bool kQInRegs = D * N * (kPair ? 2 : 1) <= 256;
-    static constexpr int kLane = D >= 32 ? D / 32 : 1;          // channels of a head's q a lane
+    static constexpr bool kQInRegs = kParts * N * kPieces <= 16;
+    static constexpr int kStages = D == 256 ? (kQInRegs ? 3 : 2) : D == 128 ? 3 : D == 64 ? 5 : 8;
+    static constexpr int kCtas = D == 256 || (D == 128 && !kQInRegs) ? 1 : 2;  // of an SM
+    static constexpr int kLeave = (2 * kMaxHeads + kHeads * D) * 4;    // m, l, O
+    static_assert(kLeave <= kStages * kPlace, "a warp's last piece in its ring");
+};
+// A piece of an owner that a warp leaves to its CTA.
+struct Piece {
+    const float *at;      // m, l, O as in Args::parts
+    long long owner_end;
+    int slot, h0, heads;  // slot < 0: there is no piece
+    int starts, ends;     // with the owner's first key, its last
 };
 template <class T, int D, int N>
 struct Smem {
     using F = Form<T, D, N>;
-    unsigned char ring[kThreads / 32][F::kStages * F::kPlace];
-    float o[kThreads / 32][F::kHeads * D];
-    __half q[F::kPair ? 2 : 1][F::kHeads * D];   // the rest of each number behind
-    float unit[F::kHeads];                       // what a logit of this q is worth
-    float m[kThreads / 32][F::kHeads], l[kThreads / 32][F::kHeads];
+    unsigned char ring[kWarps][F::kStages * F::kPlace];
+    uint2 q[kWarps][F::kQInRegs ? 1 : F::kParts * F::kPieces * N * 32];  // what a lane multiplies with
+    Piece piece[2 * kWarps];
 };
 
 // Byte of piece x (16 bytes) of row r in a tile: turned, so that eight rows' same piece touch every bank.
@@ -89,105 +102,166 @@ __device__ __forceinline__ void cp_async4_or_zero(unsigned dst, const void *src,
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 
-// What a warp gathers of a segment. A lane (g = lane / 4, t = lane % 4) has the heads 8 n + 2 t and 8 n + 2 t + 1, of a tile the keys g and g + 8, and of O
-// the channels 16 c + 2 g and 16 c + 2 g + 1.
+// Four channels of a query head, as they lie in memory.
+template <class T>
+struct Four { unsigned w[sizeof(T)]; };
+template <class T>
+__device__ __forceinline__ Four<T> load_four(const T *p, bool vec) {
+    Four<T> r;
+    if constexpr (sizeof(T) == 4) {
+        const uint4 x = vec ? *reinterpret_cast<const uint4 *>(p)
+                            : make_uint4(__float_as_uint(p[0]), __float_as_uint(p[1]), __float_as_uint(p[2]), __float_as_uint(p[3]));
+        r.w[0] = x.x; r.w[1] = x.y; r.w[2] = x.z; r.w[3] = x.w;
+    } else {
+        const uint2 x = vec ? *reinterpret_cast<const uint2 *>(p) : wp::load4(p);
+        r.w[0] = x.x; r.w[1] = x.y;
+    }
+    return r;
+}
+template <class T>
+__device__ __forceinline__ void widen(const Four<T> &f, float (&x)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) x[i] = __uint_as_float(f.w[i]);
+        else x[i] = __uint_as_float(i & 1 ? f.w[i >> 1] & 0xffff0000u : f.w[i >> 1] << 16);
+    }
+}
+
+// What a warp gathers of a segment. A lane (g = lane / 4, t = lane % 4) has the heads 8 n + 2 t and 8 n + 2 t + 1, of a tile the keys g + 8 i, and of O
+// the channels 16 c + 2 g and 16 c + 2 g + 1. As a column of K Q^T it has the channels 16 c + 4 t ... of the heads 8 n + g.
 template <class T, int D, int N>
 struct Walk {
     using F = Form<T, D, N>;
-    static constexpr int kParts = F::kPair ? 2 : 1;
+    static constexpr int kParts = F::kParts;
     unsigned q[kParts][F::kQInRegs ? F::kPieces : 1][N][2];
     float o[F::kPieces][N][4], unit[N][2], ref[N][2], top[N][2], l[N][2];  // ref: of the sum, top: of the weights for the product; units of log2
 
-    __device__ __forceinline__ void load_q(const Smem<T, D, N> &sm, int part, int c, int n, int lane, unsigned (&r)[2]) const {
-        const uint2 x = *reinterpret_cast<const uint2 *>(&sm.q[part][(8 * n + (lane >> 2)) * D + 16 * c + 4 * (lane & 3)]);
-        r[0] = x.x;
-        r[1] = x.y;
-    }
-    __device__ __forceinline__ void begin(const Smem<T, D, N> &sm, float scale_log2, int lane) {
-        if constexpr (F::kQInRegs) {
+    __device__ __forceinline__ void begin(Smem<T, D, N> &sm, int warp, const Four<T> (&raw)[F::kPieces][N], float scale_log2, int lane) {
 #pragma unroll
-            for (int p = 0; p < kParts; ++p)
+        for (int n = 0; n < N; ++n) {  // q times a power of two, in [2^14, 2^15) at its largest
+            float most = 0.f, x[4];
 #pragma unroll
-                for (int c = 0; c < F::kPieces; ++c)
+            for (int c = 0; c < F::kPieces; ++c) {
+                widen(raw[c][n], x);
+                most = fmaxf(most, fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(x[2]), fabsf(x[3]))));
+            }
+            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+            const int up = min(max(141 - (int)(__float_as_uint(most) >> 23), -114), 126);
+            const float f = __uint_as_float((unsigned)(up + 127) << 23);
 #pragma unroll
-                    for (int n = 0; n < N; ++n) load_q(sm, p, c, n, lane, q[p][c][n]);
-        }
+            for (int c = 0; c < F::kPieces; ++c) {
+                widen(raw[c][n], x);
+                unsigned r[kParts][2];
 #pragma unroll
-        for (int n = 0; n < N; ++n) {
+                for (int y = 0; y < 2; ++y) {
+                    const float a = x[2 * y] * f, b = x[2 * y + 1] * f;
+                    r[0][y] = pack(a, b);
+                    if constexpr (F::kPair) {
+                        const float2 h = __half22float2(*reinterpret_cast<const __half2 *>(&r[0][y]));
+                        r[kParts - 1][y] = pack(a - h.x, b - h.y);
+                    }
+                }
+#pragma unroll
+                for (int p = 0; p < kParts; ++p) {
+                    if constexpr (F::kQInRegs) {
+                        q[p][F::kQInRegs ? c : 0][n][0] = r[p][0];
+                        q[p][F::kQInRegs ? c : 0][n][1] = r[p][1];
+                    } else {
+                        sm.q[warp][F::kQInRegs ? 0 : ((p * F::kPieces + c) * N + n) * 32 + lane] = make_uint2(r[p][0], r[p][1]);
+                    }
+                }
+            }
+            const float worth = scale_log2 / f;  // a logit of this q
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                unit[n][y] = __shfl_sync(0xffffffffu, worth, 8 * (lane & 3) + 4 * y);
+                ref[n][y] = top[n][y] = -CUDART_INF_F;
+                l[n][y] = 0.f;
+            }
 #pragma unroll
             for (int c = 0; c < F::kPieces; ++c)
 #pragma unroll
                 for (int y = 0; y < 4; ++y) o[c][n][y] = 0.f;
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-                unit[n][y] = sm.unit[8 * n + 2 * (lane & 3) + y] * scale_log2;
-                ref[n][y] = top[n][y] = -CUDART_INF_F;
-                l[n][y] = 0.f;
-            }
         }
     }
 
-    // The tile at shared-memory address kt: K, V behind it, and the keys' scales at z.
-    __device__ __forceinline__ void step(const Smem<T, D, N> &sm, unsigned kt, const float *z, int lane) {
+    // The tile at shared-memory address kt: K, V behind it, and the keys' scales at z. Keys g, g + 8, g + 16 and g + 24 of it are this lane's.
+    __device__ __forceinline__ void step(const Smem<T, D, N> &sm, int warp, unsigned kt, const float *z, int lane) {
         const unsigned vt = kt + F::kTile;
-        const int r8 = (lane >> 3 & 1) * 8 + (lane & 7), half = lane >> 4;  // ldmatrix: this lane's row, and which of two pieces
-        float s[N][4];
+        float s[N][2][4];
 #pragma unroll
         for (int n = 0; n < N; ++n)
 #pragma unroll
-            for (int y = 0; y < 4; ++y) s[n][y] = 0.f;
+            for (int y = 0; y < 8; ++y) s[n][y >> 2][y & 3] = 0.f;
 #pragma unroll
-        for (int c = 0; c < F::kPieces; c += 2) {
+        for (int c = 0; c < F::kPieces; ++c) {
             unsigned w[4];
-            wp::ldmatrix4(kt + piece_at<D>(r8, F::kPieces > 1 ? c + half : 0), w);
+            wp::ldmatrix4(kt + piece_at<D>(lane, c), w);
+            unsigned b[kParts][N][2];
 #pragma unroll
-            for (int i = 0; i < (F::kPieces > 1 ? 2 : 1); ++i) {
+            for (int p = 0; p < kParts; ++p)
+#pragma unroll
+                for (int n = 0; n < N; ++n) {
+                    if constexpr (F::kQInRegs) {
+                        b[p][n][0] = q[p][F::kQInRegs ? c : 0][n][0];
+                        b[p][n][1] = q[p][F::kQInRegs ? c : 0][n][1];
+                    } else {
+                        const uint2 x = sm.q[warp][F::kQInRegs ? 0 : ((p * F::kPieces + c) * N + n) * 32 + lane];
+                        b[p][n][0] = x.x;
+                        b[p][n][1] = x.y;
+                    }
+                }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {  // 16 keys
                 const unsigned a0 = widen_low(w[2 * i]), a2 = widen_high(w[2 * i]), a1 = widen_low(w[2 * i + 1]), a3 = widen_high(w[2 * i + 1]);
 #pragma unroll
                 for (int n = 0; n < N; ++n) {
                     float part[4] = {0.f, 0.f, 0.f, 0.f};
-                    float(&to)[4] = F::kPair ? part : s[n];
+                    float(&to)[4] = F::kPair ? part : s[n][i];
 #pragma unroll
-                    for (int p = kParts - 1; p >= 0; --p) {  // (the small parts first)
-                        unsigned b[2];
-                        if constexpr (F::kQInRegs) {
-                            b[0] = q[p][F::kQInRegs ? c + i : 0][n][0];
-                            b[1] = q[p][F::kQInRegs ? c + i : 0][n][1];
-                        } else {
-                            load_q(sm, p, c + i, n, lane, b);
-                        }
-                        mma_f16(to, a0, a1, a2, a3, b[0], b[1]);
-                    }
+                    for (int p = kParts - 1; p >= 0; --p) mma_f16(to, a0, a1, a2, a3, b[p][n][0], b[p][n][1]);  // (the small parts first)
                     if constexpr (F::kPair) {
 #pragma unroll
-                        for (int y = 0; y < 4; ++y) s[n][y] += part[y];
+                        for (int y = 0; y < 4; ++y) s[n][i][y] += part[y];
                     }
                 }
             }
         }
-        const float sk[2] = {z[lane >> 2], z[(lane >> 2) + 8]}, sv[2] = {z[kStep + (lane >> 2)], z[kStep + (lane >> 2) + 8]};
-        const float lv[2] = {log2_of(sv[0]), log2_of(sv[1])};
+        float sk[4], sv[4], lv[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            sk[k] = z[(lane >> 2) + 8 * k];
+            sv[k] = z[kStep + (lane >> 2) + 8 * k];
+            lv[k] = log2_of(sv[k]);
+        }
         bool outgrown = false;
 #pragma unroll
         for (int n = 0; n < N; ++n)
 #pragma unroll
-            for (int y = 0; y < 4; ++y) {  // head y & 1, key y >> 1
-                s[n][y] = sk[y >> 1] != 0.f ? s[n][y] * (unit[n][y & 1] * sk[y >> 1]) : -CUDART_INF_F;
-                outgrown = outgrown || s[n][y] - ref[n][y & 1] > kOutgrown || s[n][y] + lv[y >> 1] - top[n][y & 1] > 1.f;  // (the first: infinity)
-            }
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {  // key k, head y
+                    float &x = s[n][k >> 1][2 * (k & 1) + y];
+                    x = sk[k] != 0.f ? x * (unit[n][y] * sk[k]) : -CUDART_INF_F;
+                    outgrown = outgrown || x - ref[n][y] > kOutgrown || x + lv[k] - top[n][y] > 1.f;  // (the first: infinity)
+                }
         if (__any_sync(0xffffffffu, outgrown)) {
 #pragma unroll
             for (int n = 0; n < N; ++n)
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
-                    float a = fmaxf(s[n][y], s[n][y + 2]), b = fmaxf(s[n][y] + lv[0], s[n][y + 2] + lv[1]);
+                    float a = ref[n][y], b = top[n][y];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        a = fmaxf(a, s[n][k >> 1][2 * (k & 1) + y]);
+                        b = fmaxf(b, s[n][k >> 1][2 * (k & 1) + y] + lv[k]);
+                    }
 #pragma unroll
                     for (int d = 4; d < 32; d <<= 1) {
                         a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, d));
                         b = fmaxf(b, __shfl_xor_sync(0xffffffffu, b, d));
                     }
-                    a = fmaxf(a, ref[n][y]);
-                    b = fmaxf(b, top[n][y]);
                     l[n][y] *= a == -CUDART_INF_F ? 1.f : fast_exp2(ref[n][y] - a);
                     const float f = b == -CUDART_INF_F ? 1.f : fast_exp2(top[n][y] - b);
                     ref[n][y] = a;
@@ -196,74 +270,134 @@ struct Walk {
                     for (int c = 0; c < F::kPieces; ++c) { o[c][n][y] *= f; o[c][n][y + 2] *= f; }
                 }
         }
-        unsigned p[kParts][N][2];
+        unsigned p[kParts][N][4];
 #pragma unroll
         for (int n = 0; n < N; ++n)
 #pragma unroll
-            for (int key = 0; key < 2; ++key) {
+            for (int k = 0; k < 4; ++k) {
                 float w[2];
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
-                    const float x = s[n][2 * key + y];
+                    const float x = s[n][k >> 1][2 * (k & 1) + y];
                     l[n][y] += fast_exp2(x - (ref[n][y] == -CUDART_INF_F ? 0.f : ref[n][y]));
-                    w[y] = x == -CUDART_INF_F || sv[key] == 0.f ? 0.f : fast_exp2(x - top[n][y] + kTop) * sv[key];
+                    w[y] = x == -CUDART_INF_F || sv[k] == 0.f ? 0.f : fast_exp2(x - top[n][y] + kTop) * sv[k];
                 }
                 const unsigned hi = pack(w[0], w[1]);
-                p[0][n][key] = turned(hi);
+                p[0][n][k] = turned(hi);
                 if constexpr (F::kPair) {
                     const float2 h = __half22float2(*reinterpret_cast<const __half2 *>(&hi));
-                    p[kParts - 1][n][key] = turned(pack(w[0] - h.x, w[1] - h.y));
+                    p[kParts - 1][n][k] = turned(pack(w[0] - h.x, w[1] - h.y));
                 }
             }
 #pragma unroll
-        for (int c = 0; c < F::kPieces; c += 2) {
+        for (int c = 0; c < F::kPieces; ++c) {
             unsigned w[4];
-            wp::ldmatrix4_t(vt + piece_at<D>(r8, F::kPieces > 1 ? c + half : 0), w);
+            wp::ldmatrix4_t(vt + piece_at<D>(lane, c), w);
 #pragma unroll
-            for (int i = 0; i < (F::kPieces > 1 ? 2 : 1); ++i) {
-                // bytes: two channels of one key, two of the next; turned to two keys of one channel, two of the other
-                const unsigned u0 = __byte_perm(w[2 * i], 0, 0x3120), u1 = __byte_perm(w[2 * i + 1], 0, 0x3120);
-                const unsigned a0 = widen_low(u0), a1 = widen_high(u0), a2 = widen_low(u1), a3 = widen_high(u1);
+            for (int i = 0; i < 4; ++i) w[i] = __byte_perm(w[i], 0, 0x3120);  // two channels of one key, two of the next: two keys of one channel, two of the other
+            float part[N][4] = {};
 #pragma unroll
-                for (int n = 0; n < N; ++n) {
-                    float part[4] = {0.f, 0.f, 0.f, 0.f};
-                    float(&to)[4] = F::kPair ? part : o[c + i][n];
+            for (int i = 0; i < 2; ++i) {  // 16 keys
+                const unsigned a0 = widen_low(w[2 * i]), a1 = widen_high(w[2 * i]), a2 = widen_low(w[2 * i + 1]), a3 = widen_high(w[2 * i + 1]);
 #pragma unroll
-                    for (int y = kParts - 1; y >= 0; --y) mma_f16(to, a0, a1, a2, a3, p[y][n][0], p[y][n][1]);
-                    if constexpr (F::kPair) {
+                for (int n = 0; n < N; ++n)
 #pragma unroll
-                        for (int y = 0; y < 4; ++y) o[c + i][n][y] += part[y];
-                    }
-                }
+                    for (int y = kParts - 1; y >= 0; --y) mma_f16(F::kPair ? part[n] : o[c][n], a0, a1, a2, a3, p[y][n][2 * i], p[y][n][2 * i + 1]);
+            }
+            if constexpr (F::kPair) {
+#pragma unroll
+                for (int n = 0; n < N; ++n)
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) o[c][n][y] += part[n][y];
             }
         }
     }
 
-    // m, l and O = sum_t 2^(x - m) v to shared memory.
-    __device__ __forceinline__ void leave(Smem<T, D, N> &sm, int warp, int lane) {
-        float *const own = sm.o[warp];
+    // m, l and O = sum_t 2^(x - m) v
+    __device__ __forceinline__ void leave(float *to, int lane) {
         const int g = lane >> 2, t = lane & 3;
 #pragma unroll
         for (int n = 0; n < N; ++n)
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
                 const int h = 8 * n + 2 * t + y;
-                float sum = l[n][y];
-#pragma unroll
-                for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-                if (g == 0) { sm.m[warp][h] = ref[n][y]; sm.l[warp][h] = sum; }
-                const float f = ref[n][y] == -CUDART_INF_F ? 0.f : fast_exp2(top[n][y] - kTop - ref[n][y]);
+                if (g == 0) { to[h] = ref[n][y]; to[kMaxHeads + h] = l[n][y]; }
 #pragma unroll
                 for (int c = 0; c < F::kPieces; ++c)
-                    *reinterpret_cast<float2 *>(own + h * D + 16 * c + 2 * g) = make_float2(o[c][n][y] * f, o[c][n][y + 2] * f);
+                    *reinterpret_cast<float2 *>(to + 2 * kMaxHeads + h * D + 16 * c + 2 * g) = make_float2(o[c][n][y], o[c][n][y + 2]);
+            }
+    }
+    // l of all keys, and O to l's reference.
+    __device__ __forceinline__ void close() {
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) l[n][y] += __shfl_xor_sync(0xffffffffu, l[n][y], d);
+                const float f = ref[n][y] == -CUDART_INF_F ? 0.f : fast_exp2(top[n][y] - kTop - ref[n][y]);
+#pragma unroll
+                for (int c = 0; c < F::kPieces; ++c) { o[c][n][y] *= f; o[c][n][y + 2] *= f; }
+            }
+    }
+    // The output of a segment with all of its owner's keys; row: of its first head.
+    __device__ __forceinline__ void write(const Args &A, long long row, int heads, bool pairs, int lane) {
+        const int g = lane >> 2, t = lane & 3;
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                const int h = 8 * n + 2 * t + y;
+                if (h >= heads) continue;
+                const float inv = l[n][y] > 0.f ? 1.f / l[n][y] : 0.f;
+                T *const to = (T *)A.a.out + (row + h) * D + 2 * g;
+#pragma unroll
+                for (int c = 0; c < F::kPieces; ++c) {
+                    const float a = o[c][n][y] * inv, b = o[c][n][y + 2] * inv;
+                    if (!pairs) {
+                        to[16 * c] = (T)a;
+                        to[16 * c + 1] = (T)b;
+                    } else if constexpr (F::kPair) {
+                        *reinterpret_cast<float2 *>(to + 16 * c) = make_float2(a, b);
+                    } else {
+                        *reinterpret_cast<__nv_bfloat162 *>(to + 16 * c) = __floats2bfloat162_rn(a, b);
+                    }
+                }
+                if (g == 0 && A.a.lse != nullptr) A.a.lse[row + h] = l[n][y] > 0.f ? (ref[n][y] + log2f(l[n][y])) * kLn2 : -CUDART_INF_F;
             }
     }
 };
 
+// Division of numbers below 2^31: n / d = (n + (n m >> 32)) >> s with 2^(s-1) < d <= 2^s and m = 2^32 (2^s - d) / d, rounded down, and 1.
+struct Divisor {
+    unsigned m, d;
+    int s;
+    __device__ __forceinline__ unsigned quotient(unsigned n) const { return (__umulhi(n, m) + n) >> s; }
+};
+Divisor divisor(int d) {
+    Divisor r = {0, (unsigned)d, 0};
+    while ((1ll << r.s) < d) ++r.s;
+    r.m = (unsigned)((((1ull << r.s) - (unsigned long long)d) << 32) / (unsigned long long)d + 1);
+    return r;
+}
+
+// Waits until no more than `pending` of the last kMost groups of copies are on their way.
+template <int kMost>
+__device__ __forceinline__ void wait_for(unsigned pending) {
+    if constexpr (kMost == 0) {
+        wp::cp_async_wait<0>();
+    } else {
+        if (pending >= kMost) wp::cp_async_wait<kMost>();
+        else wait_for<kMost - 1>(pending);
+    }
+}
+
 struct Args8 {
     Args A;
     Scales sc;
+    Divisor page, block;
     int vec;   // rows of the cache are read in pieces of 16 bytes
+    int pairs; // the output is written two elements at a time
 };
 
 template <class T, int D, int N, bool W>
@@ -277,171 +411,205 @@ __global__ void __launch_bounds__(kThreads, Form<T, D, N>::kCtas) decode8_kernel
     after_previous_kernel();
     T *const out = (T *)A.a.out;
     write_empty_slots<T>(A);
-    const Share mine = share_of(A, all_places<W>(A, lane), (int)blockIdx.x);
+    // the share of a CTA, and of it a warp's: a quarter of the places
+    const long long all = all_places<W, kStep, kOpen>(A, lane);
+    const unsigned n_warps = (unsigned)A.grid * kWarps;
+    const long long per_warp = all >> 31 == 0 ? ((unsigned)all + n_warps - 1) / n_warps : (all + n_warps - 1) / n_warps;
+    const Share mine = {per_warp * kWarps, min(all, per_warp * kWarps * blockIdx.x), min(all, per_warp * kWarps * (blockIdx.x + 1))};
+    const long long first = min(all, mine.first + per_warp * warp), end = min(all, mine.first + per_warp * (warp + 1));
     unsigned char *const ring_ptr = sm.ring[warp];
     const unsigned ring = wp::smem_addr(ring_ptr);
-    const bool one_page = c.page % kStep == 0;  // a tile's keys lie side by side
-    constexpr int kPieces = F::kPieces, kRowsAtOnce = 32 / kPieces < kStep ? 32 / kPieces : kStep;  // rows that 32 lanes fetch at once
+    const bool half_pages = c.page % 16 == 0;  // 16 keys of a tile lie side by side
+    constexpr int kPieces = F::kPieces, kRowsAtOnce = 32 / kPieces;  // rows that 32 lanes fetch at once
     const int row_l = lane / kPieces, piece_l = lane % kPieces;
     unsigned bad = 0;
-    // What this warp fetches: its steps of the segment that is open, step n in the ring's place (at + n) % kStages
-    const int32_t *table = nullptr;
-    const unsigned char *ks = nullptr, *vs = nullptr;
-    const float *zs = nullptr;          // lanes 0 .. 15: K's scales, the others: V's
-    int slot = 0, key_w = 0, key_end = 0, n_steps = 0;
-    unsigned at = 0;
-    int page = -1;                      // lane i < 16: the page of key i of the next step to be fetched, -1: none
-    Seen seen = {};
-    auto page_of = [&](int n) -> int {
-        const int walked = key_w + 4 * n * kStep + lane, key = W ? seen.key(walked) : walked;
-        if (n >= n_steps || lane >= kStep || walked >= key_end) return -1;
-        const int x = table[key / c.page];
-        if ((unsigned)x < (unsigned)c.n_pages) return x;
-        if (!W || seen.sees(key)) bad = (unsigned)slot + 1u;
-        return -1;
+
+    // What is fetched: one tile after the other of one segment after the other, up to kStages tiles and a segment ahead of the one that is
+    // multiplied, so that a segment's first tiles come while the one before it is finished and written out.
+    struct Source {
+        const int32_t *table;
+        int slot, kvh, key0, key_end, n_steps;
+        Seen seen;
+    } src = {};
+    int src_n = 0;                      // the step of it that is fetched next
+    int page = -1, row = 0;             // lane i: the page of key i of that step, -1: none; and its row there
+    unsigned issued = 0, used = 0;      // tiles: tile n is in place n % kStages
+    auto look_up = [&](const Source &f, int n, int &to, int &to_row) {
+        const int walked = f.key0 + n * kStep + lane, key = W ? f.seen.key(walked) : walked;
+        to = -1;
+        if (walked >= f.key_end) return;
+        const unsigned nth = B.page.quotient((unsigned)key);
+        to_row = key - (int)(nth * B.page.d);
+        to = f.table[nth];
+        if ((unsigned)to >= (unsigned)c.n_pages) {
+            to = -1;
+            if (!W || f.seen.sees(key)) bad = (unsigned)f.slot + 1u;
+        }
     };
-    auto fetch = [&](int n) {  // step n, and the pages of the one after it are looked up
-        const int own_page = page;
-        page = page_of(n + 1);
-        if (n < n_steps) {
-            const int walked = key_w + 4 * n * kStep + lane, key = W ? seen.key(walked) : walked, in_page = key % c.page;
-            const unsigned place = (at + (unsigned)n) % F::kStages, there = __ballot_sync(0xffffffffu, own_page >= 0 && (!W || seen.sees(key)));
-            const long long own = own_page >= 0 ? (long long)own_page * c.s_p + (long long)in_page * c.s_t : 0;
-            const long long z = own_page >= 0 ? (long long)own_page * B.sc.s_p + (long long)(in_page / B.sc.block) * B.sc.s_b : 0;
-            const unsigned dst = ring + place * F::kPlace;
-            const long long base = __shfl_sync(0xffffffffu, own, 0) + row_l * c.s_t;
+    auto source_of = [&](const Segment &sg) {
+        Source f;
+        f.table = c.table + (long long)sg.slot * c.max_pages;
+        f.slot = sg.slot;
+        f.kvh = sg.kvh;
+        f.key0 = sg.key0;
+        f.key_end = sg.key_end;
+        f.n_steps = (sg.key_end - sg.key0 + kStep - 1) / kStep;
+        if constexpr (W) f.seen = seen_of<W, kStep>(A.a, sg.slot);
+        return f;
+    };
+    auto fetch = [&] {  // the next tile of src, and the pages of the one after it are looked up
+        const int own_page = page, own_row = row;
+        if (src_n + 1 < src.n_steps) look_up(src, src_n + 1, page, row);
+        const bool mine = own_page >= 0 && (!W || src.seen.sees(src.seen.key(src.key0 + src_n * kStep + lane)));
+        const unsigned place = issued % F::kStages * F::kPlace, there = __ballot_sync(0xffffffffu, mine);
+        const long long own = own_page >= 0 ? (long long)own_page * c.s_p + (long long)own_row * c.s_t : 0;
+        const long long z = mine ? (long long)own_page * B.sc.s_p + (long long)B.block.quotient((unsigned)own_row) * B.sc.s_b + src.kvh * B.sc.s_h : 0;
+        cp_async4_or_zero(ring + place + 2 * F::kTile + lane * 4, B.sc.k + z, mine ? 4 : 0);
+        cp_async4_or_zero(ring + place + 2 * F::kTile + kStep * 4 + lane * 4, B.sc.v + z, mine ? 4 : 0);
+        const long long base0 = __shfl_sync(0xffffffffu, own, 0), base1 = __shfl_sync(0xffffffffu, own, 16), head = src.kvh * c.s_h + piece_l * 16;
 #pragma unroll
-            for (int r0 = 0; r0 < kStep; r0 += kRowsAtOnce) {
-                const int r = r0 + row_l;
-                long long e = base + r0 * c.s_t;
-                if (!one_page) e = __shfl_sync(0xffffffffu, own, r & 31);
-                if (r - r0 < kRowsAtOnce) {
-                    const bool is = (there >> r) & 1u;
-                    e = (is ? e : 0) + piece_l * 16;
-                    const unsigned to = place * F::kPlace + piece_at<D>(r, piece_l);
-                    if (B.vec) {
-                        wp::cp_async16(ring + to, ks + e, is ? 16 : 0);
-                        wp::cp_async16(ring + to + F::kTile, vs + e, is ? 16 : 0);
-                    } else {
+        for (int r0 = 0; r0 < kStep; r0 += kRowsAtOnce) {
+            const int r = r0 + row_l;
+            const bool upper = kRowsAtOnce > 16 ? r >= 16 : r0 >= 16;
+            long long e = upper ? base1 + (r - 16) * c.s_t : base0 + r * c.s_t;
+            if (!half_pages) e = __shfl_sync(0xffffffffu, own, r);
+            const bool is = (there >> r) & 1u;
+            e = is ? e + head : 0;
+            const unsigned char *const ks = (const unsigned char *)A.a.k + e, *const vs = (const unsigned char *)A.a.v + e;
+            const unsigned to = place + piece_at<D>(r, piece_l);
+            if (B.vec) {
+                wp::cp_async16(ring + to, ks, is ? 16 : 0);
+                wp::cp_async16(ring + to + F::kTile, vs, is ? 16 : 0);
+            } else {
 #pragma unroll 4
-                        for (int i = 0; i < 16; ++i) {
-                            ring_ptr[to + i] = is ? ks[e + i] : 0;
-                            ring_ptr[to + F::kTile + i] = is ? vs[e + i] : 0;
-                        }
-                    }
+                for (int i = 0; i < 16; ++i) {
+                    ring_ptr[to + i] = is ? ks[i] : 0;
+                    ring_ptr[to + F::kTile + i] = is ? vs[i] : 0;
                 }
             }
-            const long long z_at = __shfl_sync(0xffffffffu, z, lane & 15);
-            const bool is = (there >> (lane & 15)) & 1u;
-            cp_async4_or_zero(dst + 2 * F::kTile + lane * 4, zs + (is ? z_at : 0), is ? 4 : 0);
         }
         wp::cp_async_commit();
+        ++issued;
+        ++src_n;
     };
-    constexpr int kOwn = F::kHeads / (kThreads / 32);  // heads whose q a warp reads: lane i their channels kLane i ...
-    float qr[kOwn][F::kLane];
-    // The first steps of a segment are on their way before the one before it is written out, and so is its Q
-    auto open = [&](const Segment &sg) {
-        at += (unsigned)n_steps;
-        slot = sg.slot;
-        if constexpr (W) seen = seen_of<W>(A.a, slot);
-        table = c.table + (long long)slot * c.max_pages;
-        ks = (const unsigned char *)A.a.k + (long long)sg.kvh * c.s_h;
-        vs = (const unsigned char *)A.a.v + (long long)sg.kvh * c.s_h;
-        zs = (lane < kStep ? B.sc.k : B.sc.v) + (long long)sg.kvh * B.sc.s_h;
-        key_w = sg.key0 + warp * kStep;
-        key_end = sg.key_end;
-        n_steps = key_end > key_w ? (key_end - key_w + 4 * kStep - 1) / (4 * kStep) : 0;
-        page = page_of(0);
+    Four<T> raw[F::kPieces][N];
+    auto load_q = [&](const Segment &sg) {
+        const T *const src = (const T *)A.a.q + (long long)sg.slot * A.a.qs_s + (long long)(sg.h0 + (lane >> 2)) * A.a.qs_h + 4 * (lane & 3);
 #pragma unroll
-        for (int i = 0; i < kOwn; ++i) {
-            const int h = warp + 4 * i;
-            const T *const src = (const T *)A.a.q + (long long)slot * A.a.qs_s + (long long)(sg.h0 + h) * A.a.qs_h + lane * F::kLane;
+        for (int n = 0; n < N; ++n)
 #pragma unroll
-            for (int e = 0; e < F::kLane; ++e) qr[i][e] = h < sg.heads && lane * F::kLane < D ? to_float(src[e]) : 0.f;
-        }
-#pragma unroll
-        for (int n = 0; n < F::kStages - 1; ++n) fetch(n);
+            for (int c = 0; c < F::kPieces; ++c)
+                raw[c][n] = 8 * n + (lane >> 2) < sg.heads ? load_four<T>(src + 8 * n * A.a.qs_h + 16 * c, A.q_vec != 0) : Four<T>{};
     };
     Place pl = {0, 0, 0};
+    int n_pieces = 0;
+    if (lane < 2) sm.piece[2 * warp + lane].slot = -1;
+    __syncwarp();
+    Segment sg = open_segment<W, kStep, kOpen>(A, first, end, lane, pl);
+    if (sg.next >= 0) {
+        src = source_of(sg);
+        look_up(src, 0, page, row);
+        if constexpr (F::kQInRegs) load_q(sg);
+        for (int n = 0; n < F::kStages - 1 && n < src.n_steps; ++n) fetch();
+    }
+    while (sg.next >= 0) {
+        const int n_steps = (sg.key_end - sg.key0 + kStep - 1) / kStep;
+        // the segment behind, and the pages of its first tile
+        const Segment next = open_segment<W, kStep, kOpen>(A, sg.next, end, lane, pl);
+        bool waits = next.next >= 0;  // it is not yet fetched from
+        int next_page = -1, next_row = 0;
+        Source behind = {};
+        if (waits) {
+            behind = source_of(next);
+            look_up(behind, 0, next_page, next_row);
+        }
+        if constexpr (!F::kQInRegs) load_q(sg);
+        Walk<T, D, N> walk;
+        walk.begin(sm, warp, raw, A.a.scale_log2, lane);
+        __syncwarp();
+        for (int n = 0; n < n_steps; ++n) {
+            while (issued - used < F::kStages) {
+                if (src_n == src.n_steps) {
+                    if (!waits) break;
+                    waits = false;
+                    src = behind;
+                    src_n = 0;
+                    page = next_page;
+                    row = next_row;
+                }
+                fetch();
+            }
+            wait_for<F::kStages - 1>(issued - used - 1);  // copies that may still be on their way: those of later tiles
+            __syncwarp();
+            const unsigned place = used % F::kStages * F::kPlace;
+            walk.step(sm, warp, ring + place, reinterpret_cast<const float *>(ring_ptr + place + 2 * F::kTile), lane);
+            __syncwarp();  // (the tile is read before its place is filled again)
+            ++used;
+        }
+        if (waits) {
+            src = behind;
+            src_n = 0;
+            page = next_page;
+            row = next_row;
+        }
+        if (F::kQInRegs && next.next >= 0) load_q(next);
+        walk.close();
+        const long long to_row = (long long)sg.slot * A.a.H + sg.h0;
+        if (sg.whole) {
+            walk.write(A, to_row, sg.heads, B.pairs != 0, lane);
+        } else {  // the warp's first segment, or its last one: that one stays in the ring, which is done with
+            float *const to = next.next >= 0 ? A.warp_parts + ((long long)blockIdx.x * kWarps + warp) * kMaxHeads * (D + 2) : reinterpret_cast<float *>(ring_ptr);
+            walk.leave(to, lane);
+            if (lane == 0) sm.piece[2 * warp + n_pieces] = {to, sg.owner_end, sg.slot, sg.h0, sg.heads, sg.key0 == 0, sg.next == sg.owner_end};
+            ++n_pieces;
+        }
+        sg = next;
+    }
+    __syncthreads();
+    // The warps' pieces side by side: those of one owner are joined, and what is not all of it is left to the joins (two at most)
     int n_parts = 0;
     Left left = {};
-    Segment sg = open_segment<W>(A, mine.first, mine.end, lane, pl);
-    if (sg.next >= 0) open(sg);
-    while (sg.next >= 0) {
-        const int s = sg.slot;
-#pragma unroll
-        for (int i = 0; i < kOwn; ++i) {  // q times a power of two, in [2^14, 2^15) at its largest
-            const int h = warp + 4 * i;
-            float most = 0.f;
-#pragma unroll
-            for (int e = 0; e < F::kLane; ++e) most = fmaxf(most, fabsf(qr[i][e]));
-            most = warp_maximum(most);
-            const int up = min(max(141 - (int)(__float_as_uint(most) >> 23), -114), 126);
-            const float f = __uint_as_float((unsigned)(up + 127) << 23);
-            if (lane == 0) sm.unit[h] = 1.f / f;
-            if (lane * F::kLane < D) {
-#pragma unroll
-                for (int e = 0; e < F::kLane; ++e) {
-                    const float x = qr[i][e] * f;
-                    const __half hi = __float2half_rn(x);
-                    sm.q[0][h * D + lane * F::kLane + e] = hi;
-                    if constexpr (F::kPair) sm.q[F::kPair ? 1 : 0][h * D + lane * F::kLane + e] = __float2half_rn(x - __half2float(hi));
-                }
-            }
+    for (int k0 = 0, k1; k0 < 2 * kWarps; k0 = k1) {
+        const Piece p = sm.piece[k0];
+        int ends = p.ends;
+        for (k1 = k0 + 1; k1 < 2 * kWarps; ++k1) {
+            const Piece &o = sm.piece[k1];
+            if (o.slot >= 0 && (o.slot != p.slot || o.h0 != p.h0)) break;
+            if (o.slot >= 0) ends = o.ends;
         }
-        __syncthreads();
-        Walk<T, D, N> walk;
-        walk.begin(sm, A.a.scale_log2, lane);
-        for (int n = 0; n < n_steps; ++n) {
-            fetch(n + F::kStages - 1);
-            wp::cp_async_wait<F::kStages - 1>();
-            __syncwarp();
-            const unsigned place = (at + (unsigned)n) % F::kStages * F::kPlace;
-            walk.step(sm, ring + place, reinterpret_cast<const float *>(ring_ptr + place + 2 * F::kTile), lane);
-            __syncwarp();  // (the tile is read before its place is filled again)
-        }
-        const Segment next = open_segment<W>(A, sg.next, mine.end, lane, pl);
-        if (next.next >= 0) {
-            open(next);
-        } else {
-            at += (unsigned)n_steps;
-            wp::cp_async_wait<0>();
-        }
-        // the four warps' m, l and O meet
-        walk.leave(sm, warp, lane);
-        __syncthreads();
+        if (p.slot < 0) { k1 = k0 + 1; continue; }
+        const bool whole = p.starts && ends;
+        const long long to_row = (long long)p.slot * A.a.H + p.h0;
         float *const part = part_of(A, (int)blockIdx.x, n_parts);
-        if (!sg.whole) {
-            if (sg.key0 == 0) left = {pieces_of(sg, mine), n_parts, sg.heads, 0u, (long long)sg.slot * A.a.H + sg.h0, 0ll};
+        if (!whole) {
+            if (p.starts) left = {pieces_of(p.owner_end, mine), n_parts, p.heads, 0u, to_row, 0ll};
             ++n_parts;
         }
-        for (int i = tid; i < sg.heads * (D / 4); i += kThreads) {
-            const int h = i / (D / 4), x = (i % (D / 4)) * 4;
-            float m = sm.m[0][h];
-#pragma unroll
-            for (int w = 1; w < kThreads / 32; ++w) m = fmaxf(m, sm.m[w][h]);
+        for (int e = tid; e < p.heads * (D / 4); e += kThreads) {
+            const int h = e / (D / 4), x = (e % (D / 4)) * 4;
+            float m = -CUDART_INF_F, sum = 0.f;
+            for (int k = k0; k < k1; ++k)
+                if (sm.piece[k].slot >= 0) m = fmaxf(m, sm.piece[k].at[h]);
             const float base = m == -CUDART_INF_F ? 0.f : m;
-            float sum = 0.f;
             float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int w = 0; w < kThreads / 32; ++w) {
-                const float f = fast_exp2(sm.m[w][h] - base);
-                const float4 z = *reinterpret_cast<const float4 *>(sm.o[w] + h * D + x);
-                sum = fmaf(f, sm.l[w][h], sum);
-                y.x = fmaf(f, z.x, y.x); y.y = fmaf(f, z.y, y.y); y.z = fmaf(f, z.z, y.z); y.w = fmaf(f, z.w, y.w);
-            }
-            if (sg.whole) {
+            for (int k = k0; k < k1; ++k)
+                if (sm.piece[k].slot >= 0) {
+                    const float *const a = sm.piece[k].at;
+                    const float f = fast_exp2(a[h] - base);
+                    const float4 z = *reinterpret_cast<const float4 *>(a + 2 * kMaxHeads + h * D + x);
+                    sum = fmaf(f, a[kMaxHeads + h], sum);
+                    y.x = fmaf(f, z.x, y.x); y.y = fmaf(f, z.y, y.y); y.z = fmaf(f, z.z, y.z); y.w = fmaf(f, z.w, y.w);
+                }
+            if (whole) {
                 const float inv = sum > 0.f ? 1.f / sum : 0.f;
-                T *const to = out + ((long long)s * A.a.H + sg.h0 + h) * D + x;
+                T *const to = out + (to_row + h) * D + x;
                 to[0] = (T)(y.x * inv); to[1] = (T)(y.y * inv); to[2] = (T)(y.z * inv); to[3] = (T)(y.w * inv);
-                if (x == 0 && A.a.lse != nullptr) A.a.lse[(long long)s * A.a.H + sg.h0 + h] = sum > 0.f ? (m + log2f(sum)) * kLn2 : -CUDART_INF_F;
+                if (x == 0 && A.a.lse != nullptr) A.a.lse[to_row + h] = sum > 0.f ? (m + log2f(sum)) * kLn2 : -CUDART_INF_F;
             } else {
                 *reinterpret_cast<float4 *>(part + 2 * kMaxHeads + h * D + x) = y;
                 if (x == 0) { part[h] = m; part[kMaxHeads + h] = sum; }
             }
         }
-        __syncthreads();  // (O, m, l and q are written again)
-        sg = next;
     }
     leave_to_joins(A, left, bad);
 }
@@ -449,7 +617,7 @@ __global__ void __launch_bounds__(kThreads, Form<T, D, N>::kCtas) decode8_kernel
 template <class T, int D, int N, bool W>
 cudaError_t launch(Args8 &B, int n_sm, cudaStream_t st) {
     const int smem = (int)sizeof(Smem<T, D, N>);
-    static_assert(Form<T, D, N>::kCtas * (sizeof(Smem<T, D, N>) + 1024) <= 233472, "what an SM has");
+    static_assert(Form<T, D, N>::kCtas * (sizeof(Smem<T, D, N>) + 1024 + 256) <= 233472, "what an SM has");
     static DeviceFlags done;
     cudaError_t e = allow_smem_once(decode8_kernel<T, D, N, W>, smem, done);
     if (e != cudaSuccess) return e;
@@ -480,8 +648,13 @@ stream_status launch_decode8(const DecodeCall &a, const Scales &sc, int dtype, v
     const int n_sm = current_sm_count();
     if (n_sm <= 0) { set_error("cannot read the SM count of the current device"); return STREAM_ERR_CUDA; }
     Args8 B;
-    B.A = args_of(a, workspace, n_sm);
+    B.A = args_of(a, workspace, n_sm, kStep, kOpen);
     B.sc = sc;
+    B.page = divisor(a.c.page);
+    B.block = divisor(sc.block);
+    const int e = dtype == STREAM_F32 ? 4 : 2;
+    B.A.q_vec = ((uintptr_t)a.q & (4 * e - 1)) == 0 && ((a.qs_s | a.qs_h) & 3) == 0 ? 1 : 0;
+    B.pairs = ((uintptr_t)a.out & (2 * e - 1)) == 0 ? 1 : 0;
     B.vec = (((uintptr_t)a.k | (uintptr_t)a.v) & 15) == 0 && ((a.c.s_p | a.c.s_t | a.c.s_h) & 15) == 0 ? 1 : 0;
     cudaError_t rc = dtype == STREAM_F32 ? launch_d<float>(B, n_sm, st) : launch_d<__nv_bfloat16>(B, n_sm, st);
     if (rc != cudaSuccess) return cuda_fail(rc, "8-bit decode attention launch");

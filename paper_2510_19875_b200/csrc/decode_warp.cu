@@ -317,7 +317,7 @@ __global__ void __launch_bounds__(kThreads, Form<T, D>::kCtas) decode_warp_kerne
     auto open = [&](const Segment &sg) {
         at += (unsigned)n_steps;
         slot = sg.slot;
-        if constexpr (W) seen = seen_of<W>(A.a, slot);
+        if constexpr (W) seen = seen_of<W, kUnit64>(A.a, slot);
         table = c.table + (long long)slot * c.max_pages;
         ks = (const T *)A.a.k + (long long)sg.kvh * c.s_h;
         vs = (const T *)A.a.v + (long long)sg.kvh * c.s_h;
@@ -388,7 +388,7 @@ __global__ void __launch_bounds__(kThreads, Form<T, D>::kCtas) decode_warp_kerne
         __syncthreads();
         float *const part = part_of(A, (int)blockIdx.x, n_parts);
         if (!sg.whole) {
-            if (sg.key0 == 0) left = {pieces_of(sg, mine), n_parts, sg.heads, 0u, (long long)sg.slot * A.a.H + sg.h0, 0ll};
+            if (sg.key0 == 0) left = {pieces_of(sg.owner_end, mine), n_parts, sg.heads, 0u, (long long)sg.slot * A.a.H + sg.h0, 0ll};
             ++n_parts;
         }
         for (int i = tid; i < sg.heads * (D / 4); i += kThreads) {
