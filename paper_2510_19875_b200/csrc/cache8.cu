@@ -27,20 +27,40 @@ __device__ __forceinline__ int scale_exp(float amax) {
 }
 __device__ __forceinline__ float two_to(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }
 
-// Eight elements.
+// Eight elements, as they lie in memory.
 template <class T>
-__device__ __forceinline__ void load_piece(const T *p, bool vec, float (&x)[8]) {
-    if (!vec) {
+struct Piece { uint4 w[sizeof(T) / 2]; };
+template <class T>
+__device__ __forceinline__ Piece<T> load_piece(const T *p, bool vec) {
+    Piece<T> r;
+    constexpr int kPer = 16 / (int)sizeof(T);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = to_float(p[i]);
-    } else if constexpr (sizeof(T) == 4) {
-        const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
-        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-    } else {
-        const uint4 a = *reinterpret_cast<const uint4 *>(p);
-        const unsigned w[4] = {a.x, a.y, a.z, a.w};
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+        if (vec) {
+            r.w[i] = *reinterpret_cast<const uint4 *>(p + i * kPer);
+        } else if constexpr (sizeof(T) == 4) {
+            r.w[i] = make_uint4(__float_as_uint(p[4 * i]), __float_as_uint(p[4 * i + 1]), __float_as_uint(p[4 * i + 2]), __float_as_uint(p[4 * i + 3]));
+        } else {
+            const uint2 a = wp::load4(p), b = wp::load4(p + 4);
+            r.w[i] = make_uint4(a.x, a.y, b.x, b.y);
+        }
+    }
+    return r;
+}
+template <class T>
+__device__ __forceinline__ void widen(const Piece<T> &r, float (&x)[8]) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+        const unsigned w[4] = {r.w[i].x, r.w[i].y, r.w[i].z, r.w[i].w};
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            if constexpr (sizeof(T) == 4) {
+                x[4 * i + y] = __uint_as_float(w[y]);
+            } else {
+                x[2 * y] = __uint_as_float(w[y] << 16);
+                x[2 * y + 1] = __uint_as_float(w[y] & 0xffff0000u);
+            }
+        }
     }
 }
 __device__ __forceinline__ uint2 round8(const float (&x)[8], float f) {
@@ -86,13 +106,13 @@ __device__ __forceinline__ long long place_of(const WriteArgs &a, int s) { retur
 
 // kGroup threads a block: 32, or all of the CTA's.
 template <class T, int kGroup>
-__global__ void __launch_bounds__(kThreads) write8_kernel(const __grid_constant__ WriteArgs a) {
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 8 : 4) write8_kernel(const __grid_constant__ WriteArgs a) {
     __shared__ float tops[kThreads / 32];
     after_previous_kernel();
     const CacheGeom &c = a.c;
     if (a.done != nullptr && *a.done == 0) return;
     constexpr int kGroups = kThreads / kGroup;
-    const int lane = threadIdx.x & 31, me = threadIdx.x % kGroup, row_pieces = c.d / 8, block = a.sc.block;
+    const int lane = threadIdx.x & 31, me = threadIdx.x % kGroup, row_shift = 28 - __clz(c.d), block = a.sc.block;  // (2^row_shift pieces a row)
     const long long items = a.places * c.G * 2;
     for (long long it = (long long)blockIdx.x * kGroups + threadIdx.x / kGroup; it < items; it += (long long)gridDim.x * kGroups) {
         const int kv = (int)(it & 1), h = (int)((it >> 1) % c.G);
@@ -101,35 +121,41 @@ __global__ void __launch_bounds__(kThreads) write8_kernel(const __grid_constant_
         for (int hi = c.n_slots; hi - s > 1;) {  // the last slot that begins at or before the place (32 candidates a step)
             const int step = (hi - s + 31) / 32;
             const long long at = s + (long long)lane * step;
-            const unsigned below = __ballot_sync(0xffffffffu, at < hi && place_of(a, (int)min(at, (long long)c.n_slots - 1)) <= place);
+            const unsigned below = __ballot_sync(0xffffffffu, at < hi && place_of(a, (int)min(at, (long long)hi - 1)) <= place);
             s += (below != 0 ? 31 - __clz(below) : 0) * step;
             hi = min(hi, s + step);
         }
         const Span sp = span_of(a.cu, s, a.total);
-        const int len = tokens_of(c, s), start = max(len - sp.n, 0);  // the first new token (rows in front of the slot's first token are passed over)
+        const int len = tokens_of(c, s);
+        const int start = max(len - sp.n, 0);  // the first new token (rows in front of the slot's first token are passed over)
         const long long nth = place - place_of(a, s), lo64 = (start / block + nth) * block;
         if (nth < 0 || lo64 >= len || sp.n == 0) continue;  // (the whole group)
         const int lo = (int)lo64, hi = min(len, lo + block), first = max(lo, start);
-        const int page = c.table[(long long)s * c.max_pages + lo / c.page];
-        if ((unsigned)page >= (unsigned)c.n_pages) continue;
-        float *const scale_at = const_cast<float *>(kv ? a.sc.v : a.sc.k) + page * a.sc.s_p + (lo % c.page / block) * a.sc.s_b + h * a.sc.s_h;
-        unsigned char *const to = a.pages[kv] + page * c.s_p + (long long)(lo % c.page) * c.s_t + h * c.s_h;
+        const int page = c.table[(long long)s * c.max_pages + lo / c.page];  // (looked at behind the loads that do not need it)
         const T *const from = (const T *)a.x[kv] + (long long)(sp.first + sp.n - (len - first)) * a.s_t + h * a.s_h;
-        const int n = (hi - first) * row_pieces;
+        const int n = (hi - first) << row_shift;
         const bool held = n <= kGroup * kHold;
-        const float had = first > lo ? *scale_at : 0.f;
-        float x[kHold][8], top = 0.f;
+        Piece<T> raw[kHold];
+        float x[8], top = 0.f;
         for (int p0 = 0; p0 < n; p0 += kGroup * kHold) {
 #pragma unroll
             for (int i = 0; i < kHold; ++i) {
                 const int p = p0 + i * kGroup + me;
-                if (p < n) {
-                    load_piece(from + (long long)(p / row_pieces) * a.s_t + (p % row_pieces) * 8, a.vec_in != 0, x[i]);
+                if (p < n) raw[i] = load_piece(from + (long long)(p >> row_shift) * a.s_t + (p & ((1 << row_shift) - 1)) * 8, a.vec_in != 0);
+            }
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[i][e]));
+            for (int i = 0; i < kHold; ++i) {
+                if (p0 + i * kGroup + me < n) {
+                    widen(raw[i], x);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[e]));
                 }
             }
         }
+        if ((unsigned)page >= (unsigned)c.n_pages) continue;
+        float *const scale_at = const_cast<float *>(kv ? a.sc.v : a.sc.k) + page * a.sc.s_p + (lo % c.page / block) * a.sc.s_b + h * a.sc.s_h;
+        unsigned char *const to = a.pages[kv] + page * c.s_p + (long long)(lo % c.page) * c.s_t + h * c.s_h;
+        const float had = first > lo ? *scale_at : 0.f;
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
         if constexpr (kGroup > 32) {
@@ -144,8 +170,8 @@ __global__ void __launch_bounds__(kThreads) write8_kernel(const __grid_constant_
         if (me == 0 && scale != had) *scale_at = scale;
         if (first > lo && had != scale) {  // what the block has, rounded again
             const float f = had / scale;
-            for (int p = me; p < (first - lo) * row_pieces; p += kGroup) {
-                unsigned char *const at = to + (long long)(p / row_pieces) * c.s_t + (p % row_pieces) * 8;
+            for (int p = me; p < (first - lo) << row_shift; p += kGroup) {
+                unsigned char *const at = to + (long long)(p >> row_shift) * c.s_t + (p & ((1 << row_shift) - 1)) * 8;
                 const uint2 w = load8(at, a.vec_out != 0);
                 float y[8];
 #pragma unroll
@@ -163,8 +189,10 @@ __global__ void __launch_bounds__(kThreads) write8_kernel(const __grid_constant_
             for (int i = 0; i < kHold; ++i) {
                 const int p = p0 + i * kGroup + me;
                 if (p < n) {
-                    if (!held) load_piece(from + (long long)(p / row_pieces) * a.s_t + (p % row_pieces) * 8, a.vec_in != 0, x[i]);
-                    store8(dst + (long long)(p / row_pieces) * c.s_t + (p % row_pieces) * 8, round8(x[i], inv), a.vec_out != 0);
+                    const int row = p >> row_shift, piece = p & ((1 << row_shift) - 1);
+                    if (!held) raw[i] = load_piece(from + (long long)row * a.s_t + piece * 8, a.vec_in != 0);
+                    widen(raw[i], x);
+                    store8(dst + (long long)row * c.s_t + piece * 8, round8(x, inv), a.vec_out != 0);
                 }
             }
         }
@@ -180,7 +208,8 @@ struct ReadArgs {
     int total;
 };
 
-// A warp a token; kPiece elements at a time: 16, or one where a row or an output is off 16 bytes.
+// A warp a token; kPiece elements at a time: 16 bytes of the output, or one element where a row or an output is off its boundary.
+constexpr int kAhead = 4;  // pieces of K, and of V, that a lane reads before it writes
 template <class T, int kPiece>
 __global__ void __launch_bounds__(kThreads) read8_kernel(const __grid_constant__ ReadArgs a) {
     after_previous_kernel();
@@ -195,35 +224,42 @@ __global__ void __launch_bounds__(kThreads) read8_kernel(const __grid_constant__
         const bool there = (unsigned)page < (unsigned)c.n_pages;
         const int in_page = there ? (int)pos % c.page : 0;
         const long long from = there ? page * c.s_p + in_page * c.s_t : 0, z = there ? page * a.sc.s_p + in_page / a.sc.block * a.sc.s_b : 0;
-        for (int u = lane; u < c.G * row_pieces; u += 32) {
-            const int h = u / row_pieces, x = (u - h * row_pieces) * kPiece;
-            uint4 w[2] = {};
-            float scale[2] = {0.f, 0.f};
-            if (there) {
+        const int pieces = c.G * row_pieces;
+        for (int u0 = lane; u0 < pieces; u0 += 32 * kAhead) {
+            unsigned w[kAhead][2][2];
+            float scale[kAhead][2];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int u = u0 + 32 * i, h = u / row_pieces, x = (u - h * row_pieces) * kPiece;
 #pragma unroll
                 for (int kv = 0; kv < 2; ++kv) {
-                    const unsigned char *const at = a.pages[kv] + from + h * c.s_h + x;
-                    if constexpr (kPiece == 16) w[kv] = *reinterpret_cast<const uint4 *>(at);
-                    else w[kv].x = *at;
-                    scale[kv] = (kv ? a.sc.v : a.sc.k)[z + h * a.sc.s_h];
+                    w[i][kv][0] = w[i][kv][1] = 0;
+                    scale[i][kv] = 0.f;
+                    if (there && u < pieces) {
+                        const unsigned char *const at = a.pages[kv] + from + h * c.s_h + x;
+                        if constexpr (kPiece == 8) { const uint2 y = *reinterpret_cast<const uint2 *>(at); w[i][kv][0] = y.x; w[i][kv][1] = y.y; }
+                        else if constexpr (kPiece == 4) w[i][kv][0] = *reinterpret_cast<const unsigned *>(at);
+                        else w[i][kv][0] = *at;
+                        scale[i][kv] = (kv ? a.sc.v : a.sc.k)[z + h * a.sc.s_h];
+                    }
                 }
             }
 #pragma unroll
-            for (int kv = 0; kv < 2; ++kv) {
-                T *const to = (T *)a.x[kv] + (t * c.G + h) * c.d + x;
-                const unsigned v[4] = {w[kv].x, w[kv].y, w[kv].z, w[kv].w};
-                if constexpr (kPiece == 1) {
-                    to[0] = (T)(widen8(v[0]).x * scale[kv]);
-                } else {
-                    __align__(16) T y[16];
+            for (int i = 0; i < kAhead; ++i) {
+                const int u = u0 + 32 * i;
+                if (u >= pieces) break;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float2 f = widen8(v[i >> 1] >> (16 * (i & 1)) & 0xffffu);
-                        y[2 * i] = (T)(f.x * scale[kv]);
-                        y[2 * i + 1] = (T)(f.y * scale[kv]);
+                for (int kv = 0; kv < 2; ++kv) {
+                    T *const to = (T *)a.x[kv] + t * c.G * c.d + (long long)u * kPiece;
+                    __align__(16) T y[kPiece];
+#pragma unroll
+                    for (int e = 0; e < (kPiece + 1) / 2; ++e) {
+                        const float2 f = widen8(w[i][kv][e >> 1] >> (16 * (e & 1)) & 0xffffu);
+                        y[2 * e] = (T)(f.x * scale[i][kv]);
+                        if constexpr (kPiece > 1) y[2 * e + 1] = (T)(f.y * scale[i][kv]);
                     }
-#pragma unroll
-                    for (int i = 0; i < (int)sizeof(T); ++i) reinterpret_cast<uint4 *>(to)[i] = reinterpret_cast<const uint4 *>(y)[i];
+                    if constexpr (kPiece > 1) *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(y);
+                    else to[0] = y[0];
                 }
             }
         }
@@ -261,14 +297,15 @@ stream_status launch_read8(const CacheGeom &c, const Scales &sc, int dtype, cons
     ReadArgs a = {};
     a.c = c; a.sc = sc; a.pages[0] = (const unsigned char *)k_pages; a.pages[1] = (const unsigned char *)v_pages; a.x[0] = k_out; a.x[1] = v_out;
     a.cu = cu; a.total = total;
-    const bool vec = on(16, k_pages, v_pages) && on(16, k_out, v_out) && ((c.s_p | c.s_t | c.s_h) & 15) == 0;
+    const int piece = dtype == STREAM_F32 ? 4 : 8;
+    const bool vec = on(piece, k_pages, v_pages) && on(16, k_out, v_out) && ((c.s_p | c.s_t | c.s_h) & (piece - 1)) == 0;
     const int n_sm = current_sm_count();
     if (n_sm <= 0) { set_error("cannot read the SM count of the current device"); return STREAM_ERR_CUDA; }
     const long long ctas = ((long long)total + kThreads / 32 - 1) / (kThreads / 32), most = (long long)n_sm * kCtas;
     const unsigned grid = (unsigned)(ctas < most ? ctas : most);
     cudaError_t rc;
-    if (dtype == STREAM_F32) rc = vec ? launch_early(read8_kernel<float, 16>, grid, kThreads, 0, st, a) : launch_early(read8_kernel<float, 1>, grid, kThreads, 0, st, a);
-    else rc = vec ? launch_early(read8_kernel<__nv_bfloat16, 16>, grid, kThreads, 0, st, a) : launch_early(read8_kernel<__nv_bfloat16, 1>, grid, kThreads, 0, st, a);
+    if (dtype == STREAM_F32) rc = vec ? launch_early(read8_kernel<float, 4>, grid, kThreads, 0, st, a) : launch_early(read8_kernel<float, 1>, grid, kThreads, 0, st, a);
+    else rc = vec ? launch_early(read8_kernel<__nv_bfloat16, 8>, grid, kThreads, 0, st, a) : launch_early(read8_kernel<__nv_bfloat16, 1>, grid, kThreads, 0, st, a);
     return rc == cudaSuccess ? STREAM_OK : cuda_fail(rc, "8-bit cache read launch");
 }
 

@@ -24,12 +24,11 @@ using namespace decode;
 constexpr int kWarps = kThreads / 32;
 constexpr int kStep = 32;            // keys of a warp's tile: one a lane where pages are looked up. And the keys of a unit
 // What a segment costs a warp beside its keys, in units.
-#ifndef OPEN8
-#define OPEN8 2
-#endif
-constexpr int kOpen = OPEN8;
+constexpr int kOpen = 3;
 constexpr float kOutgrown = 30.f;    // log2: of the sum's reference
-constexpr float kTop = 14.f;         // log2: a weight for the product at its reference
+constexpr float kTop = 14.f;         // log2: a weight for the product where it is the largest, times its value's scale
+constexpr float kNone = -3e38f;      // a reference before the first key, finite so that it has differences
+constexpr float kLeastScale = 7.8886090522101181e-31f;  // 2^-100: of values (a smaller one, 0 too, counts as this)
 
 template <class T, int D, int N>
 struct Form {
@@ -40,10 +39,13 @@ struct Form {
     static constexpr int kPlace = 2 * kTile + 2 * kStep * 4;    // K, V, the keys' scales
     static constexpr int kHeads = 8 * N;
     static constexpr bool kQInRegs = kParts * N * kPieces <= 16;
+    static constexpr bool kQEarly = !kPair && N * kPieces <= 8; // the next segment's q is in registers beside the present one
     static constexpr int kStages = D == 256 ? (kQInRegs ? 3 : 2) : D == 128 ? 3 : D == 64 ? 5 : 8;
     static constexpr int kCtas = D == 256 || (D == 128 && !kQInRegs) ? 1 : 2;  // of an SM
-    static constexpr int kLeave = (2 * kMaxHeads + kHeads * D) * 4;    // m, l, O
+    static constexpr int kLeave = (2 * kMaxHeads + kHeads * D) * 4;    // bytes of a piece: m, l, O
     static_assert(kLeave <= kStages * kPlace, "a warp's last piece in its ring");
+    // the first pieces of the warps but the first in shared memory, where that is large enough, else in the workspace
+    static constexpr bool kFirstHere = kCtas * (kWarps * kStages * kPlace + (kWarps - 1) * kLeave + (kQInRegs ? 0 : kWarps * kParts * kPieces * N * 256) + 2048) <= 233472;
 };
 // A piece of an owner that a warp leaves to its CTA.
 struct Piece {
@@ -57,7 +59,9 @@ struct Smem {
     using F = Form<T, D, N>;
     unsigned char ring[kWarps][F::kStages * F::kPlace];
     uint2 q[kWarps][F::kQInRegs ? 1 : F::kParts * F::kPieces * N * 32];  // what a lane multiplies with
+    float first[F::kFirstHere ? kWarps - 1 : 1][F::kFirstHere ? F::kLeave / 4 : 1];
     Piece piece[2 * kWarps];
+    int n_parts;   // that the first warp has left to the joins
 };
 
 // Byte of piece x (16 bytes) of row r in a tile: turned, so that eight rows' same piece touch every bank.
@@ -176,7 +180,7 @@ struct Walk {
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
                 unit[n][y] = __shfl_sync(0xffffffffu, worth, 8 * (lane & 3) + 4 * y);
-                ref[n][y] = top[n][y] = -CUDART_INF_F;
+                ref[n][y] = top[n][y] = kNone;
                 l[n][y] = 0.f;
             }
 #pragma unroll
@@ -232,26 +236,30 @@ struct Walk {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             sk[k] = z[(lane >> 2) + 8 * k];
-            sv[k] = z[kStep + (lane >> 2) + 8 * k];
+            sv[k] = fmaxf(z[kStep + (lane >> 2) + 8 * k], kLeastScale);
             lv[k] = log2_of(sv[k]);
         }
         bool outgrown = false;
 #pragma unroll
         for (int n = 0; n < N; ++n)
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
+            for (int y = 0; y < 2; ++y) {
+                float a = -CUDART_INF_F, b = -CUDART_INF_F;
 #pragma unroll
-                for (int y = 0; y < 2; ++y) {  // key k, head y
+                for (int k = 0; k < 4; ++k) {  // (a tile that is not there is zeros)
                     float &x = s[n][k >> 1][2 * (k & 1) + y];
-                    x = sk[k] != 0.f ? x * (unit[n][y] * sk[k]) : -CUDART_INF_F;
-                    outgrown = outgrown || x - ref[n][y] > kOutgrown || x + lv[k] - top[n][y] > 1.f;  // (the first: infinity)
+                    x = fmaf(x, unit[n][y] * sk[k], sk[k] != 0.f ? 0.f : -CUDART_INF_F);
+                    a = fmaxf(a, x);
+                    b = fmaxf(b, x + lv[k]);
                 }
+                outgrown = outgrown || a > ref[n][y] + kOutgrown || b > top[n][y] + (kTop + 1.f);
+            }
         if (__any_sync(0xffffffffu, outgrown)) {
 #pragma unroll
             for (int n = 0; n < N; ++n)
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
-                    float a = ref[n][y], b = top[n][y];
+                    float a = -CUDART_INF_F, b = -CUDART_INF_F;
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         a = fmaxf(a, s[n][k >> 1][2 * (k & 1) + y]);
@@ -262,8 +270,10 @@ struct Walk {
                         a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, d));
                         b = fmaxf(b, __shfl_xor_sync(0xffffffffu, b, d));
                     }
-                    l[n][y] *= a == -CUDART_INF_F ? 1.f : fast_exp2(ref[n][y] - a);
-                    const float f = b == -CUDART_INF_F ? 1.f : fast_exp2(top[n][y] - b);
+                    a = fmaxf(a, ref[n][y]);
+                    b = fmaxf(b - kTop, top[n][y]);
+                    l[n][y] *= fast_exp2(ref[n][y] - a);
+                    const float f = fast_exp2(top[n][y] - b);
                     ref[n][y] = a;
                     top[n][y] = b;
 #pragma unroll
@@ -279,8 +289,8 @@ struct Walk {
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
                     const float x = s[n][k >> 1][2 * (k & 1) + y];
-                    l[n][y] += fast_exp2(x - (ref[n][y] == -CUDART_INF_F ? 0.f : ref[n][y]));
-                    w[y] = x == -CUDART_INF_F || sv[k] == 0.f ? 0.f : fast_exp2(x - top[n][y] + kTop) * sv[k];
+                    l[n][y] += fast_exp2(x - ref[n][y]);
+                    w[y] = fast_exp2(x - top[n][y]) * sv[k];
                 }
                 const unsigned hi = pack(w[0], w[1]);
                 p[0][n][k] = turned(hi);
@@ -321,7 +331,7 @@ struct Walk {
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
                 const int h = 8 * n + 2 * t + y;
-                if (g == 0) { to[h] = ref[n][y]; to[kMaxHeads + h] = l[n][y]; }
+                if (g == 0) { to[h] = ref[n][y] == kNone ? -CUDART_INF_F : ref[n][y]; to[kMaxHeads + h] = l[n][y]; }
 #pragma unroll
                 for (int c = 0; c < F::kPieces; ++c)
                     *reinterpret_cast<float2 *>(to + 2 * kMaxHeads + h * D + 16 * c + 2 * g) = make_float2(o[c][n][y], o[c][n][y + 2]);
@@ -335,7 +345,7 @@ struct Walk {
             for (int y = 0; y < 2; ++y) {
 #pragma unroll
                 for (int d = 4; d < 32; d <<= 1) l[n][y] += __shfl_xor_sync(0xffffffffu, l[n][y], d);
-                const float f = ref[n][y] == -CUDART_INF_F ? 0.f : fast_exp2(top[n][y] - kTop - ref[n][y]);
+                const float f = fast_exp2(top[n][y] - ref[n][y]);  // (1 where no key was there)
 #pragma unroll
                 for (int c = 0; c < F::kPieces; ++c) { o[c][n][y] *= f; o[c][n][y + 2] *= f; }
             }
@@ -381,6 +391,9 @@ Divisor divisor(int d) {
     return r;
 }
 
+__device__ __forceinline__ void cp_async16_whole(unsigned dst, const void *src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
 // Waits until no more than `pending` of the last kMost groups of copies are on their way.
 template <int kMost>
 __device__ __forceinline__ void wait_for(unsigned pending) {
@@ -419,7 +432,7 @@ __global__ void __launch_bounds__(kThreads, Form<T, D, N>::kCtas) decode8_kernel
     const long long first = min(all, mine.first + per_warp * warp), end = min(all, mine.first + per_warp * (warp + 1));
     unsigned char *const ring_ptr = sm.ring[warp];
     const unsigned ring = wp::smem_addr(ring_ptr);
-    const bool half_pages = c.page % 16 == 0;  // 16 keys of a tile lie side by side
+    const bool plain = c.page % 16 == 0 && B.vec != 0;  // 16 keys of a tile lie side by side, in pieces of 16 bytes
     constexpr int kPieces = F::kPieces, kRowsAtOnce = 32 / kPieces;  // rows that 32 lanes fetch at once
     const int row_l = lane / kPieces, piece_l = lane % kPieces;
     unsigned bad = 0;
@@ -433,7 +446,7 @@ __global__ void __launch_bounds__(kThreads, Form<T, D, N>::kCtas) decode8_kernel
     } src = {};
     int src_n = 0;                      // the step of it that is fetched next
     int page = -1, row = 0;             // lane i: the page of key i of that step, -1: none; and its row there
-    unsigned issued = 0, used = 0;      // tiles: tile n is in place n % kStages
+    unsigned put = 0, take = 0, ahead = 0;  // the ring's places that are filled next, and multiplied next; how many are filled
     auto look_up = [&](const Source &f, int n, int &to, int &to_row) {
         const int walked = f.key0 + n * kStep + lane, key = W ? f.seen.key(walked) : walked;
         to = -1;
@@ -461,35 +474,51 @@ __global__ void __launch_bounds__(kThreads, Form<T, D, N>::kCtas) decode8_kernel
         const int own_page = page, own_row = row;
         if (src_n + 1 < src.n_steps) look_up(src, src_n + 1, page, row);
         const bool mine = own_page >= 0 && (!W || src.seen.sees(src.seen.key(src.key0 + src_n * kStep + lane)));
-        const unsigned place = issued % F::kStages * F::kPlace, there = __ballot_sync(0xffffffffu, mine);
+        const unsigned there = __ballot_sync(0xffffffffu, mine);
         const long long own = own_page >= 0 ? (long long)own_page * c.s_p + (long long)own_row * c.s_t : 0;
         const long long z = mine ? (long long)own_page * B.sc.s_p + (long long)B.block.quotient((unsigned)own_row) * B.sc.s_b + src.kvh * B.sc.s_h : 0;
-        cp_async4_or_zero(ring + place + 2 * F::kTile + lane * 4, B.sc.k + z, mine ? 4 : 0);
-        cp_async4_or_zero(ring + place + 2 * F::kTile + kStep * 4 + lane * 4, B.sc.v + z, mine ? 4 : 0);
-        const long long base0 = __shfl_sync(0xffffffffu, own, 0), base1 = __shfl_sync(0xffffffffu, own, 16), head = src.kvh * c.s_h + piece_l * 16;
+        const unsigned to = ring + put * F::kPlace;
+        cp_async4_or_zero(to + 2 * F::kTile + lane * 4, B.sc.k + z, mine ? 4 : 0);
+        cp_async4_or_zero(to + 2 * F::kTile + kStep * 4 + lane * 4, B.sc.v + z, mine ? 4 : 0);
+        const long long head = src.kvh * c.s_h + piece_l * 16;
+        if (plain && there == 0xffffffffu) {
 #pragma unroll
-        for (int r0 = 0; r0 < kStep; r0 += kRowsAtOnce) {
-            const int r = r0 + row_l;
-            const bool upper = kRowsAtOnce > 16 ? r >= 16 : r0 >= 16;
-            long long e = upper ? base1 + (r - 16) * c.s_t : base0 + r * c.s_t;
-            if (!half_pages) e = __shfl_sync(0xffffffffu, own, r);
-            const bool is = (there >> r) & 1u;
-            e = is ? e + head : 0;
-            const unsigned char *const ks = (const unsigned char *)A.a.k + e, *const vs = (const unsigned char *)A.a.v + e;
-            const unsigned to = place + piece_at<D>(r, piece_l);
-            if (B.vec) {
-                wp::cp_async16(ring + to, ks, is ? 16 : 0);
-                wp::cp_async16(ring + to + F::kTile, vs, is ? 16 : 0);
-            } else {
-#pragma unroll 4
-                for (int i = 0; i < 16; ++i) {
-                    ring_ptr[to + i] = is ? ks[i] : 0;
-                    ring_ptr[to + F::kTile + i] = is ? vs[i] : 0;
+            for (int half = 0; half < (kRowsAtOnce > 16 ? 1 : 2); ++half) {
+                const long long base = __shfl_sync(0xffffffffu, own, kRowsAtOnce > 16 ? lane & 16 : half * 16) + head + (row_l & 15) * c.s_t;
+                const unsigned char *ks = (const unsigned char *)A.a.k + base, *vs = (const unsigned char *)A.a.v + base;
+#pragma unroll
+                for (int r0 = half * 16; r0 < (kRowsAtOnce > 16 ? 32 : half * 16 + 16); r0 += kRowsAtOnce) {
+                    const unsigned at = to + piece_at<D>(r0 + row_l, piece_l);
+                    cp_async16_whole(at, ks);
+                    cp_async16_whole(at + F::kTile, vs);
+                    ks += kRowsAtOnce * c.s_t;
+                    vs += kRowsAtOnce * c.s_t;
+                }
+            }
+        } else {
+#pragma unroll 1
+            for (int r0 = 0; r0 < kStep; r0 += kRowsAtOnce) {
+                const int r = r0 + row_l;
+                const long long e0 = __shfl_sync(0xffffffffu, own, r);
+                const bool is = (there >> r) & 1u;
+                const long long e = is ? e0 + head : 0;
+                const unsigned char *const ks = (const unsigned char *)A.a.k + e, *const vs = (const unsigned char *)A.a.v + e;
+                const unsigned at = put * F::kPlace + piece_at<D>(r, piece_l);
+                if (B.vec) {
+                    wp::cp_async16(ring + at, ks, is ? 16 : 0);
+                    wp::cp_async16(ring + at + F::kTile, vs, is ? 16 : 0);
+                } else {
+#pragma unroll 1
+                    for (int i = 0; i < 16; ++i) {
+                        ring_ptr[at + i] = is ? ks[i] : 0;
+                        ring_ptr[at + F::kTile + i] = is ? vs[i] : 0;
+                    }
                 }
             }
         }
         wp::cp_async_commit();
-        ++issued;
+        put = put + 1 == F::kStages ? 0 : put + 1;
+        ++ahead;
         ++src_n;
     };
     Four<T> raw[F::kPieces][N];
@@ -504,17 +533,13 @@ __global__ void __launch_bounds__(kThreads, Form<T, D, N>::kCtas) decode8_kernel
     Place pl = {0, 0, 0};
     int n_pieces = 0;
     if (lane < 2) sm.piece[2 * warp + lane].slot = -1;
+    if (tid == 0) sm.n_parts = 0;
     __syncwarp();
-    Segment sg = open_segment<W, kStep, kOpen>(A, first, end, lane, pl);
-    if (sg.next >= 0) {
-        src = source_of(sg);
-        look_up(src, 0, page, row);
-        if constexpr (F::kQInRegs) load_q(sg);
-        for (int n = 0; n < F::kStages - 1 && n < src.n_steps; ++n) fetch();
-    }
-    while (sg.next >= 0) {
-        const int n_steps = (sg.key_end - sg.key0 + kStep - 1) / kStep;
-        // the segment behind, and the pages of its first tile
+    // (Every part of the work stands once in the code: its first pass comes from cold instruction caches.)
+    Segment sg = {};
+    sg.next = first;
+    for (bool begun = false; ; begun = true) {
+        // the segment behind sg, and the pages of its first tile
         const Segment next = open_segment<W, kStep, kOpen>(A, sg.next, end, lane, pl);
         bool waits = next.next >= 0;  // it is not yet fetched from
         int next_page = -1, next_row = 0;
@@ -523,51 +548,72 @@ __global__ void __launch_bounds__(kThreads, Form<T, D, N>::kCtas) decode8_kernel
             behind = source_of(next);
             look_up(behind, 0, next_page, next_row);
         }
-        if constexpr (!F::kQInRegs) load_q(sg);
-        Walk<T, D, N> walk;
-        walk.begin(sm, warp, raw, A.a.scale_log2, lane);
-        __syncwarp();
-        for (int n = 0; n < n_steps; ++n) {
-            while (issued - used < F::kStages) {
-                if (src_n == src.n_steps) {
-                    if (!waits) break;
-                    waits = false;
-                    src = behind;
-                    src_n = 0;
-                    page = next_page;
-                    row = next_row;
-                }
-                fetch();
-            }
-            wait_for<F::kStages - 1>(issued - used - 1);  // copies that may still be on their way: those of later tiles
-            __syncwarp();
-            const unsigned place = used % F::kStages * F::kPlace;
-            walk.step(sm, warp, ring + place, reinterpret_cast<const float *>(ring_ptr + place + 2 * F::kTile), lane);
-            __syncwarp();  // (the tile is read before its place is filled again)
-            ++used;
-        }
-        if (waits) {
+        auto go_on = [&] {
+            waits = false;
             src = behind;
             src_n = 0;
             page = next_page;
             row = next_row;
+        };
+        if (!begun) {
+            if (!waits) break;
+            go_on();
+            if constexpr (F::kQInRegs) load_q(next);
+            sg = next;
+            continue;
         }
-        if (F::kQInRegs && next.next >= 0) load_q(next);
+        if constexpr (!F::kQInRegs) load_q(sg);
+        Walk<T, D, N> walk;
+        const int n_steps = (sg.key_end - sg.key0 + kStep - 1) / kStep;
+        for (int n = 0; n < n_steps; ++n) {
+            while (ahead < F::kStages) {
+                if (src_n == src.n_steps) {
+                    if (!waits) break;
+                    go_on();
+                }
+                fetch();
+            }
+            if (n == 0) {
+                walk.begin(sm, warp, raw, A.a.scale_log2, lane);
+                if (F::kQEarly && next.next >= 0) load_q(next);
+                __syncwarp();
+            }
+            wait_for<F::kStages - 1>(ahead - 1);  // copies that may still be on their way: those of later tiles
+            __syncwarp();
+            const unsigned place = take * F::kPlace;
+            walk.step(sm, warp, ring + place, reinterpret_cast<const float *>(ring_ptr + place + 2 * F::kTile), lane);
+            __syncwarp();  // (the tile is read before its place is filled again)
+            take = take + 1 == F::kStages ? 0 : take + 1;
+            --ahead;
+        }
+        if (waits) go_on();
+        if (F::kQInRegs && !F::kQEarly && next.next >= 0) load_q(next);
         walk.close();
         const long long to_row = (long long)sg.slot * A.a.H + sg.h0;
         if (sg.whole) {
             walk.write(A, to_row, sg.heads, B.pairs != 0, lane);
-        } else {  // the warp's first segment, or its last one: that one stays in the ring, which is done with
-            float *const to = next.next >= 0 ? A.warp_parts + ((long long)blockIdx.x * kWarps + warp) * kMaxHeads * (D + 2) : reinterpret_cast<float *>(ring_ptr);
+        } else {
+            // The warp's first segment or its last one, which stays in the ring: that is done with. A first one that others follow ends its owner: the
+            // first warp's began in another CTA and is left to the joins as it is.
+            const bool last = next.next < 0;
+            float *const to = last        ? reinterpret_cast<float *>(ring_ptr)
+                              : warp == 0 ? part_of(A, (int)blockIdx.x, 0)
+                              : F::kFirstHere ? sm.first[F::kFirstHere ? warp - 1 : 0]
+                                              : A.warp_parts + ((long long)blockIdx.x * kWarps + warp) * kMaxHeads * (D + 2);
             walk.leave(to, lane);
-            if (lane == 0) sm.piece[2 * warp + n_pieces] = {to, sg.owner_end, sg.slot, sg.h0, sg.heads, sg.key0 == 0, sg.next == sg.owner_end};
-            ++n_pieces;
+            if (!last && warp == 0) {
+                if (lane == 0) sm.n_parts = 1;
+            } else {
+                if (lane == 0) sm.piece[2 * warp + n_pieces] = {to, sg.owner_end, sg.slot, sg.h0, sg.heads, sg.key0 == 0, sg.next == sg.owner_end};
+                ++n_pieces;
+            }
         }
+        if (next.next < 0) break;
         sg = next;
     }
     __syncthreads();
     // The warps' pieces side by side: those of one owner are joined, and what is not all of it is left to the joins (two at most)
-    int n_parts = 0;
+    int n_parts = sm.n_parts;
     Left left = {};
     for (int k0 = 0, k1; k0 < 2 * kWarps; k0 = k1) {
         const Piece p = sm.piece[k0];
