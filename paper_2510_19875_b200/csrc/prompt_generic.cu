@@ -69,7 +69,7 @@ __global__ void __launch_bounds__(kThreads) prompt_kernel(PromptGeom g, const T 
     };
     const int most = keys_of(n_rows - 1);
     Walked wk = {};
-    if constexpr (W) wk = walked_keys<kKeys>(g, (int)(row_base / g.hpg) + shift, sk.n);
+    if constexpr (W) wk = walked_keys(g, kKeys, (int)(row_base / g.hpg) + shift, sk.n);
     const int walked = most - wk.gap;  // keys without the gap
     auto key_of = [&](long long j) -> long long { return W && j >= wk.sink_keys ? j + wk.gap : j; };
     const T *const qs = q + (long long)sq.first * g.qs_t + (long long)kvh * g.hpg * g.qs_h;

@@ -49,7 +49,7 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas) prompt_mma_kernel(co
         return min(sk.n, max(0, tok + sk.n - sq.n + 1));
     };
     Walked wk = {};
-    if constexpr (W) wk = walked_keys<kKeys>(g, (int)(row_base / g.hpg) + sk.n - sq.n, sk.n);
+    if constexpr (W) wk = walked_keys(g, kKeys, (int)(row_base / g.hpg) + sk.n - sq.n, sk.n);
     const int most = keys_of(n_rows - 1), walked = most - wk.gap, warp_most = keys_of(warp * 16 + 15);
     const __nv_bfloat16 *const qs = q + (long long)sq.first * g.qs_t + (long long)kvh * g.hpg * g.qs_h;
     const __nv_bfloat16 *const ks = k + (long long)sk.first * g.ks_t + (long long)kvh * g.ks_h;

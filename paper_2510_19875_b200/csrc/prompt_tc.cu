@@ -14,6 +14,9 @@
 // Order of the issuing warp, per key tile: P_0 V_j, Q_0 K_(j+1), P_1 V_j, Q_1 K_(j+1). MMAs of one thread run in order, so that S_X
 // may overwrite P_X behind its product, and a tile's logits being there says that its last product is, too.
 //
+// Where there is a window, a pair of tiles walks the sinks and then, behind a gap, the keys from the first row's window on, wherever that begins. Up to 16 sinks
+// are the first rows of the first tile (which comes in pieces of 16 rows), more of them have tiles of their own.
+//
 // Roles (384 threads): warp 0 loads Q, K and V by TMA (one ring for K and V, in the order of their use); warp 1 issues the MMAs and
 // owns TMEM; warp 2 writes zeros over the rows of a V tile behind the sequence's last key (a weight of zero times what lies
 // there, which may be anything, has to be zero); warps 4..7 and 8..11 are the softmax of the two tiles and store their output.
@@ -34,6 +37,7 @@ using namespace tc;
 
 constexpr int kThreads = 384;
 constexpr int kRows = 128, kKeys = 128;  // of a tile
+constexpr int kFewSinks = 16;            // rows of a box of the tile that sinks share with others
 constexpr int kMaxSeqs = 256;            // of a launch
 constexpr int kMaxLevels = 2048;         // items of a kv head that are put in order
 constexpr long long kMaxItems = 0x7fffffffll - (1 << 20);
@@ -74,6 +78,7 @@ struct Tail {
 
 struct Params {
     PromptGeom g;
+    int sink_unit; // kFewSinks: the sinks share a tile with the window's first keys; kKeys: they have their own
     int per_tile;  // tokens of a tile: 128 / hpg
     int heads;     // kv heads whose items are walked together
 };
@@ -86,8 +91,12 @@ struct Item {
     int most;             // of both
     Walked wk;            // (where there is a window)
 };
+// The key that column 0 of key tile j has, or would have if the sinks were not in its place.
 template <bool W>
-__device__ __forceinline__ int first_key(const Item &it, int j) { return W ? it.wk.key(j * kKeys) : j * kKeys; }  // of key tile j
+__device__ __forceinline__ int first_key(const Params &P, const Item &it, int j) {
+    if constexpr (!W) return j * kKeys;
+    return j * kKeys < it.wk.sink_keys && P.sink_unit == kKeys ? j * kKeys : j * kKeys + it.wk.gap;
+}
 
 // The first sequence whose levels end behind the nth.
 template <class F>
@@ -121,7 +130,7 @@ __device__ __forceinline__ Item item_at(const Params &P, const Tail<F> *tl, int 
     const int pairs = ceil_div(it.s.q_n, 2 * P.per_tile);
     it.tok0 = (pairs - 1 - level) * 2 * P.per_tile;  // late tokens, with the most keys, first
     it.most = 0;
-    it.wk = W ? walked_keys<kKeys>(g, it.tok0 + it.s.k_n - it.s.q_n, it.s.k_n) : Walked{0, 0};
+    it.wk = W ? walked_keys(g, P.sink_unit, it.tok0 + it.s.k_n - it.s.q_n, it.s.k_n) : Walked{0, 0};
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
         const int t0 = it.tok0 + x * P.per_tile;
@@ -150,7 +159,7 @@ struct Use {
 };
 
 template <bool W, class F>
-__device__ void load_role(const Params &P, const CUtensorMap *tq, const CUtensorMap *tk, const CUtensorMap *tv, Tail<F> *tl,
+__device__ void load_role(const Params &P, const CUtensorMap *tq, const CUtensorMap *tk, const CUtensorMap *tv, const CUtensorMap *few, Tail<F> *tl,
                           unsigned q_smem, unsigned ring) {
     Use<F> use;
     unsigned n_q[2] = {0, 0};
@@ -159,8 +168,16 @@ __device__ void load_role(const Params &P, const CUtensorMap *tq, const CUtensor
         if (elect_one()) {
             const unsigned bar = smem_u32(raw ? &tl->v_raw[use.stage()] : &tl->full[use.stage()]), dst = ring + use.stage() * F::kTile;
             mbar_arrive_expect_tx(bar, F::kTile);
+            if (W && j == 0 && P.sink_unit == kFewSinks && it.wk.gap > 0 && it.wk.sink_keys > 0) {
+#pragma unroll 1
+                for (int r = 0; r < kKeys; r += kFewSinks)
 #pragma unroll
-            for (int c = 0; c < F::kHalves; ++c) tma_load_4d(dst + c * F::kHalf, map, bar, c * 64, it.s.k_first + first_key<W>(it, j), it.kvh, 0);
+                    for (int c = 0; c < F::kHalves; ++c)
+                        tma_load_4d(dst + c * F::kHalf + r * 128, few + (map == tv ? 1 : 0), bar, c * 64, it.s.k_first + it.wk.key(r), it.kvh, 0);
+            } else {
+#pragma unroll
+                for (int c = 0; c < F::kHalves; ++c) tma_load_4d(dst + c * F::kHalf, map, bar, c * 64, it.s.k_first + first_key<W>(P, it, j), it.kvh, 0);
+            }
         }
         __syncwarp();
         ++use.u;
@@ -185,7 +202,7 @@ __device__ void load_role(const Params &P, const CUtensorMap *tq, const CUtensor
         }
         if (it.n[0] <= 0 && !kv(it, tk, 0, false)) return;
         for (int j = 0; j < it.most; ++j) {
-            if (!kv(it, tv, j, (long long)first_key<W>(it, j) + kKeys > it.s.k_n)) return;
+            if (!kv(it, tv, j, (long long)first_key<W>(P, it, j) + kKeys > it.s.k_n)) return;
             if (j + 1 < it.most && !kv(it, tk, j + 1, false)) return;
         }
     }
@@ -200,7 +217,7 @@ __device__ void zero_role(const Params &P, Tail<F> *tl, unsigned char *ring, int
         const Item it = item_at<W>(P, tl, id);
         if (it.most == 0) continue;
         use.u += 2 * (unsigned)it.most;
-        const int last_key = first_key<W>(it, it.most - 1);  // (of the tiles the last alone can reach beyond the last key)
+        const int last_key = first_key<W>(P, it, it.most - 1);  // (of the tiles the last alone can reach beyond the last key)
         if ((long long)last_key + kKeys <= it.s.k_n) continue;
         Use<F> last;
         last.u = use.u - 1;
@@ -360,14 +377,31 @@ __device__ void softmax_role(const Params &P, Tail<F> *tl, unsigned tmem, int t)
 #pragma unroll
             for (int c = 0; c < 4; ++c) tmem_ld_32x32_issue(s_addr + c * 32, sr[c >> 1] + (c & 1) * 32);
             tmem_ld_wait();
-            const int base = first_key<W>(it, j), n_hi = min(keys - base, kKeys);
+            const int base = first_key<W>(P, it, j);
+            int n_hi = min(keys - base, kKeys);
             if constexpr (W) {  // keys between the sinks and the window
-                const int from = max(g.sinks - base, 0), to = min(low - base, kKeys);
-                if (__any_sync(0xffffffffu, from < to)) {
+                const bool gap = it.wk.gap > 0, own_tile = P.sink_unit == kKeys;
+                const int to = min(low - base, kKeys);  // columns from there on are the window's
+                if (gap && own_tile && j * kKeys < it.wk.sink_keys) {
+                    n_hi = min(n_hi, g.sinks - base);
+                } else {
+                    // columns in front of `from` are sinks: none where the sinks are further back, few where they share the tile
+                    const int from = gap ? (j == 0 && !own_tile ? min(g.sinks, kFewSinks) : 0) : max(g.sinks - base, 0);
+                    if (__any_sync(0xffffffffu, from < to)) {
+                        if (gap) {
 #pragma unroll
-                    for (int i = 0; i < 64; ++i) {
-                        sr[0][i] = i >= from && i < to ? 0xff800000u : sr[0][i];
-                        sr[1][i] = i + 64 >= from && i + 64 < to ? 0xff800000u : sr[1][i];
+                            for (int i = 0; i < 64; ++i) {
+                                if (i < kFewSinks) sr[0][i] = i < to && i >= from ? 0xff800000u : sr[0][i];
+                                else sr[0][i] = i < to ? 0xff800000u : sr[0][i];
+                                sr[1][i] = i + 64 < to ? 0xff800000u : sr[1][i];
+                            }
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 64; ++i) {
+                                sr[0][i] = i >= from && i < to ? 0xff800000u : sr[0][i];
+                                sr[1][i] = i + 64 >= from && i + 64 < to ? 0xff800000u : sr[1][i];
+                            }
+                        }
                     }
                 }
             }
@@ -465,10 +499,12 @@ __device__ void softmax_role(const Params &P, Tail<F> *tl, unsigned tmem, int t)
     }
 }
 
+struct Few { CUtensorMap map[2]; };  // K and V in boxes of kFewSinks rows
+
 template <class F, bool W>
 __global__ void __launch_bounds__(kThreads, 1)
 prompt_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
-                 const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ Params P) {
+                 const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ Few few, const __grid_constant__ Params P) {
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char *const smem = aligned_smem(smem_raw);
     unsigned char *const ring = smem + 2 * F::kTile;
@@ -540,7 +576,7 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
     // a CTA's sum then, and counting costs more than order gives (us as the sequences lie, and put in order all the same, 28 / 4 heads: 64 prompts of 500 tokens
     // 222, 273; of 100 to 900 311, 351; of 50 to 2000 337, 361; 32 / 8 heads 234, 259; 304, 315; 361, 363).
     const int n_levels = tl->n_levels;
-    const bool sorted = !W && g.n_seqs > 1 && tl->n_items > (int)gridDim.x && n_levels <= kMaxLevels && n_levels * g.n_seqs <= 16 * kThreads;
+    const bool sorted = g.n_seqs > 1 && tl->n_items > (int)gridDim.x && n_levels <= kMaxLevels && n_levels * g.n_seqs <= 16 * kThreads;
     if (tid == 0) tl->sorted = sorted ? 1 : 0;
     for (int i = tid; sorted && i < n_levels; i += kThreads) {
         const int own = sequence_of(tl, g.n_seqs, i), level = i - (own > 0 ? tl->level_end[own - 1] : 0), span2 = 2 * P.per_tile;
@@ -565,7 +601,7 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
     }
     __syncthreads();
     if (warp < 4) {
-        if (warp == 0) load_role<W>(P, &tmap_q, &tmap_k, &tmap_v, tl, smem_u32(smem), smem_u32(ring));
+        if (warp == 0) load_role<W>(P, &tmap_q, &tmap_k, &tmap_v, few.map, tl, smem_u32(smem), smem_u32(ring));
         else if (warp == 1) mma_role<W>(P, tl, smem_u32(smem), smem_u32(ring), tmem);
         else if (warp == 2) zero_role<W>(P, tl, ring, lane);
     } else {
@@ -602,6 +638,13 @@ stream_status launch(const PromptGeom &g, const void *q, const void *k, const vo
     if (rc != STREAM_OK) return rc;
     rc = make_map_bf16(&tv, v, g.total_k, g.G, 1, g.ks_t, g.ks_h, 0, "v", kKeys, g.d);
     if (rc != STREAM_OK) return rc;
+    P.sink_unit = W && g.sinks <= kFewSinks ? kFewSinks : kKeys;
+    Few few = {};
+    if (W && g.sinks > 0 && g.sinks <= kFewSinks) {
+        rc = make_map_bf16(&few.map[0], k, g.total_k, g.G, 1, g.ks_t, g.ks_h, 0, "k", kFewSinks, g.d);
+        if (rc == STREAM_OK) rc = make_map_bf16(&few.map[1], v, g.total_k, g.G, 1, g.ks_t, g.ks_h, 0, "v", kFewSinks, g.d);
+        if (rc != STREAM_OK) return rc;
+    }
     const int smem = (2 + F::kStages) * F::kTile + (int)sizeof(Tail<F>) + 1024;
     static_assert((2 + F::kStages) * F::kTile + (int)sizeof(Tail<F>) + 1024 <= 232448, "what a CTA may have");
     static DeviceFlags done;
@@ -614,7 +657,7 @@ stream_status launch(const PromptGeom &g, const void *q, const void *k, const vo
         P.g.cu_q = g.cu_q + s0;
         P.g.cu_k = g.cu_k + s0;
         const long long items = ((long long)g.total_q / (2 * P.per_tile) + P.g.n_seqs) * g.G;  // at most
-        e = launch_early(prompt_tc_kernel<F, W>, (unsigned)(items < n_sm ? items : n_sm), kThreads, smem, st, tq, tk, tv, P);
+        e = launch_early(prompt_tc_kernel<F, W>, (unsigned)(items < n_sm ? items : n_sm), kThreads, smem, st, tq, tk, tv, few, P);
         if (e != cudaSuccess) return cuda_fail(e, "prompt_tc launch");
     }
     return STREAM_OK;

@@ -21,15 +21,14 @@ struct PromptGeom {
     int window, sinks; // window > 0: a query at position p sees the keys j <= p with j > p - window or j < sinks
 };
 
-// What a tile of rows walks of the keys where there is a window, in tiles of kKeys: those of the sinks, and behind a gap all from the first key that
-// the first row's window has. (Positions below 0 see nothing. Counted without the gap, a tile's first key is a multiple of kKeys.)
+// What a tile of rows walks of the keys where there is a window: those of the sinks, in whole units, and behind a gap all from the first key that the
+// first row's window has. Tiles are cut from the keys as they are counted without the gap. (Positions below 0 see nothing.)
 struct Walked {
-    int sink_keys, gap;  // keys in front of the gap, a multiple of kKeys; keys of the gap
+    int sink_keys, gap;  // keys in front of the gap, a multiple of the unit; keys of the gap
     __device__ __forceinline__ int key(int walked) const { return walked < sink_keys ? walked : walked + gap; }
 };
-template <int kKeys>
-__device__ __forceinline__ Walked walked_keys(const PromptGeom &g, int first_pos, int n_keys) {
-    const int low = max(0, max(first_pos, 0) - g.window + 1), sinks = (min(g.sinks, n_keys) + kKeys - 1) / kKeys * kKeys;
+__device__ __forceinline__ Walked walked_keys(const PromptGeom &g, int unit, int first_pos, int n_keys) {
+    const int low = max(0, max(first_pos, 0) - g.window + 1), sinks = (min(g.sinks, n_keys) + unit - 1) / unit * unit;
     return {sinks, max(0, low - sinks)};
 }
 // The first key of a position's window.
