@@ -39,6 +39,7 @@ constexpr int kThreads = 384;
 constexpr int kRows = 128, kKeys = 128;  // of a tile
 constexpr int kFewSinks = 16;            // rows of a box of the tile that sinks share with others
 constexpr int kMaxSeqs = 256;            // of a launch
+constexpr int kKnown = 64;               // items of a CTA that are worked out once (each role would take some 2000 cycles for each of them)
 constexpr int kMaxLevels = 2048;         // items of a kv head that are put in order
 constexpr long long kMaxItems = 0x7fffffffll - (1 << 20);
 constexpr float kOutgrown = 30.f;        // log2
@@ -59,6 +60,15 @@ constexpr unsigned kHi = desc_hi_sw128(1024);
 
 struct Seq { int q_first, q_n, k_first, k_n; };
 
+// What a CTA works on.
+struct Item {
+    Seq s;
+    int kvh, tok0;        // the first tile's first token; the second one's is per_tile later
+    int n[2];             // key tiles of each; -1: there is no such tile
+    int most;             // of both
+    Walked wk;            // (where there is a window)
+};
+
 template <class F>
 struct Tail {
     unsigned long long full[F::kStages], empty[F::kStages];
@@ -74,6 +84,7 @@ struct Tail {
     Seq seq[kMaxSeqs];                                   // the longest first
     int level_end[kMaxSeqs];                             // levels (pairs of tiles, items of a kv head) of the sequences up to and with this one
     uint4 stage[8][128];                                 // of each softmax warp: 32 rows x 32 channels of the output
+    Item items[kKnown];                                  // of this CTA: the first ones
 };
 
 struct Params {
@@ -83,14 +94,6 @@ struct Params {
     int heads;     // kv heads whose items are walked together
 };
 
-// What a CTA works on.
-struct Item {
-    Seq s;
-    int kvh, tok0;        // the first tile's first token; the second one's is per_tile later
-    int n[2];             // key tiles of each; -1: there is no such tile
-    int most;             // of both
-    Walked wk;            // (where there is a window)
-};
 // The key that column 0 of key tile j has, or would have if the sinks were not in its place.
 template <bool W>
 __device__ __forceinline__ int first_key(const Params &P, const Item &it, int j) {
@@ -115,9 +118,10 @@ __device__ __forceinline__ Item item_at(const Params &P, const Tail<F> *tl, int 
     const PromptGeom &g = P.g;
     Item it;
     // some kv heads at a time, and of them the sequences' levels (pairs of tiles) in order, head by head
-    const int per_phase = tl->n_levels * P.heads, phase = id / per_phase, rem = id - phase * per_phase;
-    const int heads = min(P.heads, g.G - phase * P.heads), nth = rem / heads;
-    it.kvh = phase * P.heads + rem - nth * heads;
+    const unsigned per_phase = (unsigned)(tl->n_levels * P.heads), phase = P.heads == g.G ? 0 : (unsigned)id / per_phase, rem = (unsigned)id - phase * per_phase;
+    const unsigned heads = (unsigned)min(P.heads, g.G - (int)phase * P.heads);
+    const int nth = (int)(rem / heads);
+    it.kvh = (int)(phase * P.heads + rem - nth * heads);
     int lo = 0, level;
     if (tl->sorted) {
         lo = (int)(tl->order[nth] >> 12);
@@ -140,6 +144,12 @@ __device__ __forceinline__ Item item_at(const Params &P, const Tail<F> *tl, int 
         it.most = max(it.most, it.n[x]);
     }
     return it;
+}
+
+template <bool W, class F>
+__device__ __forceinline__ Item nth_of_cta(const Params &P, const Tail<F> *tl, int round, int id) {
+    if (round < kKnown) return tl->items[round];
+    return item_at<W>(P, tl, id);
 }
 
 template <class F>
@@ -184,7 +194,7 @@ __device__ void load_role(const Params &P, const CUtensorMap *tq, const CUtensor
         return true;
     };
     for (int round = 0, id; (id = nth_item(round)) < tl->n_items; ++round) {
-        const Item it = item_at<W>(P, tl, id);
+        const Item it = nth_of_cta<W>(P, tl, round, id);
         if (it.most == 0) continue;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
@@ -214,7 +224,7 @@ __device__ void zero_role(const Params &P, Tail<F> *tl, unsigned char *ring, int
     Use<F> use;
     unsigned parity = 0;  // of each stage's barrier
     for (int round = 0, id; (id = nth_item(round)) < tl->n_items; ++round) {
-        const Item it = item_at<W>(P, tl, id);
+        const Item it = nth_of_cta<W>(P, tl, round, id);
         if (it.most == 0) continue;
         use.u += 2 * (unsigned)it.most;
         const int last_key = first_key<W>(P, it, it.most - 1);  // (of the tiles the last alone can reach beyond the last key)
@@ -267,7 +277,7 @@ __device__ void mma_role(const Params &P, Tail<F> *tl, unsigned q_smem, unsigned
         __syncwarp();
     };
     for (int round = 0, id; (id = nth_item(round)) < tl->n_items; ++round) {
-        const Item it = item_at<W>(P, tl, id);
+        const Item it = nth_of_cta<W>(P, tl, round, id);
         if (it.most == 0) continue;
         if (!wait_w(&tl->full[use.stage()], use.phase(), tl, 1011)) return;
 #pragma unroll
@@ -360,8 +370,8 @@ __device__ void softmax_role(const Params &P, Tail<F> *tl, unsigned tmem, int t)
     unsigned n_s = 0, n_o = 0;
     __nv_bfloat16 *const out = (__nv_bfloat16 *)g.out;
     for (int round = 0, id; (id = nth_item(round)) < tl->n_items; ++round) {
-        const Item it = item_at<W>(P, tl, id);
-        const int n_tiles = it.n[x];
+        const Item it = nth_of_cta<W>(P, tl, round, id);
+        const int n_tiles = x == 0 ? it.n[0] : it.n[1];
         if (n_tiles < 0) continue;
         const int tok0 = it.tok0 + x * P.per_tile, tok = tok0 + tok_r;
         // rows that are none see what the last one does, so that they cost nothing
@@ -463,26 +473,27 @@ __device__ void softmax_role(const Params &P, Tail<F> *tl, unsigned tmem, int t)
             if (!wait_w(&tl->o_done[x], n_o++ & 1u, tl, 1022)) return;
             tc_fence_after();
         }
-#pragma unroll 1
-        for (int c = 0; c < F::D / 32; ++c) {
-            unsigned r[32];
-            if (n_tiles > 0) {
-                tmem_ld_32x32_issue(o_addr + c * 32, r);
-                tmem_ld_wait();
-                if (c == F::D / 32 - 1) {
-                    tc_fence_before();
-                    mbar_arrive_if(smem_u32(&tl->o_free[x]), lane == 0);
-                }
-            } else {  // (no key for any row)
+        unsigned r[F::D / 32][32];  // (in the place of the logits: the next item's products need not wait for the output)
+        if (n_tiles > 0) {
 #pragma unroll
-                for (int i = 0; i < 32; ++i) r[i] = 0u;
-            }
+            for (int c = 0; c < F::D / 32; ++c) tmem_ld_32x32_issue(o_addr + c * 32, r[c]);
+            tmem_ld_wait();
+            tc_fence_before();
+            mbar_arrive_if(smem_u32(&tl->o_free[x]), lane == 0);
+        } else {  // (no key for any row)
+#pragma unroll
+            for (int c = 0; c < F::D / 32; ++c)
+#pragma unroll
+                for (int i = 0; i < 32; ++i) r[c][i] = 0u;
+        }
+#pragma unroll
+        for (int c = 0; c < F::D / 32; ++c) {
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 unsigned w[4];
 #pragma unroll
                 for (int y = 0; y < 4; ++y) {
-                    const __nv_bfloat162 pk = __floats2bfloat162_rn(__uint_as_float(r[8 * u + 2 * y]) * inv, __uint_as_float(r[8 * u + 2 * y + 1]) * inv);
+                    const __nv_bfloat162 pk = __floats2bfloat162_rn(__uint_as_float(r[c][8 * u + 2 * y]) * inv, __uint_as_float(r[c][8 * u + 2 * y + 1]) * inv);
                     w[y] = *reinterpret_cast<const unsigned *>(&pk);
                 }
                 stage[lane * 4 + (u ^ ((lane >> 1) & 3))] = make_uint4(w[0], w[1], w[2], w[3]);
@@ -599,6 +610,8 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
             if (o != own) place += above(tl->seq[o], o < own ? v - 1 : v);
         tl->order[place] = (unsigned)own << 12 | (unsigned)level;
     }
+    __syncthreads();
+    if (tid < kKnown && nth_item(tid) < tl->n_items) tl->items[tid] = item_at<W>(P, tl, nth_item(tid));
     __syncthreads();
     if (warp < 4) {
         if (warp == 0) load_role<W>(P, &tmap_q, &tmap_k, &tmap_v, few.map, tl, smem_u32(smem), smem_u32(ring));

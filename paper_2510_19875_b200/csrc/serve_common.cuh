@@ -64,7 +64,8 @@ __device__ __forceinline__ int slot_of_row(const int32_t *cu, int n_slots, long 
 }
 // Tokens of a slot.
 __device__ __forceinline__ int tokens_of(const CacheGeom &c, int s) { return min(max(c.len[s], 0), c.max_pages * c.page); }
-__host__ __device__ __forceinline__ int ceil_div(int a, int b) { return (int)(((long long)a + b - 1) / b); }
+// a >= 0, b > 0. (A division of 64 bits is hundreds of cycles.)
+__host__ __device__ __forceinline__ int ceil_div(int a, int b) { return (int)(((unsigned)a + (unsigned)b - 1u) / (unsigned)b); }
 
 // The kernels that give every tile of `rows` rows of a kv head's queries a CTA: which sequence the nth one lies in, and its number
 // there. By a whole warp. seq < 0: there are fewer.
