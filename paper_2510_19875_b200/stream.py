@@ -864,10 +864,12 @@ def new_cache(n_slots: int, n_pages: int, page_size: int, max_pages: int, n_kv_h
 
 def new_cache8(n_slots: int, n_pages: int, page_size: int, max_pages: int, n_kv_heads: int, d: int, *, block: int, n_layers: int = 1,
                dtype: torch.dtype = torch.bfloat16, device="cuda") -> PagedCache8:
-    """An empty cache in 8 bits whose tokens share a scale in blocks of ``block``, which divides ``page_size``."""
+    """An empty cache in 8 bits whose tokens share a scale in blocks of ``block``, which divides ``page_size``. In memory a page has head after
+    head: rows of 128 bytes that lie side by side are read faster than rows a token apart (four chains of up to 131072 tokens, 8 kv heads,
+    d = 128: 52 us for 60)."""
     if block < 1 or page_size % block != 0:
         raise ValueError("block must be positive and divide page_size")
-    k, v = (torch.empty(n_layers, n_pages, page_size, n_kv_heads, d, dtype=torch.float8_e4m3fn, device=device) for _ in range(2))
+    k, v = (torch.empty(n_layers, n_pages, n_kv_heads, page_size, d, dtype=torch.float8_e4m3fn, device=device).transpose(2, 3) for _ in range(2))
     k_scale, v_scale = (torch.zeros(n_layers, n_pages, page_size // block, n_kv_heads, device=device) for _ in range(2))
     return PagedCache8(k, v, k_scale, v_scale, torch.full((n_slots, max_pages), -1, dtype=torch.int32, device=k.device),
                        torch.zeros(n_slots, dtype=torch.int32, device=k.device), torch.zeros(n_pages, dtype=torch.int32, device=k.device), dtype=dtype)
