@@ -349,7 +349,7 @@ constexpr size_t kLeftBytes = (kMaxGrid * sizeof(Left) + 255) & ~(size_t)255;
 
 namespace decode {
 
-Args args_of(const DecodeCall &a, void *workspace, int n_sm, int unit, int open) {
+Args args_of(const DecodeCall &a, void *workspace, int n_sm, int unit, int open, int least) {
     Args A;
     A.a = a;
     A.chunks = (a.hpg + kMaxHeads - 1) / kMaxHeads;
@@ -360,9 +360,9 @@ Args args_of(const DecodeCall &a, void *workspace, int n_sm, int unit, int open)
     A.warp_parts = A.parts + (size_t)kMaxGrid * 2 * kMaxHeads * (a.c.d + 2);
     long long keys = (long long)a.c.max_pages * a.c.page;  // of a slot, at most
     if (a.window > 0) keys = std::min(keys, (long long)a.window + a.sinks + 2 * (unit - 1));
-    const long long most = (long long)a.c.n_slots * A.per_slot * ((keys + unit - 1) / unit + open);
+    const long long most = (long long)a.c.n_slots * A.per_slot * ((keys + unit - 1) / unit + open), ctas = (most + least - 1) / least;
     const int want = 2 * n_sm < kMaxGrid ? 2 * n_sm : kMaxGrid;
-    A.grid = (int)(most < want ? most : want);
+    A.grid = (int)(ctas < want ? ctas : want);
     return A;
 }
 

@@ -41,7 +41,7 @@ struct Args {
 };
 
 // The arguments that follow from the call, and the grid at most; the joins' launch.
-Args args_of(const DecodeCall &a, void *workspace, int n_sm, int unit = kUnit64, int open = kOpen64);
+Args args_of(const DecodeCall &a, void *workspace, int n_sm, int unit = kUnit64, int open = kOpen64, int least = 1);  // least: places of a CTA
 cudaError_t launch_joins(const Args &A, int dtype, cudaStream_t st);
 
 // Rows of 16-byte pieces, up to 512 bytes. May lower A.grid.

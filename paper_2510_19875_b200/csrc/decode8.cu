@@ -694,7 +694,7 @@ stream_status launch_decode8(const DecodeCall &a, const Scales &sc, int dtype, v
     const int n_sm = current_sm_count();
     if (n_sm <= 0) { set_error("cannot read the SM count of the current device"); return STREAM_ERR_CUDA; }
     Args8 B;
-    B.A = args_of(a, workspace, n_sm, kStep, kOpen);
+    B.A = args_of(a, workspace, n_sm, kStep, kOpen, kWarps);
     B.sc = sc;
     B.page = divisor(a.c.page);
     B.block = divisor(sc.block);
