@@ -1,11 +1,13 @@
 // A paged cache in 8 bits: new tokens rounded into their pages, and tokens read back.
 //
 // A block's scale is the smallest power of two 2^e with amax <= 448 2^e, which the exponent and the fraction of amax say, so that x 2^-e is exact and
-// one rounding, to e4m3, is all there is. A group of threads has a block of one kv head's keys or values: their largest
-// element, the block's scale, the numbers. Which blocks have new tokens nobody has to count: n tokens touch n / block + 2 blocks at most, so that
-// slot s has the places cu[s] / block + 2 s and those behind it, up to the next slot's, and some of them stay empty. Both kernels move every
-// byte once (a new token's twice where a block is more than the group's registers hold) and are bound by HBM or, for few tokens, by the chain of
-// loads: offsets, lengths, page, tokens.
+// one rounding, to e4m3, is all there is. A group of threads (a warp, or a CTA where a block's new tokens are more than a warp's registers
+// hold) has a block of one kv head's keys or values: its largest element, of magnitudes compared as whole numbers, the block's scale, the numbers.
+// Which blocks have new tokens nobody has to count: n tokens touch n / block + 2 blocks at most, so that slot s has the places cu[s] / block + 2 s and
+// those behind it, up to the next slot's, and some of them stay empty. Both kernels move every byte once (a new token's twice where a block is more than
+// the group's registers hold). 18566 new tokens of 8 kv heads, d = 128, bf16, blocks of 64: 27 us, 114 MB at 64 % of the copy rate (6556 GB/s): a CTA's
+// chain of offsets, length, page, tokens, barrier and stores, of six CTAs an SM side by side (elements held as fp32, four of them: 65). 29562 tokens
+// read back: 31 us, 182 MB at 90 % (32 bytes of the output a lane, whose stores are halves of sectors: 37). 64 new tokens: 3.8 us, launch and chain.
 #include <cuda_fp8.h>
 
 #include "serve_common.cuh"
@@ -63,6 +65,26 @@ __device__ __forceinline__ void widen(const Piece<T> &r, float (&x)[8]) {
         }
     }
 }
+// The largest magnitude of a piece and of `top` as the bits of numbers without their signs, whose order is that of the numbers: of two bf16 at
+// once, or of an fp32. NaN is above all.
+template <class T>
+__device__ __forceinline__ unsigned larger(const Piece<T> &r, unsigned top) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+        const unsigned w[4] = {r.w[i].x, r.w[i].y, r.w[i].z, r.w[i].w};
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            if constexpr (sizeof(T) == 4) top = max(top, w[y] & 0x7fffffffu);
+            else top = __vmaxu2(top, w[y] & 0x7fff7fffu);
+        }
+    }
+    return top;
+}
+template <class T>
+__device__ __forceinline__ unsigned bits_of(unsigned top) {  // of the one number
+    if constexpr (sizeof(T) == 4) return top;
+    else return max(top << 16, top & 0xffff0000u);
+}
 __device__ __forceinline__ uint2 round8(const float (&x)[8], float f) {
     unsigned w[4];
 #pragma unroll
@@ -99,14 +121,15 @@ struct WriteArgs {
     long long s_t, s_h;      // elements, of x
     int vec_in, vec_out;
     long long places;        // of blocks
+    Divisor heads, page, block;
 };
 
 // Place of the first block of slot s.
-__device__ __forceinline__ long long place_of(const WriteArgs &a, int s) { return min(max(a.cu[s], 0), a.total) / a.sc.block + 2ll * s; }
+__device__ __forceinline__ long long place_of(const WriteArgs &a, int s) { return a.block.quotient((unsigned)min(max(a.cu[s], 0), a.total)) + 2ll * s; }
 
 // kGroup threads a block: 32, or all of the CTA's.
 template <class T, int kGroup>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 8 : 4) write8_kernel(const __grid_constant__ WriteArgs a) {
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 6 : 4) write8_kernel(const __grid_constant__ WriteArgs a) {
     __shared__ float tops[kThreads / 32];
     after_previous_kernel();
     const CacheGeom &c = a.c;
@@ -115,8 +138,8 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 8 : 4) write8_kerne
     const int lane = threadIdx.x & 31, me = threadIdx.x % kGroup, row_shift = 28 - __clz(c.d), block = a.sc.block;  // (2^row_shift pieces a row)
     const long long items = a.places * c.G * 2;
     for (long long it = (long long)blockIdx.x * kGroups + threadIdx.x / kGroup; it < items; it += (long long)gridDim.x * kGroups) {
-        const int kv = (int)(it & 1), h = (int)((it >> 1) % c.G);
-        const long long place = (it >> 1) / c.G;
+        const long long x2 = it >> 1, place = x2 >> 31 == 0 ? (long long)a.heads.quotient((unsigned)x2) : x2 / c.G;
+        const int kv = (int)(it & 1), h = (int)(x2 - place * c.G);
         int s = 0;
         for (int hi = c.n_slots; hi - s > 1;) {  // the last slot that begins at or before the place (32 candidates a step)
             const int step = (hi - s + 31) / 32;
@@ -128,33 +151,45 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 8 : 4) write8_kerne
         const Span sp = span_of(a.cu, s, a.total);
         const int len = tokens_of(c, s);
         const int start = max(len - sp.n, 0);  // the first new token (rows in front of the slot's first token are passed over)
-        const long long nth = place - place_of(a, s), lo64 = (start / block + nth) * block;
+        const long long nth = place - place_of(a, s), lo64 = ((int)a.block.quotient((unsigned)start) + nth) * block;
         if (nth < 0 || lo64 >= len || sp.n == 0) continue;  // (the whole group)
         const int lo = (int)lo64, hi = min(len, lo + block), first = max(lo, start);
-        const int page = c.table[(long long)s * c.max_pages + lo / c.page];  // (looked at behind the loads that do not need it)
-        const T *const from = (const T *)a.x[kv] + (long long)(sp.first + sp.n - (len - first)) * a.s_t + h * a.s_h;
-        const int n = (hi - first) << row_shift;
-        const bool held = n <= kGroup * kHold;
+        const int nth_page = (int)a.page.quotient((unsigned)lo), in_page = lo - nth_page * c.page;
+        const int page = c.table[(long long)s * c.max_pages + nth_page];
+        if ((unsigned)page >= (unsigned)c.n_pages) continue;
+        float *const scale_at = const_cast<float *>(kv ? a.sc.v : a.sc.k) + page * a.sc.s_p + a.block.quotient((unsigned)in_page) * a.sc.s_b + h * a.sc.s_h;
+        unsigned char *const to = a.pages[kv] + page * c.s_p + (long long)in_page * c.s_t + h * c.s_h;
+        // this thread's rows of the new ones: row0 and every `rows`-th from there on, a piece of each
+        const int rows = kGroup >> row_shift, row0 = me >> row_shift, piece = (me & ((1 << row_shift) - 1)) * 8, n = hi - first;
+        const T *const from = (const T *)a.x[kv] + (long long)(sp.first + sp.n - (len - first) + row0) * a.s_t + h * a.s_h + piece;
+        const long long step = rows * a.s_t;
+        const bool held = n <= rows * kHold;
         Piece<T> raw[kHold];
-        float x[8], top = 0.f;
-        for (int p0 = 0; p0 < n; p0 += kGroup * kHold) {
+        unsigned largest = 0;
+        {
+            const T *at = from;
+            for (int r = row0; r < n; r += rows * kHold) {
 #pragma unroll
-            for (int i = 0; i < kHold; ++i) {
-                const int p = p0 + i * kGroup + me;
-                if (p < n) raw[i] = load_piece(from + (long long)(p >> row_shift) * a.s_t + (p & ((1 << row_shift) - 1)) * 8, a.vec_in != 0);
-            }
-#pragma unroll
-            for (int i = 0; i < kHold; ++i) {
-                if (p0 + i * kGroup + me < n) {
-                    widen(raw[i], x);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[e]));
+                for (int i = 0; i < kHold; ++i) {
+                    raw[i] = Piece<T>{};
+                    if (r + i * rows < n) raw[i] = load_piece(at, a.vec_in != 0);
+                    at += step;
                 }
+#pragma unroll
+                for (int i = 0; i < kHold; ++i) largest = larger(raw[i], largest);
             }
         }
-        if ((unsigned)page >= (unsigned)c.n_pages) continue;
-        float *const scale_at = const_cast<float *>(kv ? a.sc.v : a.sc.k) + page * a.sc.s_p + (lo % c.page / block) * a.sc.s_b + h * a.sc.s_h;
-        unsigned char *const to = a.pages[kv] + page * c.s_p + (long long)(lo % c.page) * c.s_t + h * c.s_h;
+        float top = __uint_as_float(bits_of<T>(largest));
+        if (top != top) {  // NaN: which is no number to ask for a scale
+            top = 0.f;
+            const T *at = from;
+            for (int r = row0; r < n; r += rows, at += step) {
+                float x[8];
+                widen(load_piece(at, a.vec_in != 0), x);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[e]));
+            }
+        }
         const float had = first > lo ? *scale_at : 0.f;
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
@@ -183,17 +218,20 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 8 : 4) write8_kerne
                 store8(at, round8(y, f), a.vec_out != 0);
             }
         }
-        unsigned char *const dst = to + (long long)(first - lo) * c.s_t;
-        for (int p0 = 0; p0 < n; p0 += kGroup * kHold) {
+        unsigned char *dst = to + (long long)(first - lo + row0) * c.s_t + piece;
+        const long long step_out = rows * c.s_t;
+        const T *at = from;
+        for (int r = row0; r < n; r += rows * kHold) {
 #pragma unroll
             for (int i = 0; i < kHold; ++i) {
-                const int p = p0 + i * kGroup + me;
-                if (p < n) {
-                    const int row = p >> row_shift, piece = p & ((1 << row_shift) - 1);
-                    if (!held) raw[i] = load_piece(from + (long long)row * a.s_t + piece * 8, a.vec_in != 0);
+                if (r + i * rows < n) {
+                    if (!held) raw[i] = load_piece(at, a.vec_in != 0);
+                    float x[8];
                     widen(raw[i], x);
-                    store8(dst + (long long)row * c.s_t + piece * 8, round8(x, inv), a.vec_out != 0);
+                    store8(dst, round8(x, inv), a.vec_out != 0);
                 }
+                at += step;
+                dst += step_out;
             }
         }
     }
@@ -206,6 +244,7 @@ struct ReadArgs {
     void *x[2];
     const int32_t *cu;
     int total;
+    Divisor page, block;
 };
 
 // A warp a token; kPiece elements at a time: 16 bytes of the output, or one element where a row or an output is off its boundary.
@@ -214,23 +253,23 @@ template <class T, int kPiece>
 __global__ void __launch_bounds__(kThreads) read8_kernel(const __grid_constant__ ReadArgs a) {
     after_previous_kernel();
     const CacheGeom &c = a.c;
-    const int lane = threadIdx.x & 31, row_pieces = c.d / kPiece;
+    const int lane = threadIdx.x & 31, row_shift = 31 - __clz(c.d / kPiece);  // (2^row_shift pieces a row)
     for (long long t = (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); t < a.total; t += (long long)gridDim.x * (kThreads / 32)) {
         const int s = slot_of_row(a.cu, c.n_slots, t, lane);
         const Span sp = span_of(a.cu, s, a.total);
         if (t < sp.first || t >= (long long)sp.first + sp.n) continue;
         const long long pos = (long long)tokens_of(c, s) - sp.n + (t - sp.first);
-        const int page = pos >= 0 ? c.table[(long long)s * c.max_pages + (int)pos / c.page] : -1;
+        const int nth_page = pos >= 0 ? (int)a.page.quotient((unsigned)pos) : 0, page = pos >= 0 ? c.table[(long long)s * c.max_pages + nth_page] : -1;
         const bool there = (unsigned)page < (unsigned)c.n_pages;
-        const int in_page = there ? (int)pos % c.page : 0;
-        const long long from = there ? page * c.s_p + in_page * c.s_t : 0, z = there ? page * a.sc.s_p + in_page / a.sc.block * a.sc.s_b : 0;
-        const int pieces = c.G * row_pieces;
+        const int in_page = there ? (int)pos - nth_page * c.page : 0;
+        const long long from = there ? page * c.s_p + in_page * c.s_t : 0, z = there ? page * a.sc.s_p + a.block.quotient((unsigned)in_page) * a.sc.s_b : 0;
+        const int pieces = c.G << row_shift;
         for (int u0 = lane; u0 < pieces; u0 += 32 * kAhead) {
             unsigned w[kAhead][2][2];
             float scale[kAhead][2];
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
-                const int u = u0 + 32 * i, h = u / row_pieces, x = (u - h * row_pieces) * kPiece;
+                const int u = u0 + 32 * i, h = u >> row_shift, x = (u - (h << row_shift)) * kPiece;
 #pragma unroll
                 for (int kv = 0; kv < 2; ++kv) {
                     w[i][kv][0] = w[i][kv][1] = 0;
@@ -278,7 +317,8 @@ stream_status launch_write8(const CacheGeom &c, const Scales &sc, int dtype, con
     a.cu = cu_new; a.done = done; a.total = total; a.s_t = s_t; a.s_h = s_h;
     a.vec_in = on(16, k, v) && ((s_t | s_h) * e & 15) == 0;
     a.vec_out = on(8, k_pages, v_pages) && ((c.s_p | c.s_t | c.s_h) & 7) == 0;
-    a.places = total / sc.block + 2ll * c.n_slots;
+    a.places = total / sc.block + 2ll * c.n_slots; a.heads = make_divisor(c.G);
+    a.page = make_divisor(c.page); a.block = make_divisor(sc.block);
     const int n_sm = current_sm_count();
     if (n_sm <= 0) { set_error("cannot read the SM count of the current device"); return STREAM_ERR_CUDA; }
     // a warp a block where a block's new tokens fit its registers (few tokens a slot, or small blocks), else a CTA
@@ -299,6 +339,7 @@ stream_status launch_read8(const CacheGeom &c, const Scales &sc, int dtype, cons
     a.cu = cu; a.total = total;
     const int piece = dtype == STREAM_F32 ? 4 : 8;
     const bool vec = on(piece, k_pages, v_pages) && on(16, k_out, v_out) && ((c.s_p | c.s_t | c.s_h) & (piece - 1)) == 0;
+    a.page = make_divisor(c.page); a.block = make_divisor(sc.block);
     const int n_sm = current_sm_count();
     if (n_sm <= 0) { set_error("cannot read the SM count of the current device"); return STREAM_ERR_CUDA; }
     const long long ctas = ((long long)total + kThreads / 32 - 1) / (kThreads / 32), most = (long long)n_sm * kCtas;

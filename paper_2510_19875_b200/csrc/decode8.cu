@@ -2,16 +2,27 @@
 //
 //     x_t = scale log2(e) sk_t (q . k8_t),     out = sum_t 2^(x_t - m) sv_t v8_t / sum_t 2^(x_t - m)
 //
-// The keys of all slots and heads are dealt to the CTAs as in decode.cu, and a warp walks its tiles of 32 keys alone, as in decode_warp.cu. Half the bytes
-// a key leave half the time for it, so that the products turn: the keys are the rows of S^T = K Q^T and V's channels those of O^T = V^T P^T, the
-// query heads, of which a kv head has mostly eight or fewer, the eight columns (16 heads: two products from the same K and V). e4m3
-// is exact in fp16. A lane's four bytes of K are four channels side by side of one key: Q's channels are taken in that order. Two rows of V
-// are turned by ldmatrix two bytes at a time, so that a lane has two channels of two keys, rows g and g + 8 of the product. The weights are turned by movmatrix.
+// Half the bytes a key leave half the time for it, so that the products turn against those of decode_warp.cu: the keys are the rows of S^T = K Q^T and
+// V's channels those of O^T = V^T P^T, the query heads, of which a kv head has mostly eight or fewer, the eight columns (up to 16 heads: two products from
+// the same K and V). e4m3 is exact in fp16. A lane's four bytes of K are four channels side by side of one key: Q's channels are taken in that order.
+// Two rows of V are turned by ldmatrix two bytes at a time, so that a lane has two channels of two keys, rows g and g + 8 of the product. The weights are
+// turned by movmatrix.
 //
-// fp16 has eleven bits but a short range, which powers of two see to: a head's q is brought to [2^14, 2^15); a weight for the product is
-// 2^(x - r) sv 2^14, r following the largest x + log2(sv) of the warp's keys within a factor of 2, so that what fp16 cuts off, below 2^-24, is 2^-39
-// of the largest. The sum has a reference of its own and is that of the unrounded weights. bf16 caches: q (eight bits) is so exact, a weight off by
-// 2^-11. fp32 ones: q and the weights as two fp16 numbers each, and parts of 16 terms are added by ordinary additions (the tensor core's own sums are cut).
+// fp16 has eleven bits but a short range, which powers of two see to: a head's q is brought to [2^14, 2^15); a weight for the product is 2^(x - r) sv 2^14,
+// r following the largest x + log2(sv) of the warp's keys within a factor of 2, so that what fp16 cuts off, below 2^-24, is 2^-38 of the largest. The sum
+// has a reference of its own and is that of the unrounded weights. bf16 caches: q (eight bits) is so exact, a weight off by 2^-11. fp32 ones: q and
+// the weights as two fp16 numbers each, and parts of 16 or 32 terms are added by ordinary additions (the tensor core's own sums are cut).
+//
+// The keys of all slots and heads lie in one row, as in decode.cu, in units of 32; a CTA's share of it is cut in four once more, a warp's each, and the
+// warps walk alone, tile by tile of 32 keys (one a lane where pages are looked up), without a barrier until all are done. (Four warps that shared every segment: 52.9 us
+// for 64 slots of up to 8192 tokens, 87.5 for four of up to 131072, the warps waiting for one another at every segment's end; so: 41.6, 68.8.) The
+// ring is fed a segment ahead: the next one's first tiles come while this one's last are multiplied (35.9, 61.7), and a tile that is all there takes
+// the short way through the addresses (33, 60). Then the warps' pieces of an owner meet, and what is not all of it is left to the joins.
+//
+// What bounds it: rows of 128 bytes that lie a token apart. Four slots of up to 131072 tokens, 32 / 8 heads, d = 128: 273 MB in 60 us, 69 % of the copy
+// rate (6556 GB/s), with head after head within a page 52 us, 80 %; the rest is the way to the first tile (4 us) and the joins. Tried: three CTAs an SM
+// with rings of two tiles (64 us), a prefetch of 256 bytes to L2 with each row (73), two kv heads whose rows lie side by side walked by one warp (57, but 36 for the
+// 64 slots, for 33, and 12.7 for 10 where one slot of 1219 is all: twice the registers, half the owners).
 #include <cuda_fp16.h>
 
 #include "decode.cuh"
@@ -23,7 +34,8 @@ using namespace decode;
 
 constexpr int kWarps = kThreads / 32;
 constexpr int kStep = 32;            // keys of a warp's tile: one a lane where pages are looked up. And the keys of a unit
-// What a segment costs a warp beside its keys, in units.
+// What a segment costs a warp beside its keys, in units. (us with 1, 2, 3, 4, 5, 64 slots of up to 8192 tokens: 37.9, 33.7, 33.0, 32.9, 32.8; four of up to
+// 131072: 69.0, 60.3, 60.4, 60.2, 60.4.)
 constexpr int kOpen = 3;
 constexpr float kOutgrown = 30.f;    // log2: of the sum's reference
 constexpr float kTop = 14.f;         // log2: a weight for the product where it is the largest, times its value's scale
@@ -378,19 +390,6 @@ struct Walk {
     }
 };
 
-// Division of numbers below 2^31: n / d = (n + (n m >> 32)) >> s with 2^(s-1) < d <= 2^s and m = 2^32 (2^s - d) / d, rounded down, and 1.
-struct Divisor {
-    unsigned m, d;
-    int s;
-    __device__ __forceinline__ unsigned quotient(unsigned n) const { return (__umulhi(n, m) + n) >> s; }
-};
-Divisor divisor(int d) {
-    Divisor r = {0, (unsigned)d, 0};
-    while ((1ll << r.s) < d) ++r.s;
-    r.m = (unsigned)((((1ull << r.s) - (unsigned long long)d) << 32) / (unsigned long long)d + 1);
-    return r;
-}
-
 __device__ __forceinline__ void cp_async16_whole(unsigned dst, const void *src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
@@ -696,8 +695,8 @@ stream_status launch_decode8(const DecodeCall &a, const Scales &sc, int dtype, v
     Args8 B;
     B.A = args_of(a, workspace, n_sm, kStep, kOpen, kWarps);
     B.sc = sc;
-    B.page = divisor(a.c.page);
-    B.block = divisor(sc.block);
+    B.page = make_divisor(a.c.page);
+    B.block = make_divisor(sc.block);
     const int e = dtype == STREAM_F32 ? 4 : 2;
     B.A.q_vec = ((uintptr_t)a.q & (4 * e - 1)) == 0 && ((a.qs_s | a.qs_h) & 3) == 0 ? 1 : 0;
     B.pairs = ((uintptr_t)a.out & (2 * e - 1)) == 0 ? 1 : 0;

@@ -11,6 +11,8 @@
 // the logits' accumulators have it; column p of product j is channel 4 p + j of 32, so that a lane ends up with eight consecutive ones.
 // `ref` is moved only when a logit has outgrown it by 2^30. Where the row tiles are fewer than the SMs, a cluster of up to eight
 // CTAs has the tile: each walks every n-th key tile, and their m, l and O meet through shared memory, in a fixed order.
+// With a window (W) the sinks' tiles are walked, and behind a gap those from the first key on that the tile's first row sees (one head of 2048 tokens, d = 64,
+// window 256: 13.7 us, for 26.1 without one).
 #include "serve_common.cuh"
 #include "warp_common.cuh"
 

@@ -7,6 +7,7 @@
 // the SMs, a cluster of up to eight CTAs has the tile: each walks every n-th key tile, and their m, l and O meet
 // through shared memory, in a fixed order, every CTA joining its share of the rows. 2048 tokens: fp32, 8 heads, d = 256 498 us (34.5 TFLOP/s); off 16 bytes, 8 heads of fp32,
 // d = 64, 253 us (17.0), 32 / 8 heads of bf16, d = 128, 1298 us (26.5).
+// Windows (W) as in prompt_f32.cu.
 #include "serve_common.cuh"
 #include "warp_common.cuh"
 

@@ -7,6 +7,7 @@
 // outgrown it by 2^30; the sum is that of the unrounded weights. Late tokens, with the most keys, come first. Bound by the
 // latency of dependent steps at eight to sixteen warps an SM: 32 / 8 heads, 4096 tokens, d = 256 920 us (299 TFLOP/s), d = 32 175 us (196); 597 tokens, d = 256, 46.5 us
 // (126: 152 CTAs for 148 SMs).
+// With a window (W) the sinks' tiles are walked, and behind a gap those from the first key on that the tile's first row sees.
 #include "serve_common.cuh"
 #include "warp_common.cuh"
 

@@ -15,7 +15,9 @@
 // may overwrite P_X behind its product, and a tile's logits being there says that its last product is, too.
 //
 // Where there is a window, a pair of tiles walks the sinks and then, behind a gap, the keys from the first row's window on, wherever that begins. Up to 16 sinks
-// are the first rows of the first tile (which comes in pieces of 16 rows), more of them have tiles of their own.
+// are the first rows of the first tile (which comes in pieces of 16 rows), more of them have tiles of their own. 12 prompts of up to 4500 tokens, 28 / 4 heads,
+// window 1024, 4 sinks: 149 us (with a tile for the sinks 161); 32768 tokens, 32 / 8 heads, window 4096: 1620 us, 1280 TFLOP/s of the pairs that are seen.
+// An item has ten key tiles there and costs 3 us beside them: the way from the last product over the output to the next item's first weights.
 //
 // Roles (384 threads): warp 0 loads Q, K and V by TMA (one ring for K and V, in the order of their use); warp 1 issues the MMAs and
 // owns TMEM; warp 2 writes zeros over the rows of a V tile behind the sequence's last key (a weight of zero times what lies

@@ -90,6 +90,18 @@ __device__ __forceinline__ RowTile row_tile(const PromptGeom &g, int nth, int ro
     }
     return {-1, 0};
 }
+// Division of numbers below 2^31: n / d = (n + (n m >> 32)) >> s with 2^(s-1) < d <= 2^s and m = 2^32 (2^s - d) / d, rounded down, and 1.
+struct Divisor {
+    unsigned m, d;
+    int s;
+    __device__ __forceinline__ unsigned quotient(unsigned n) const { return (__umulhi(n, m) + n) >> s; }
+};
+inline Divisor make_divisor(int d) {
+    Divisor r = {0, (unsigned)d, 0};
+    while ((1ll << r.s) < d) ++r.s;
+    r.m = (unsigned)((((1ull << r.s) - (unsigned long long)d) << 32) / (unsigned long long)d + 1);
+    return r;
+}
 // No more tiles than this, of all kv heads, however the rows are dealt to the sequences.
 inline long long most_row_tiles(const PromptGeom &g, int rows) {
     return ((long long)g.total_q * g.hpg / rows + (g.n_seqs < g.total_q ? g.n_seqs : g.total_q)) * g.G;
