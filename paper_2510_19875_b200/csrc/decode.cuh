@@ -48,7 +48,7 @@ cudaError_t launch_joins(const Args &A, int dtype, cudaStream_t st);
 bool warp_supported(const DecodeCall &a, int dtype);
 cudaError_t launch_warp(Args &A, int dtype, int n_sm, cudaStream_t st);
 
-// Which keys of a slot are walked where there is a window (W; 64 slots of up to 8192 tokens, window 1024, 32 / 8 heads, bf16: 30 to 36 us, 101 MB; a
+// Which keys of a slot are walked where there is a window (W; 64 slots of up to 8192 tokens, window 1024, 32 / 8 heads, bf16: 30 to 36 us, 106 MB; a
 // segment's own cost, which is 3 us, is what bounds it): the units of the sinks, then, behind a gap, those from the window's first key on. A
 // segment counts its keys without the gap; units are whole on both sides of it, so that a tile's keys lie as they do without.
 struct Seen {
