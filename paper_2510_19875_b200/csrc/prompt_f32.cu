@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_f32_kernel(const __grid_co
         return g.causal ? min(sk.n, max(0, token_of(min(r, n_rows - 1)) + sk.n - sq.n + 1)) : sk.n;
     };
     Walked wk = {};
-    if constexpr (W) wk = walked_keys(g, kKeys, tok_base + sk.n - sq.n, sk.n);
+    if constexpr (W) wk = walked_keys(g, kKeys, tok_base + (sk.n - sq.n), sk.n);
     const int most = keys_of(n_rows - 1), walked = most - wk.gap, warp_most = keys_of(warp * 16 + 15), warp_least = keys_of(warp * 16);
     const int see[2] = {keys_of(warp * 16 + quad), keys_of(warp * 16 + quad + 8)};
     const float *const ks = k + (long long)sk.first * g.ks_t + (long long)kvh * g.ks_h;
@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_f32_kernel(const __grid_co
     int low[2] = {0, 0};  // the first keys of their windows
     if constexpr (W) {
 #pragma unroll
-        for (int r = 0; r < 2; ++r) low[r] = window_begin(g, token_of(min(warp * 16 + quad + 8 * r, n_rows - 1)) + sk.n - sq.n);
+        for (int r = 0; r < 2; ++r) low[r] = window_begin(g, token_of(min(warp * 16 + quad + 8 * r, n_rows - 1)) + (sk.n - sq.n));
     }
     for (int jw = first, buf = 0; jw < walked; jw += stride, buf ^= 1) {
         const int j = W ? wk.key(jw) : jw;

@@ -50,7 +50,7 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas) prompt_mma_kernel(co
         return min(sk.n, max(0, tok + sk.n - sq.n + 1));
     };
     Walked wk = {};
-    if constexpr (W) wk = walked_keys(g, kKeys, (int)(row_base / g.hpg) + sk.n - sq.n, sk.n);
+    if constexpr (W) wk = walked_keys(g, kKeys, (int)(row_base / g.hpg) + (sk.n - sq.n), sk.n);
     const int most = keys_of(n_rows - 1), walked = most - wk.gap, warp_most = keys_of(warp * 16 + 15);
     const __nv_bfloat16 *const qs = q + (long long)sq.first * g.qs_t + (long long)kvh * g.hpg * g.qs_h;
     const __nv_bfloat16 *const ks = k + (long long)sk.first * g.ks_t + (long long)kvh * g.ks_h;
@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas) prompt_mma_kernel(co
     int low[2] = {0, 0};  // the first keys of their windows
     if constexpr (W) {
 #pragma unroll
-        for (int r = 0; r < 2; ++r) low[r] = window_begin(g, (int)((row_base + min(warp * 16 + quad + 8 * r, n_rows - 1)) / g.hpg) + sk.n - sq.n);
+        for (int r = 0; r < 2; ++r) low[r] = window_begin(g, (int)((row_base + min(warp * 16 + quad + 8 * r, n_rows - 1)) / g.hpg) + (sk.n - sq.n));
     }
     for (int jw = 0, buf = 0; jw < walked; jw += kKeys, buf ^= 1) {
         const int j = W ? wk.key(jw) : jw;

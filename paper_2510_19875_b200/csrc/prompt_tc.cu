@@ -136,7 +136,7 @@ __device__ __forceinline__ Item item_at(const Params &P, const Tail<F> *tl, int 
     const int pairs = ceil_div(it.s.q_n, 2 * P.per_tile);
     it.tok0 = (pairs - 1 - level) * 2 * P.per_tile;  // late tokens, with the most keys, first
     it.most = 0;
-    it.wk = W ? walked_keys(g, P.sink_unit, it.tok0 + it.s.k_n - it.s.q_n, it.s.k_n) : Walked{0, 0};
+    it.wk = W ? walked_keys(g, P.sink_unit, it.tok0 + (it.s.k_n - it.s.q_n), it.s.k_n) : Walked{0, 0};
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
         const int t0 = it.tok0 + x * P.per_tile;
@@ -379,7 +379,7 @@ __device__ void softmax_role(const Params &P, Tail<F> *tl, unsigned tmem, int t)
         // rows that are none see what the last one does, so that they cost nothing
         const int last = min(tok, min(tok0 + P.per_tile, it.s.q_n) - 1);
         const int keys = g.causal ? min(it.s.k_n, max(0, last + 1 + it.s.k_n - it.s.q_n)) : it.s.k_n;
-        const int low = W ? window_begin(g, last + it.s.k_n - it.s.q_n) : 0;
+        const int low = W ? window_begin(g, last + (it.s.k_n - it.s.q_n)) : 0;
         const bool mine = tok_r < P.per_tile && tok < it.s.q_n;
         float ref = -CUDART_INF_F, l = 0.f;
         for (int j = 0; j < n_tiles; ++j) {
