@@ -44,25 +44,27 @@ def check8(got, lse, q, k, v, v_scale, scale, dtype, what=""):
     H, d = q.shape
     m, G = k.shape[:2]
     scale = 1 / math.sqrt(d) if scale is None else scale
-    for h in range(H):
-        a, b, w, z = q[h].double(), k[:, h * G // H].double(), v[:, h * G // H].double(), v_scale[:, h * G // H].double()
-        if m == 0:
-            assert (got[h] == 0).all() and lse[h] == -math.inf, what
-            continue
-        s = b @ a * scale
-        ls = torch.logsumexp(s, 0)
-        p = torch.exp(s - ls)
-        out, mag = p @ w, p @ w.abs()
-        top = (b.abs() @ a.abs()).amax() * scale
-        bf16 = dtype is torch.bfloat16
-        logit = (d + 2) * U * top + scale * a.abs().amax() * b.abs().sum(1).amax() * 2.0 ** -39 + (0 if bf16 else 2.0 ** -22 * top)
-        weight = 2 * (logit + 2 ** -22 + 8 * U * top) + 2 * (m + 2) * U
-        each = weight * (1 + 2.0 ** -6) + (2.0 ** -11 if bf16 else 2.0 ** -22)
-        bound = (2.0 ** -8 if bf16 else U) * out.abs() + mag * each * (1 + 2.0 ** -6) + m * 2.0 ** -38 * 448 * (p * z).amax() + 1e-30
-        off = (got[h].double() - out).abs()
-        assert torch.isfinite(got[h].float()).all(), what
-        assert (off <= bound).all(), (what, h, float((off / bound).max()))
-        assert (lse[h].double() - ls).abs() <= logit + weight + 4 * U * ls.abs() + 2 ** -21, (what, h, float(lse[h]), float(ls))
+    if m == 0:
+        assert (got == 0).all() and (lse == -math.inf).all(), what
+        return
+    a = q.double()
+    b, w, z = (x.double().repeat_interleave(H // G, 1) for x in (k, v, v_scale))  # of each query head
+    s = torch.einsum("hd,mhd->hm", a, b) * scale
+    ls = torch.logsumexp(s, 1)
+    p = torch.exp(s - ls[:, None])
+    out, mag = torch.einsum("hm,mhd->hd", p, w), torch.einsum("hm,mhd->hd", p, w.abs())
+    top = torch.einsum("hd,mhd->hm", a.abs(), b.abs()).amax(1) * scale
+    bf16 = dtype is torch.bfloat16
+    logit = (d + 2) * U * top + scale * a.abs().amax(1) * b.abs().sum(2).amax(0) * 2.0 ** -39 + (0 if bf16 else 2.0 ** -22 * top)
+    weight = 2 * (logit + 2 ** -22 + 8 * U * top) + 2 * (m + 2) * U
+    each = weight * (1 + 2.0 ** -6) + (2.0 ** -11 if bf16 else 2.0 ** -22)
+    cut = m * 2.0 ** -38 * 448 * (p * z.T).amax(1)
+    bound = (2.0 ** -8 if bf16 else U) * out.abs() + mag * each[:, None] * (1 + 2.0 ** -6) + cut[:, None] + 1e-30
+    off = (got.double() - out).abs()
+    assert torch.isfinite(got.float()).all(), what
+    assert (off <= bound).all(), (what, float((off / bound).max()))
+    far = (lse.double() - ls).abs()
+    assert (far <= logit + weight + 4 * U * ls.abs() + 2 ** -21).all(), (what, float(far.max()))
 
 
 def scale_of(top):

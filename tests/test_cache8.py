@@ -319,6 +319,25 @@ def test_decode_again_on_streams_and_in_a_graph(S, d, dtype):
             assert torch.equal(o, e) and torch.equal(x, f)
 
 
+@pytest.mark.parametrize("d,dtype", [(128, BF16), (64, F32), (16, BF16)])
+def test_outputs_that_lie_off_their_boundaries_and_very_long_windows(S, d, dtype):
+    """Contiguous outputs one element behind a boundary; windows beyond 32 bits."""
+    lens = [70, 0, 600]
+    cache, held, _ = filled_cache8(S, lens, 16, 16, 2, d, dtype)
+    q = torch.randn(3, 4, d, device="cuda").to(dtype)
+    a, la = decode_checked(S, q, cache, held)
+    odd = torch.zeros(q.numel() + 1, dtype=dtype, device="cuda")[1:].view(q.shape)
+    lse = torch.zeros(3 * 4 + 1, device="cuda")[1:].view(3, 4)
+    assert S.decode_attention(q, cache, out=odd, lse_out=lse)[0] is odd and torch.equal(odd, a) and torch.equal(lse, la)
+    b, lb = S.decode_attention(q, cache, window=2 ** 40, sinks=2 ** 40, want_lse=True)
+    assert torch.equal(a, b) and torch.equal(la, lb)
+    cu = ints(offsets(lens))
+    k, v = S.cache_read(cache, cu, 670)
+    out = [torch.zeros(k.numel() + 1, dtype=dtype, device="cuda")[1:].view(k.shape) for _ in range(2)]
+    S.cache_read(cache, cu, 670, out=out)
+    assert torch.equal(out[0], k) and torch.equal(out[1], v)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_offsets_beyond_32_bits(S, dtype):
     """Pages further apart than 2^31 elements in all."""
