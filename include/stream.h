@@ -597,7 +597,8 @@ stream_status stream_cache8_copy_pages(const stream_cache8 *c, void *k_pages, vo
 
 /*
  * stream_decode_attention over a cache in 8 bits, with a window and sinks where window > 0 (stream_decode_window_attention; 0: every key is
- * seen, whatever sinks says). Any scales of 2^-100 to 2^100 will do, powers of two or not; a token whose key scale is 0 counts as not there. Products are those of
+ * seen, whatever sinks says). Any scales of 2^-100 to 2^100 will do, powers of two or not; a token whose key scale is 0 counts as not there,
+ * whatever its bytes and its value's scale are. Products are those of
  * e4m3 numbers, which fp16 holds, with queries and weights in fp16 (bf16 caches: 2^-11 of a weight; fp32 ones: two fp16 numbers each, 2^-22). Everything
  * else, the workspace too (stream_decode_workspace_bytes of &c->cache), as stream_decode_attention.
  */

@@ -40,6 +40,7 @@ constexpr int kOpen = 3;
 constexpr float kOutgrown = 30.f;    // log2: of the sum's reference
 constexpr float kTop = 14.f;         // log2: a weight for the product where it is the largest, times its value's scale
 constexpr float kNone = -3e38f;      // a reference before the first key, finite so that it has differences
+constexpr float kAbsent = -1.f;      // in the place of the value's scale where a tile has no token; the key's is 0
 constexpr float kLeastScale = 7.8886090522101181e-31f;  // 2^-100: of values (a smaller one, 0 too, counts as this)
 
 template <class T, int D, int N>
@@ -114,8 +115,8 @@ __device__ __forceinline__ float log2_of(float x) {
     asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
-__device__ __forceinline__ void cp_async4_or_zero(unsigned dst, const void *src, int bytes) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+__device__ __forceinline__ void cp_async4(unsigned dst, const void *src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
 
 // Four channels of a query head, as they lie in memory.
@@ -202,9 +203,10 @@ struct Walk {
         }
     }
 
-    // The tile at shared-memory address kt: K, V behind it, and the keys' scales at z. Keys g, g + 8, g + 16 and g + 24 of it are this lane's.
-    __device__ __forceinline__ void step(const Smem<T, D, N> &sm, int warp, unsigned kt, const float *z, int lane) {
-        const unsigned vt = kt + F::kTile;
+    // A tile: K, V behind it, then the keys' scales and the values'. Keys g, g + 8, g + 16 and g + 24 of it are this lane's.
+    __device__ __forceinline__ void step(const Smem<T, D, N> &sm, int warp, unsigned char *tile, int lane) {
+        const unsigned kt = wp::smem_addr(tile), vt = kt + F::kTile;
+        const float *const z = reinterpret_cast<const float *>(tile + 2 * F::kTile);
         float s[N][2][4];
 #pragma unroll
         for (int n = 0; n < N; ++n)
@@ -251,6 +253,7 @@ struct Walk {
             sv[k] = fmaxf(z[kStep + (lane >> 2) + 8 * k], kLeastScale);
             lv[k] = log2_of(sv[k]);
         }
+        const bool lacks = sk[0] == 0.f || sk[1] == 0.f || sk[2] == 0.f || sk[3] == 0.f;  // keys that are not there
         bool outgrown = false;
 #pragma unroll
         for (int n = 0; n < N; ++n)
@@ -258,15 +261,37 @@ struct Walk {
             for (int y = 0; y < 2; ++y) {
                 float a = -CUDART_INF_F, b = -CUDART_INF_F;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {  // (a tile that is not there is zeros)
+                for (int k = 0; k < 4; ++k) {
                     float &x = s[n][k >> 1][2 * (k & 1) + y];
-                    x = fmaf(x, unit[n][y] * sk[k], sk[k] != 0.f ? 0.f : -CUDART_INF_F);
+                    x *= unit[n][y] * sk[k];
                     a = fmaxf(a, x);
                     b = fmaxf(b, x + lv[k]);
                 }
                 outgrown = outgrown || a > ref[n][y] + kOutgrown || b > top[n][y] + (kTop + 1.f);
             }
-        if (__any_sync(0xffffffffu, outgrown)) {
+        bool moves = __any_sync(0xffffffffu, lacks || outgrown);
+        if (moves) {
+            moves = __any_sync(0xffffffffu, outgrown);
+            // what is not there, whatever its bytes and its value's scale are (NaN times a weight of zero would be NaN)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (sk[k] == 0.f) {
+                    sv[k] = 1.f;
+                    lv[k] = 0.f;
+#pragma unroll
+                    for (int n = 0; n < N; ++n) s[n][k >> 1][2 * (k & 1)] = s[n][k >> 1][2 * (k & 1) + 1] = -CUDART_INF_F;
+                }
+            const unsigned unset = __ballot_sync(0xffffffffu, z[lane] == 0.f && z[kStep + lane] != kAbsent);
+            if (unset != 0) {
+#pragma unroll
+                for (int i = 0; i < F::kPieces; ++i) {
+                    const int at = (i * 32 + lane) * 16;
+                    if ((unset >> (at / D)) & 1u) *reinterpret_cast<uint4 *>(tile + F::kTile + at) = make_uint4(0, 0, 0, 0);
+                }
+                __syncwarp();
+            }
+        }
+        if (moves) {
 #pragma unroll
             for (int n = 0; n < N; ++n)
 #pragma unroll
@@ -477,8 +502,14 @@ __global__ void __launch_bounds__(kThreads, Form<T, D, N>::kCtas) decode8_kernel
         const long long own = own_page >= 0 ? (long long)own_page * c.s_p + (long long)own_row * c.s_t : 0;
         const long long z = mine ? (long long)own_page * B.sc.s_p + (long long)B.block.quotient((unsigned)own_row) * B.sc.s_b + src.kvh * B.sc.s_h : 0;
         const unsigned to = ring + put * F::kPlace;
-        cp_async4_or_zero(to + 2 * F::kTile + lane * 4, B.sc.k + z, mine ? 4 : 0);
-        cp_async4_or_zero(to + 2 * F::kTile + kStep * 4 + lane * 4, B.sc.v + z, mine ? 4 : 0);
+        if (mine) {
+            cp_async4(to + 2 * F::kTile + lane * 4, B.sc.k + z);
+            cp_async4(to + 2 * F::kTile + kStep * 4 + lane * 4, B.sc.v + z);
+        } else {
+            float *const scales = reinterpret_cast<float *>(ring_ptr + put * F::kPlace + 2 * F::kTile);
+            scales[lane] = 0.f;
+            scales[kStep + lane] = kAbsent;
+        }
         const long long head = src.kvh * c.s_h + piece_l * 16;
         if (plain && there == 0xffffffffu) {
 #pragma unroll
@@ -579,8 +610,7 @@ __global__ void __launch_bounds__(kThreads, Form<T, D, N>::kCtas) decode8_kernel
             }
             wait_for<F::kStages - 1>(ahead - 1);  // copies that may still be on their way: those of later tiles
             __syncwarp();
-            const unsigned place = take * F::kPlace;
-            walk.step(sm, warp, ring + place, reinterpret_cast<const float *>(ring_ptr + place + 2 * F::kTile), lane);
+            walk.step(sm, warp, ring_ptr + take * F::kPlace, lane);
             __syncwarp();  // (the tile is read before its place is filled again)
             take = take + 1 == F::kStages ? 0 : take + 1;
             --ahead;
