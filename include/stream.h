@@ -579,7 +579,8 @@ typedef struct {
  * stream_cache_write for a cache in 8 bits. A block whose first token is among the new ones gets a scale for its new tokens. One that
  * has tokens in front of them keeps its scale or takes the one that the new tokens ask for, whichever is larger; where it grows, those
  * tokens are rounded again: rn(x old / new). The sum of a block's roundings is so at most a step of its last scale. Infinities become +-448
- * scales, with e = 120; NaN stays NaN and asks for no scale. Everything else as stream_cache_write.
+ * scales, with e = 120, and as that is more than fp32 holds they are read as infinities (what is rounded to 2^128 too); NaN stays NaN and
+ * asks for no scale. Everything else as stream_cache_write.
  *   k_scale, v_scale  the scales' first elements (layer 0); written: layer `layer`
  */
 stream_status stream_cache8_write(const stream_cache8 *c, int32_t layer, const void *k, const void *v, int64_t total, int64_t stride_t,
@@ -597,8 +598,8 @@ stream_status stream_cache8_copy_pages(const stream_cache8 *c, void *k_pages, vo
 
 /*
  * stream_decode_attention over a cache in 8 bits, with a window and sinks where window > 0 (stream_decode_window_attention; 0: every key is
- * seen, whatever sinks says). Any scales of 2^-100 to 2^100 will do, powers of two or not; a token whose key scale is 0 counts as not there,
- * whatever its bytes and its value's scale are. Products are those of
+ * seen, whatever sinks says). Any scales of 0 to 2^120 for keys (with logits that fp32 holds) and of 0 to 2^100 for values (of which those up
+ * to 2^64 cannot overflow) will do, powers of two or not; a token whose key scale is 0 counts as not there, whatever its bytes and its value's scale are. Products are those of
  * e4m3 numbers, which fp16 holds, with queries and weights in fp16 (bf16 caches: 2^-11 of a weight; fp32 ones: two fp16 numbers each, 2^-22). Everything
  * else, the workspace too (stream_decode_workspace_bytes of &c->cache), as stream_decode_attention.
  */

@@ -41,7 +41,7 @@ constexpr float kOutgrown = 30.f;    // log2: of the sum's reference
 constexpr float kTop = 14.f;         // log2: a weight for the product where it is the largest, times its value's scale
 constexpr float kNone = -3e38f;      // a reference before the first key, finite so that it has differences
 constexpr float kAbsent = -1.f;      // in the place of the value's scale where a tile has no token; the key's is 0
-constexpr float kLeastScale = 7.8886090522101181e-31f;  // 2^-100: of values (a smaller one, 0 too, counts as this)
+constexpr float kLeastScale = 7.8886090522101181e-31f;  // 2^-100: of a value's scale, for the reference (a smaller one, 0 or NaN counts as this there)
 
 template <class T, int D, int N>
 struct Form {
@@ -250,8 +250,8 @@ struct Walk {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             sk[k] = z[(lane >> 2) + 8 * k];
-            sv[k] = fmaxf(z[kStep + (lane >> 2) + 8 * k], kLeastScale);
-            lv[k] = log2_of(sv[k]);
+            sv[k] = z[kStep + (lane >> 2) + 8 * k];
+            lv[k] = log2_of(fmaxf(sv[k], kLeastScale));
         }
         const bool lacks = sk[0] == 0.f || sk[1] == 0.f || sk[2] == 0.f || sk[3] == 0.f;  // keys that are not there
         bool outgrown = false;
