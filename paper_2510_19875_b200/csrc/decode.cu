@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(Args A, int vec) {
         }
         if (tid < nh) {
             if (!sg.whole) { part[tid] = sm.m[tid]; part[kMaxHeads + tid] = sm.l[tid]; }
-            else if (A.a.lse != nullptr) A.a.lse[(long long)s * A.a.H + h0 + tid] = sm.l[tid] > 0.f ? (sm.m[tid] + log2f(sm.l[tid])) * kLn2 : -CUDART_INF_F;
+            else if (A.a.lse != nullptr) A.a.lse[(long long)s * A.a.H + h0 + tid] = lse_of(sm.m[tid], sm.l[tid]);
         }
     }
     leave_to_joins(A, left, bad);
@@ -312,7 +312,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     const long long to = left.to + h;
     T *const out = (T *)A.a.out + to * d + at;
     out[0] = (T)(o.x * inv); out[1] = (T)(o.y * inv); out[2] = (T)(o.z * inv); out[3] = (T)(o.w * inv);
-    if (A.a.lse != nullptr && tid == 0) A.a.lse[to] = l > 0.f ? (m + log2f(l)) * kLn2 : -CUDART_INF_F;
+    if (A.a.lse != nullptr && tid == 0) A.a.lse[to] = lse_of(m, l);
 }
 
 template <class T, int D, bool W>

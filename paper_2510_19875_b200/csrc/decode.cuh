@@ -183,6 +183,9 @@ __device__ __forceinline__ void leave_to_joins(const Args &A, Left left, unsigne
     if (threadIdx.x == 0) A.left[blockIdx.x] = left;
 }
 
+// The logarithm of a softmax sum l, of weights relative to 2^m; NaN where a logit is.
+__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -CUDART_INF_F : (m + log2f(l)) * kLn2; }
+
 __device__ __forceinline__ float warp_maximum(float x) {
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));

@@ -410,7 +410,7 @@ struct Walk {
                         *reinterpret_cast<__nv_bfloat162 *>(to + 16 * c) = __floats2bfloat162_rn(a, b);
                     }
                 }
-                if (g == 0 && A.a.lse != nullptr) A.a.lse[row + h] = l[n][y] > 0.f ? (ref[n][y] + log2f(l[n][y])) * kLn2 : -CUDART_INF_F;
+                if (g == 0 && A.a.lse != nullptr) A.a.lse[row + h] = lse_of(ref[n][y], l[n][y]);
             }
     }
 };
@@ -679,7 +679,7 @@ __global__ void __launch_bounds__(kThreads, Form<T, D, N>::kCtas) decode8_kernel
                 const float inv = sum > 0.f ? 1.f / sum : 0.f;
                 T *const to = out + (to_row + h) * D + x;
                 to[0] = (T)(y.x * inv); to[1] = (T)(y.y * inv); to[2] = (T)(y.z * inv); to[3] = (T)(y.w * inv);
-                if (x == 0 && A.a.lse != nullptr) A.a.lse[to_row + h] = sum > 0.f ? (m + log2f(sum)) * kLn2 : -CUDART_INF_F;
+                if (x == 0 && A.a.lse != nullptr) A.a.lse[to_row + h] = lse_of(m, sum);
             } else {
                 *reinterpret_cast<float4 *>(part + 2 * kMaxHeads + h * D + x) = y;
                 if (x == 0) { part[h] = m; part[kMaxHeads + h] = sum; }

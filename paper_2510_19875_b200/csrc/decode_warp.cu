@@ -410,7 +410,7 @@ __global__ void __launch_bounds__(kThreads, Form<T, D>::kCtas) decode_warp_kerne
                 const float inv = sum > 0.f ? 1.f / sum : 0.f;
                 T *const to = out + ((long long)s * A.a.H + sg.h0 + h) * D + x;
                 to[0] = (T)(y.x * inv); to[1] = (T)(y.y * inv); to[2] = (T)(y.z * inv); to[3] = (T)(y.w * inv);
-                if (x == 0 && A.a.lse != nullptr) A.a.lse[(long long)s * A.a.H + sg.h0 + h] = sum > 0.f ? (m + log2f(sum)) * kLn2 : -CUDART_INF_F;
+                if (x == 0 && A.a.lse != nullptr) A.a.lse[(long long)s * A.a.H + sg.h0 + h] = lse_of(m, sum);
             } else {
                 *reinterpret_cast<float4 *>(part + 2 * kMaxHeads + h * D + x) = y;
                 if (x == 0) { part[h] = m; part[kMaxHeads + h] = sum; }
