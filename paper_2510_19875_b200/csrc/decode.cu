@@ -357,7 +357,6 @@ Args args_of(const DecodeCall &a, void *workspace, int n_sm, int unit, int open,
     A.header = (WorkspaceHeader *)workspace;
     A.left = (Left *)((char *)workspace + sizeof(WorkspaceHeader));
     A.parts = (float *)((char *)A.left + kLeftBytes);
-    A.warp_parts = A.parts + (size_t)kMaxGrid * 2 * kMaxHeads * (a.c.d + 2);
     long long keys = (long long)a.c.max_pages * a.c.page;  // of a slot, at most
     if (a.window > 0) keys = std::min(keys, (long long)a.window + a.sinks + 2 * (unit - 1));
     const long long most = (long long)a.c.n_slots * A.per_slot * ((keys + unit - 1) / unit + open), ctas = (most + least - 1) / least;
@@ -374,7 +373,7 @@ cudaError_t launch_joins(const Args &A, int dtype, cudaStream_t st) {
 }  // namespace decode
 
 size_t decode_workspace_bytes(const CacheGeom &c) {
-    return sizeof(WorkspaceHeader) + kLeftBytes + (size_t)kMaxGrid * (2 + kThreads / 32) * kMaxHeads * (c.d + 2) * sizeof(float);
+    return sizeof(WorkspaceHeader) + kLeftBytes + (size_t)kMaxGrid * 2 * kMaxHeads * (c.d + 2) * sizeof(float);
 }
 
 stream_status launch_decode(const DecodeCall &a, int dtype, void *workspace, cudaStream_t st) {

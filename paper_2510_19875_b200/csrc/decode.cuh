@@ -34,7 +34,6 @@ struct Args {
     int per_slot;                // owners of a slot's units: (kv head, up to 16 of its query heads)
     int chunks;                  // owners of a kv head
     float *parts;                // [grid][2][kMaxHeads * (d + 2)]: m, l, O
-    float *warp_parts;           // (decode8.cu) [grid][warps][kMaxHeads * (d + 2)]
     struct Left *left;           // [grid]
     WorkspaceHeader *header;
     int q_vec;                   // q is read in pieces (decode_warp.cu: of 16 bytes; decode8.cu: of four elements)

@@ -57,8 +57,9 @@ struct Form {
     static constexpr int kCtas = D == 256 || (D == 128 && !kQInRegs) ? 1 : 2;  // of an SM
     static constexpr int kLeave = (2 * kMaxHeads + kHeads * D) * 4;    // bytes of a piece: m, l, O
     static_assert(kLeave <= kStages * kPlace, "a warp's last piece in its ring");
-    // the first pieces of the warps but the first in shared memory, where that is large enough, else in the workspace
-    static constexpr bool kFirstHere = kCtas * (kWarps * kStages * kPlace + (kWarps - 1) * kLeave + (kQInRegs ? 0 : kWarps * kParts * kPieces * N * 256) + 2048) <= 233472;
+    // the first pieces of the warps but the first beside the rings, where shared memory is large enough, else in a place of the warp's ring
+    static constexpr bool kFirstBeside = kCtas * (kWarps * kStages * kPlace + (kWarps - 1) * kLeave + (kQInRegs ? 0 : kWarps * kParts * kPieces * N * 256) + 2048) <= 233472;
+    static_assert(kFirstBeside || (kLeave <= kPlace && kStages > 1), "a warp's first piece in a place of its ring");
 };
 // A piece of an owner that a warp leaves to its CTA.
 struct Piece {
@@ -72,7 +73,7 @@ struct Smem {
     using F = Form<T, D, N>;
     unsigned char ring[kWarps][F::kStages * F::kPlace];
     uint2 q[kWarps][F::kQInRegs ? 1 : F::kParts * F::kPieces * N * 32];  // what a lane multiplies with
-    float first[F::kFirstHere ? kWarps - 1 : 1][F::kFirstHere ? F::kLeave / 4 : 1];
+    float first[F::kFirstBeside ? kWarps - 1 : 1][F::kFirstBeside ? F::kLeave / 4 : 1];
     Piece piece[2 * kWarps];
     int n_parts;   // that the first warp has left to the joins
 };
@@ -471,6 +472,12 @@ __global__ void __launch_bounds__(kThreads, Form<T, D, N>::kCtas) decode8_kernel
     int src_n = 0;                      // the step of it that is fetched next
     int page = -1, row = 0;             // lane i: the page of key i of that step, -1: none; and its row there
     unsigned put = 0, take = 0, ahead = 0;  // the ring's places that are filled next, and multiplied next; how many are filled
+    unsigned held = F::kStages;             // the place that has the warp's first piece, if one has
+    auto behind = [&](unsigned place) {
+        place = place + 1 == F::kStages ? 0 : place + 1;
+        if (!F::kFirstBeside && place == held) place = place + 1 == F::kStages ? 0 : place + 1;
+        return place;
+    };
     auto look_up = [&](const Source &f, int n, int &to, int &to_row) {
         const int walked = f.key0 + n * kStep + lane, key = W ? f.seen.key(walked) : walked;
         to = -1;
@@ -547,7 +554,7 @@ __global__ void __launch_bounds__(kThreads, Form<T, D, N>::kCtas) decode8_kernel
             }
         }
         wp::cp_async_commit();
-        put = put + 1 == F::kStages ? 0 : put + 1;
+        put = behind(put);
         ++ahead;
         ++src_n;
     };
@@ -573,14 +580,14 @@ __global__ void __launch_bounds__(kThreads, Form<T, D, N>::kCtas) decode8_kernel
         const Segment next = open_segment<W, kStep, kOpen>(A, sg.next, end, lane, pl);
         bool waits = next.next >= 0;  // it is not yet fetched from
         int next_page = -1, next_row = 0;
-        Source behind = {};
+        Source follows = {};
         if (waits) {
-            behind = source_of(next);
-            look_up(behind, 0, next_page, next_row);
+            follows = source_of(next);
+            look_up(follows, 0, next_page, next_row);
         }
         auto go_on = [&] {
             waits = false;
-            src = behind;
+            src = follows;
             src_n = 0;
             page = next_page;
             row = next_row;
@@ -596,7 +603,7 @@ __global__ void __launch_bounds__(kThreads, Form<T, D, N>::kCtas) decode8_kernel
         Walk<T, D, N> walk;
         const int n_steps = (sg.key_end - sg.key0 + kStep - 1) / kStep;
         for (int n = 0; n < n_steps; ++n) {
-            while (ahead < F::kStages) {
+            while (ahead < (F::kFirstBeside || held == F::kStages ? F::kStages : F::kStages - 1)) {
                 if (src_n == src.n_steps) {
                     if (!waits) break;
                     go_on();
@@ -612,7 +619,7 @@ __global__ void __launch_bounds__(kThreads, Form<T, D, N>::kCtas) decode8_kernel
             __syncwarp();
             walk.step(sm, warp, ring_ptr + take * F::kPlace, lane);
             __syncwarp();  // (the tile is read before its place is filled again)
-            take = take + 1 == F::kStages ? 0 : take + 1;
+            take = behind(take);
             --ahead;
         }
         if (waits) go_on();
@@ -623,12 +630,23 @@ __global__ void __launch_bounds__(kThreads, Form<T, D, N>::kCtas) decode8_kernel
             walk.write(A, to_row, sg.heads, B.pairs != 0, lane);
         } else {
             // The warp's first segment or its last one, which stays in the ring: that is done with. A first one that others follow ends its owner: the
-            // first warp's began in another CTA and is left to the joins as it is.
+            // first warp's began in another CTA and is left to the joins as it is. Where another one's has no room beside the rings it takes the
+            // place that is filled next, which is empty, and the others go round without it (a warp that has met an owner's end has a tile
+            // less ahead: bf16, d = 128 and fp32, d = 256 with more than eight heads).
             const bool last = next.next < 0;
-            float *const to = last        ? reinterpret_cast<float *>(ring_ptr)
-                              : warp == 0 ? part_of(A, (int)blockIdx.x, 0)
-                              : F::kFirstHere ? sm.first[F::kFirstHere ? warp - 1 : 0]
-                                              : A.warp_parts + ((long long)blockIdx.x * kWarps + warp) * kMaxHeads * (D + 2);
+            float *to;
+            if (last) {
+                to = reinterpret_cast<float *>(ring_ptr + (!F::kFirstBeside && held == 0 ? F::kPlace : 0));
+            } else if (warp == 0) {
+                to = part_of(A, (int)blockIdx.x, 0);
+            } else if constexpr (F::kFirstBeside) {
+                to = sm.first[warp - 1];
+            } else {
+                held = put;
+                to = reinterpret_cast<float *>(ring_ptr + held * F::kPlace);
+                put = behind(put);
+                if (take == held) take = put;
+            }
             walk.leave(to, lane);
             if (!last && warp == 0) {
                 if (lane == 0) sm.n_parts = 1;
