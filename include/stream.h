@@ -563,7 +563,7 @@ stream_status stream_decode_window_attention(const stream_cache *c, int32_t laye
 /*
  * A paged cache in 8 bits: K and V are e4m3 (sign, four bits of exponent, three of mantissa; up to 448), and the tokens of a block, in one kv
  * head, share a scale: a key is its e4m3 numbers times its block's scale. The scales of K and V are each float32 [n_layers, n_pages,
- * page_size / block, n_kv_heads] with the strides below. The ledger is that of any cache: its calls take &c->cache.
+ * page_size / block, n_kv_heads] with the strides below, which are positive. The ledger is that of any cache: its calls take &c->cache.
  *
  * A block's scale is the smallest power of two 2^e, -90 <= e <= 120, of which no element is more than 448 times: e4m3's relative precision, 2^-4 at most, does
  * not depend on a scale, powers of two make the division exact, and what is rounded again when a block's scale grows stays

@@ -17,7 +17,7 @@
 // Where there is a window, a pair of tiles walks the sinks and then, behind a gap, the keys from the first row's window on, wherever that begins. Up to 16 sinks
 // are the first rows of the first tile (which comes in pieces of 16 rows), more of them have tiles of their own. 12 prompts of up to 4500 tokens, 28 / 4 heads,
 // window 1024, 4 sinks: 149 us (with a tile for the sinks 161); 32768 tokens, 32 / 8 heads, window 4096: 1620 us, 1280 TFLOP/s of the pairs that are seen.
-// An item has ten key tiles there and costs 3 us beside them: the way from the last product over the output to the next item's first weights.
+// An item of the 12 prompts has nine key tiles (1075 keys) and costs 3 us beside them: the way from the last product over the output to the next item's first weights.
 //
 // Roles (384 threads): warp 0 loads Q, K and V by TMA (one ring for K and V, in the order of their use); warp 1 issues the MMAs and
 // owns TMEM; warp 2 writes zeros over the rows of a V tile behind the sequence's last key (a weight of zero times what lies
@@ -647,6 +647,8 @@ stream_status launch(const PromptGeom &g, const void *q, const void *k, const vo
     P.g = g;
     P.per_tile = kRows / g.hpg;
     const long long fit = kKvInL2 / ((long long)g.total_k * F::D * 4);
+    // (A window of some thousand keys has a working set that L2 holds whatever the length: all heads side by side, which is faster then: 32768 tokens, window 4096,
+    // 32 / 8 heads 1610 us, walked as the dense call does 1660. Windows beyond L2 lose by it: 131072 tokens, window 4096 the same, 16384 27.9 ms for 26.0, 65536 94 for 88, 131072 126 for 120.)
     P.heads = W || fit > g.G ? g.G : (int)(fit < 1 ? 1 : fit);
     CUtensorMap tq, tk, tv;
     stream_status rc = make_map_q(&tq, g, q, P.per_tile);

@@ -821,8 +821,8 @@ class PagedCache:
 class PagedCache8(PagedCache):
     """A paged key-value cache in 8 bits; see ``stream_cache8`` in stream.h.
 
-    ``k`` and ``v`` are float8_e4m3fn, ``k_scale`` and ``v_scale`` float32 ``[n_layers, n_pages, page_size / block, n_kv_heads]`` (any strides,
-    both alike): a key is its e4m3 numbers times its block's scale. ``dtype``: that of queries, outputs and new keys and values.
+    ``k`` and ``v`` are float8_e4m3fn, ``k_scale`` and ``v_scale`` float32 ``[n_layers, n_pages, page_size / block, n_kv_heads]`` (any positive
+    strides, both alike): a key is its e4m3 numbers times its block's scale. ``dtype``: that of queries, outputs and new keys and values.
     The rest, and the ``cache_*`` functions and :func:`decode_attention`, as for :class:`PagedCache`; :func:`new_cache8` makes an empty one."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, page_table: torch.Tensor, seq_len: torch.Tensor,
