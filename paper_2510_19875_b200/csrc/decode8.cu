@@ -23,7 +23,7 @@
 // rate (6556 GB/s), with head after head within a page 52 us, 80 %; the rest is the way to the first tile (4 us) and the joins. Tried: three CTAs an SM
 // with rings of two tiles (64 us), a prefetch of 256 bytes to L2 with each row (73), two kv heads whose rows lie side by side walked by one warp (57, but 36 for the
 // 64 slots, for 33, and 12.7 for 10 where one slot of 1219 is all: twice the registers, half the owners). 16 query heads a kv head (32 / 2 heads): 64 slots of up to 8192
-// tokens 28.9 us in bf16, d = 128, 63 in bf16, d = 256, 104 in fp32, d = 256, the last two with 0.7 to 1.6 KB of spilled registers a thread.
+// tokens 28.9 us in bf16, d = 128, 62 in bf16, d = 256, 107 in fp32, d = 256, the last two with 0.7 to 1.6 KB of spilled registers a thread.
 #include <cuda_fp16.h>
 
 #include "decode.cuh"
@@ -41,7 +41,6 @@ constexpr int kOpen = 3;
 constexpr float kOutgrown = 30.f;    // log2: of the sum's reference
 constexpr float kTop = 14.f;         // log2: a weight for the product where it is the largest, times its value's scale
 constexpr float kNone = -3e38f;      // a reference before the first key, finite so that it has differences
-constexpr float kAbsent = -1.f;      // in the place of the value's scale where a tile has no token; the key's is 0
 constexpr float kLeastScale = 7.8886090522101181e-31f;  // 2^-100: of a value's scale, for the reference (a smaller one, 0 or NaN counts as this there)
 
 template <class T, int D, int N>
@@ -76,6 +75,7 @@ struct Smem {
     uint2 q[kWarps][F::kQInRegs ? 1 : F::kParts * F::kPieces * N * 32];  // what a lane multiplies with
     float first[F::kFirstBeside ? kWarps - 1 : 1][F::kFirstBeside ? F::kLeave / 4 : 1];
     Piece piece[2 * kWarps];
+    unsigned there[kWarps][F::kStages];  // the keys of each place that are there
     int n_parts;   // that the first warp has left to the joins
 };
 
@@ -117,8 +117,8 @@ __device__ __forceinline__ float log2_of(float x) {
     asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
-__device__ __forceinline__ void cp_async4(unsigned dst, const void *src) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+__device__ __forceinline__ void cp_async4_or_zero(unsigned dst, const void *src, int bytes) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 
 // Four channels of a query head, as they lie in memory.
@@ -205,8 +205,8 @@ struct Walk {
         }
     }
 
-    // A tile: K, V behind it, then the keys' scales and the values'. Keys g, g + 8, g + 16 and g + 24 of it are this lane's.
-    __device__ __forceinline__ void step(const Smem<T, D, N> &sm, int warp, unsigned char *tile, int lane) {
+    // A tile: K, V behind it, then the keys' scales and the values'; the keys that it has tokens for. Keys g, g + 8, g + 16 and g + 24 of it are this lane's.
+    __device__ __forceinline__ void step(const Smem<T, D, N> &sm, int warp, unsigned char *tile, const unsigned *there, int lane) {
         const unsigned kt = wp::smem_addr(tile), vt = kt + F::kTile;
         const float *const z = reinterpret_cast<const float *>(tile + 2 * F::kTile);
         float s[N][2][4];
@@ -283,8 +283,8 @@ struct Walk {
 #pragma unroll
                     for (int n = 0; n < N; ++n) s[n][k >> 1][2 * (k & 1)] = s[n][k >> 1][2 * (k & 1) + 1] = -CUDART_INF_F;
                 }
-            const unsigned unset = __ballot_sync(0xffffffffu, z[lane] == 0.f && z[kStep + lane] != kAbsent);
-            if (unset != 0) {
+            const unsigned unset = __ballot_sync(0xffffffffu, z[lane] == 0.f) & *there;
+            if (unset != 0) {  // (what the tile has no token for is zeros)
 #pragma unroll
                 for (int i = 0; i < F::kPieces; ++i) {
                     const int at = (i * 32 + lane) * 16;
@@ -510,14 +510,9 @@ __global__ void __launch_bounds__(kThreads, Form<T, D, N>::kCtas) decode8_kernel
         const long long own = own_page >= 0 ? (long long)own_page * c.s_p + (long long)own_row * c.s_t : 0;
         const long long z = mine ? (long long)own_page * B.sc.s_p + (long long)B.block.quotient((unsigned)own_row) * B.sc.s_b + src.kvh * B.sc.s_h : 0;
         const unsigned to = ring + put * F::kPlace;
-        if (mine) {
-            cp_async4(to + 2 * F::kTile + lane * 4, B.sc.k + z);
-            cp_async4(to + 2 * F::kTile + kStep * 4 + lane * 4, B.sc.v + z);
-        } else {
-            float *const scales = reinterpret_cast<float *>(ring_ptr + put * F::kPlace + 2 * F::kTile);
-            scales[lane] = 0.f;
-            scales[kStep + lane] = kAbsent;
-        }
+        cp_async4_or_zero(to + 2 * F::kTile + lane * 4, B.sc.k + z, mine ? 4 : 0);
+        cp_async4_or_zero(to + 2 * F::kTile + kStep * 4 + lane * 4, B.sc.v + z, mine ? 4 : 0);
+        if (lane == 0) sm.there[warp][put] = there;
         const long long head = src.kvh * c.s_h + piece_l * 16;
         if (plain && there == 0xffffffffu) {
 #pragma unroll
@@ -618,7 +613,7 @@ __global__ void __launch_bounds__(kThreads, Form<T, D, N>::kCtas) decode8_kernel
             }
             wait_for<F::kStages - 1>(ahead - 1);  // copies that may still be on their way: those of later tiles
             __syncwarp();
-            walk.step(sm, warp, ring_ptr + take * F::kPlace, lane);
+            walk.step(sm, warp, ring_ptr + take * F::kPlace, &sm.there[warp][take], lane);
             __syncwarp();  // (the tile is read before its place is filled again)
             take = behind(take);
             --ahead;

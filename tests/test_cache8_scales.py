@@ -27,7 +27,7 @@ def test_tokens_whose_key_scale_is_zero_are_not_there(S, H, G, d, dtype, page, b
                 if s in (1, 3) or torch.rand(1, generator=gen) < 0.3:  # (two slots lose all of them)
                     p, r = led.table[s][b * block // page], b * block % page
                     cache.k_scale[0, p, r // block, g] = 0.0
-                    cache.v_scale[0, p, r // block, g] = (0.0, float("nan"), float("inf"), 1.0)[b % 4]
+                    cache.v_scale[0, p, r // block, g] = (0.0, float("nan"), float("inf"), 1.0, -1.0)[b % 5]
                     for x in (cache.k, cache.v):
                         x.view(torch.uint8)[0, p, r:r + block, g] = (NAN, 255, 126)[b % 3]
                     left[s][g][b * block:(b + 1) * block] = False
